@@ -69,6 +69,7 @@ typedef struct CUstream_st* gmc_stream_t; /* identical to cudaStream_t */
 #define GMC_STATUS_TIMEOUT 0x2u    /* a bounded device wait gave up; outputs are not valid */
 #define GMC_STATUS_TEXT_LEN 0x4u   /* text_offsets gave some T_b < 1 or T_b > T */
 #define GMC_STATUS_INTERNAL 0x8u   /* a device-side consistency check failed */
+#define GMC_STATUS_CACHE 0x10u     /* a cache's length, page number or new-row offset was out of range */
 
 /* Shape limits of this build (GMC_ERR_UNSUPPORTED beyond them). */
 #define GMC_MAX_N 8192            /* visual tokens per image */
@@ -79,6 +80,7 @@ typedef struct CUstream_st* gmc_stream_t; /* identical to cudaStream_t */
 #define GMC_MAX_N_LONG 16384      /* visual tokens per image on the long-prefix path */
 #define GMC_MAX_POOL_WIDE 4096    /* pool_mult * batch_b on the long-prefix path and gmc_select */
 #define GMC_MAX_RANK 256          /* rows of the long-prefix Rademacher map */
+#define GMC_MAX_CACHE_D 256       /* head size of a key-value cache */
 
 /*
  * Method constants.  gmc_default_params() fills the values of the paper's
@@ -497,6 +499,132 @@ int gmc_clients(const gmc_problem* prob, const gmc_params* params, const gmc_vie
                 const float* vo_probe, int N, int T, int H, int d, int D, int K,
                 float* out_clients, void* workspace, size_t ws_bytes, void* trace,
                 gmc_stream_t stream);
+
+/*
+ * The key-value cache after the boundary.  A compressed prompt (out_kv of
+ * gmc_compress, or a prefix layer's) goes on in a paged cache, from which the
+ * later tokens are prefilled and decoded.  The paper has no counterpart: these
+ * entry points serve the layers that run on the compressed rows.
+ *
+ * A pool holds num_pages pages of page_size slots, each slot one token's key
+ * (or value) of every key head.  Element x of slot `s` of page `p` and key head
+ * `h` is  k[p * page_stride + h * head_stride + s * slot_stride + x]  (likewise
+ * v, with the same strides), so [page][head][slot][d] and [page][slot][head][d]
+ * pools are both described.  Token j of sequence b lies in slot j % page_size
+ * of page page_table[b][j / page_size]; a page belongs to one sequence.
+ *
+ *   - lens[b] counts the tokens of sequence b, the new ones of the call
+ *     included: T_b new rows are tokens lens[b] - T_b .. lens[b] - 1.
+ *   - Slots from lens[b] on are never used, whatever they hold.
+ *   - max_len bounds every lens[b] (0: the table's max_pages * page_size); it
+ *     sizes launches and workspaces, so the nearer it is the better.
+ *   - status: NULL, or a DEVICE word that calls set GMC_STATUS_* bits of
+ *     (they never clear it).  A length below 0 or above max_len is clamped, a
+ *     page number outside the pool is neither read nor written, new-row
+ *     offsets out of range give a sequence no new rows: each sets
+ *     GMC_STATUS_CACHE, and the sequence's outputs are not valid.
+ * Requirements: d a multiple of 8 (bf16) or 4 (fp32), d <= GMC_MAX_CACHE_D
+ * (GMC_ERR_UNSUPPORTED beyond); k, v 16-byte aligned, strides multiples of 16
+ * bytes and non-negative (GMC_ERR_ARG).
+ */
+typedef struct gmc_kv_cache {
+  int B;                     /* sequences, >= 1 */
+  int Hkv, d;                /* key/value heads, head size */
+  int dtype;                 /* GMC_F32 or GMC_BF16: pools, queries, new rows and outputs */
+  int page_size, num_pages;  /* slots of a page, pages of the pool */
+  int max_pages;             /* columns of the page table */
+  int max_len;               /* bound on every lens[b], 0: max_pages * page_size */
+  int64_t page_stride, head_stride, slot_stride; /* elements */
+  void* k;
+  void* v;
+  const int32_t* page_table; /* DEVICE int32 [B][max_pages] */
+  int32_t* lens;             /* DEVICE int32 [B] (written by gmc_evict's destination only) */
+  uint32_t* status;          /* DEVICE word or NULL */
+} gmc_kv_cache;
+
+/*
+ * The attention of gmc_attend and gmc_decode.  The query at place i of a
+ * sequence sees key j when  j <= i  and  (window == 0 or i - j < window or
+ * j < sinks):  its own key and the window - 1 before it, and the first `sinks`
+ * keys of the sequence.  With x_j = scale * q . k_j over the seen keys,
+ *   out = sum_j exp(x_j) v_j / sum_j exp(x_j),   lse = log sum_j exp(x_j);
+ * a query that sees nothing gets out = 0, lse = -inf.  Query head h reads key
+ * head h / (H / Hkv).  Products accumulate in fp32, softmax statistics are
+ * fp32; with a bf16 cache gmc_attend may round the weights to bf16 for their
+ * product with v (gmc_decode does not).  Keys and values that a query does not
+ * see do not reach its output, whatever they hold.
+ */
+typedef struct gmc_attn {
+  int H;       /* query heads, a multiple of Hkv, H / Hkv <= 128 */
+  int window;  /* >= 0; 0: no window */
+  int sinks;   /* >= 0; ignored without a window */
+  float scale; /* 0: 1 / sqrt(d) */
+  int64_t q_row_stride, q_head_stride;     /* elements; 0, 0: dense [rows][H][d] */
+  int64_t out_row_stride, out_head_stride; /* elements; 0, 0: dense [rows][H][d] */
+} gmc_attn;
+
+/*
+ * gmc_cache_append -- new keys and values written to their pages.
+ *   k_new, v_new  [rows][Hkv][d], sequence after sequence; or v_new NULL and
+ *                 k_new in the layout of gmc_compress's out_kv: sequence b's
+ *                 T_b key rows, then its T_b value rows, from row 2 * offsets[b] on
+ *   offsets       DEVICE int32 [B+1], T_b = offsets[b+1] - offsets[b], 0 <= T_b <= T;
+ *                 or NULL: every sequence has T new rows
+ *   rows          rows of all sequences (offsets past it are out of range)
+ * One launch.  Rows whose place would lie before the sequence are dropped
+ * (GMC_STATUS_CACHE).
+ */
+int gmc_cache_append(const gmc_kv_cache* cache, const void* k_new, const void* v_new,
+                     const int32_t* offsets, int rows, int T, gmc_stream_t stream);
+
+/*
+ * gmc_attend -- causal attention of every sequence's T_b new tokens (already
+ * appended) over its cached keys, whole or through a window with sinks.
+ *   q        [rows][H][d] (strides in attn), sequence after sequence as q_offsets says
+ *   out      as q;  lse  fp32 [rows][H] or NULL
+ * q_offsets, rows, T: as offsets, rows, T of gmc_cache_append.  q and out
+ * 16-byte aligned, their strides multiples of 16 bytes.
+ */
+size_t gmc_attend_workspace_size(const gmc_kv_cache* cache, int H, int T);
+int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
+               const int32_t* q_offsets, int rows, int T, void* out, float* lse, void* workspace,
+               size_t ws_bytes, gmc_stream_t stream);
+
+/*
+ * gmc_decode -- one new token a sequence: its attention over the cached keys,
+ * the key at place lens[b] - 1 being its own.
+ *   q           [B][H][d] (strides in attn);  out as q;  lse fp32 [B][H] or NULL
+ *   k_new,v_new [B][Hkv][d]: appended at place lens[b] - 1 in the same launch
+ *               (and read from here); both NULL: the cache holds them already
+ *   scores      fp32 [B][Hkv][score_stride] or NULL: what every key has gathered so far
+ *   out_scores  out_scores[b][g][j] = scores[b][g][j] + the weight that key j
+ *               received, summed over the H / Hkv query heads of key head g, for
+ *               j < lens[b] (later entries are left alone); unseen keys receive
+ *               nothing, and a key appended by this call starts from 0.  May be
+ *               `scores` itself; both or neither are NULL.
+ */
+size_t gmc_decode_workspace_size(const gmc_kv_cache* cache, int H);
+int gmc_decode(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q, const void* k_new,
+               const void* v_new, void* out, float* lse, const float* scores, float* out_scores,
+               int64_t score_stride, void* workspace, size_t ws_bytes, gmc_stream_t stream);
+
+/*
+ * gmc_evict -- every key head of a sequence keeps the `keep` tokens with the
+ * largest scores (all of them where it holds no more): the first `sinks` and
+ * the last `recent` always, the others by score, equal scores by the lowest
+ * place, a NaN below every number.  The kept rows go, in ascending order, to
+ * places 0 .. of the sequence in `dst`, whose pages must not be among the
+ * sequence's in `src`; dst->lens[b] = min(keep, lens[b]) is written.
+ *   scores      fp32 [B][Hkv][score_stride]
+ *   out_idx     int32 [B][Hkv][keep]: the places kept, -1 after the last
+ *   out_scores  fp32 [B][Hkv][keep]: their scores, 0 after the last; may be NULL
+ * src and dst: the same B, Hkv, d and dtype; sinks + recent <= keep; dst must
+ * have room for `keep` tokens a sequence (GMC_ERR_ARG).  One launch.
+ */
+size_t gmc_evict_workspace_size(const gmc_kv_cache* src, int keep);
+int gmc_evict(const gmc_kv_cache* src, const gmc_kv_cache* dst, const float* scores,
+              int64_t score_stride, int keep, int sinks, int recent, int32_t* out_idx,
+              float* out_scores, void* workspace, size_t ws_bytes, gmc_stream_t stream);
 
 /*
  * gmc_selftest_bounded_wait -- checks the failure path of the bounded device

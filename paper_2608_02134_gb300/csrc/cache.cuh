@@ -1,0 +1,149 @@
+// The paged key-value cache as the kernels see it, and which keys a query sees.
+#pragma once
+
+#include "common.cuh"
+#include "kernels.cuh"
+
+namespace gmc {
+
+constexpr uint32_t CACHE_BAD = GMC_STATUS_CACHE;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// gmc_kv_cache by value; cap = the longest a sequence may be.
+struct KV {
+  char *k, *v;
+  const int32_t* table;
+  int32_t* lens;
+  uint32_t* status;
+  long long page_stride, head_stride, slot_stride;  // elements
+  int B, Hkv, d, ps, num_pages, max_pages, cap;
+};
+
+// Tokens of sequence b, clamped to what the cache can hold.
+__device__ __forceinline__ int kv_len(const KV& c, int b) {
+  const int n = c.lens[b];
+  if (n < 0 || n > c.cap) {
+    set_status(c.status, CACHE_BAD);
+    return n < 0 ? 0 : c.cap;
+  }
+  return n;
+}
+
+// Element offset of token j's row of key head h (the same in both pools), or -1
+// where the page table names a page outside the pool.
+__device__ __forceinline__ long long kv_row(const KV& c, int b, int h, int j) {
+  const unsigned p = (unsigned)j / (unsigned)c.ps, s = (unsigned)j - p * (unsigned)c.ps;
+  const int page = c.table[(long long)b * c.max_pages + p];
+  if ((unsigned)page >= (unsigned)c.num_pages) {
+    set_status(c.status, CACHE_BAD);
+    return -1;
+  }
+  return page * c.page_stride + h * c.head_stride + s * c.slot_stride;
+}
+
+// New rows of a sequence: rows [off, off + T) of the packed input.
+struct NewRows {
+  int off, T;
+};
+__device__ __forceinline__ NewRows new_rows(const int32_t* offsets, int b, int rows, int Tmax,
+                                            uint32_t* status) {
+  NewRows r;
+  if (!offsets) {
+    r.off = b * Tmax;
+    r.T = Tmax;
+    return r;
+  }
+  r.off = offsets[b];
+  r.T = offsets[b + 1] - r.off;
+  if (r.T < 0 || r.T > Tmax || r.off < 0 || (long long)r.off + r.T > rows) {
+    set_status(status, CACHE_BAD);
+    r.off = 0;
+    r.T = 0;
+  }
+  return r;
+}
+
+// The keys that the queries at places i0 .. i1 see between them: [0, a) and
+// [b0, b1), a <= b0 (a = 0 without sinks before the window).
+struct Seen {
+  int a, b0, b1;
+  __device__ __forceinline__ int count() const { return a + (b1 - b0); }
+  __device__ __forceinline__ int place(int x) const { return x < a ? x : x - a + b0; }
+};
+__device__ __forceinline__ Seen seen_keys(int i0, int i1, int window, int sinks) {
+  Seen s;
+  s.b1 = i1 + 1 > 0 ? i1 + 1 : 0;
+  s.b0 = window > 0 && i0 - window + 1 > 0 ? i0 - window + 1 : 0;
+  if (s.b0 > s.b1) s.b0 = s.b1;
+  s.a = window > 0 && sinks < s.b0 ? sinks : s.b0;
+  if (s.a == s.b0) {  // the sinks reach the window: one range
+    s.a = 0;
+    s.b0 = 0;
+  }
+  return s;
+}
+// 2^x (relative error 2^-22, ptx ex2.approx); 0 for x = -infinity.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ bool sees(int i, int j, int window, int sinks) {
+  return j <= i && (window == 0 || i - j < window || j < sinks);
+}
+
+struct AttnArgs {
+  KV c;
+  const char* q;
+  char* out;
+  float* lse;
+  const int32_t* q_offsets;
+  long long q_row, q_head, o_row, o_head;  // elements
+  int H, G, window, sinks, rows, T;
+  float scale2;  // scale * log2(e): softmax in powers of two
+  // a long key axis split over CTAs: partial sums [split][row][H][d], maxima and sums
+  int splits;
+  float* part;
+  float2* ml;  // [split][row][H]
+};
+
+cudaError_t launch_cache_append(const KV&, int dtype, const void* k_new, const void* v_new,
+                                const int32_t* offsets, int rows, int T, cudaStream_t);
+
+size_t attend_workspace(const KV&, int dtype, int H, int T);
+// The join of a split key axis (AttnArgs::part, ml).
+cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t);
+cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t, int* launches);
+
+struct DecodeArgs {
+  KV c;
+  const char *q, *k_new, *v_new;
+  char* out;
+  float* lse;
+  const float* scores;
+  float* out_scores;
+  long long score_stride;
+  long long q_row, q_head, o_row, o_head;
+  int H, G, window, sinks;
+  float scale2;
+  int h0;          // first query head of its key head in this launch
+  bool fresh;      // the appended key's score starts from 0
+  int chunk;       // seen keys of a split
+  float* logits;   // [B][Hkv][splits][heads][chunk] or NULL: kept in shared memory
+  int chunk_smem;
+};
+size_t decode_workspace(const KV&, int dtype, int H);
+cudaError_t launch_decode(DecodeArgs a, int dtype, void* ws, cudaStream_t, int* launches);
+
+struct EvictArgs {
+  KV src, dst;
+  const float* scores;
+  long long score_stride;
+  int keep, sinks, recent;
+  int32_t* out_idx;
+  float* out_scores;
+};
+cudaError_t launch_evict(const EvictArgs&, int dtype, cudaStream_t);
+
+}  // namespace gmc

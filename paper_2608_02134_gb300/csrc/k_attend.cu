@@ -1,0 +1,359 @@
+// Causal attention of new tokens over a paged key-value cache on the CUDA cores: fp32
+// caches, and bf16 ones whose shape the tensor-core kernel does not take.
+//
+// A CTA takes R rows, the query heads of one key head of some consecutive tokens (so
+// each key is read once for all of them), and walks the seen keys 64 at a time with a
+// running maximum and sum for every row.  A thread holds 8 (4 at d > 128) rows x 4
+// keys of the logits and 8 x 8 of the output in registers; queries, keys, values and
+// weights are fp32 in shared memory, read four at a time: 12 loads of 16 bytes per 128
+// multiply-adds, 16 per 256, which is what bounds it.  The keys' copies run behind the
+// products with the values and the values' behind the logits.  Where the rows are too
+// few to fill the GPU the keys are split over CTAs and a second kernel joins them.
+#include <algorithm>
+
+#include "cache.cuh"
+
+namespace gmc {
+
+namespace {
+constexpr int AT_THREADS = 256, AT_K = 64;
+constexpr int AT_MAX_SPLITS = 32;
+
+template <int DP> constexpr int at_rows() { return DP > 128 ? 64 : 128; }
+template <int DP> constexpr size_t at_smem() {
+  return (size_t)at_rows<DP>() * DP * 4 + 2 * (size_t)AT_K * DP * 4 + at_rows<DP>() * AT_K * 4 +
+         2 * AT_K * 8;
+}
+
+// o += weights x values of one tile; SKIP: zero weights are left out.
+template <int RT, int NC, bool SKIP>
+__device__ __forceinline__ void times_values(float (&o)[RT][NC * 4], const char* Pr,
+                                             const char* Vs, int tx, int sw) {
+#pragma unroll 1
+  for (int k4 = 0; k4 < AT_K / 4; ++k4) {
+    float4 pv[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+      pv[i] = *reinterpret_cast<const float4*>(Pr + i * AT_K * 4 + ((k4 ^ sw) * 16));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int k = k4 * 4 + e;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const float4 vv = *reinterpret_cast<const float4*>(Vs + k * (NC * 256) +
+                                                           (((tx + 16 * c) ^ (k & 7)) * 16));
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          const float p = e == 0 ? pv[i].x : e == 1 ? pv[i].y : e == 2 ? pv[i].z : pv[i].w;
+          if (SKIP && p == 0.f) continue;
+          o[i][4 * c + 0] = fmaf(p, vv.x, o[i][4 * c + 0]);
+          o[i][4 * c + 1] = fmaf(p, vv.y, o[i][4 * c + 1]);
+          o[i][4 * c + 2] = fmaf(p, vv.z, o[i][4 * c + 2]);
+          o[i][4 * c + 3] = fmaf(p, vv.w, o[i][4 * c + 3]);
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(AT_THREADS) k_attend_simt(AttnArgs a, int gsub, int ntile) {
+  constexpr int R = at_rows<DP>(), RT = R / 16, P = DP / 4, NC = DP / 64, E = 16 / sizeof(T);
+  extern __shared__ __align__(128) char smem[];
+  char* Qs = smem;
+  char* Ks = Qs + R * DP * 4;
+  char* Vs = Ks + AT_K * DP * 4;
+  char* Ps = Vs + AT_K * DP * 4;
+  long long* offs = reinterpret_cast<long long*>(Ps + R * AT_K * 4);  // [2][AT_K]
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  grid_dep_wait();
+  const int b = blockIdx.z;
+  const int ng = ceil_div(a.G, gsub);
+  const int h = blockIdx.y / ng, hg = (blockIdx.y - h * ng) * gsub;
+  const int split = blockIdx.x % a.splits;
+  const int tpt = R / gsub;
+  // the last tokens see the most keys: they go first
+  const int t0 = (ntile - 1 - (int)blockIdx.x / a.splits) * tpt;
+  const NewRows nr = new_rows(a.q_offsets, b, a.rows, a.T, a.c.status);
+  const int nt = min(tpt, nr.T - t0);
+  if (nt <= 0) return;
+  const int n = kv_len(a.c, b);
+  const int i0 = n - nr.T + t0;  // place of the first token of the tile
+  const Seen seen = seen_keys(i0, i0 + nt - 1, a.window, a.sinks);
+  const int na = ceil_div(seen.a, AT_K), nb = ceil_div(seen.b1 - seen.b0, AT_K);
+  const int per = ceil_div(na + nb, a.splits);
+  const int u0 = min(na + nb, split * per), u1 = min(na + nb, u0 + per);
+  auto key0 = [&](int u) { return u < na ? u * AT_K : seen.b0 + (u - na) * AT_K; };
+  auto key1 = [&](int u) { return u < na ? seen.a : seen.b1; };
+  auto look_up = [&](int u) {
+    if (tid < AT_K && u < u1) {
+      const int j = key0(u) + tid;
+      offs[(u & 1) * AT_K + tid] = j < key1(u) ? kv_row(a.c, b, h, j) : -1;
+    }
+  };
+  // one tile's rows into shared memory as fp32, piece p of row r at p ^ (r & 7)
+  auto copy_rows = [&](char* dst, const char* pool, int u) {
+    for (int x = tid; x < AT_K * (DP / E); x += AT_THREADS) {
+      const int r = x / (DP / E), p = x - r * (DP / E);
+      const long long o = offs[(u & 1) * AT_K + r];
+      const bool ok = o >= 0 && p * E < a.c.d;
+      const char* src = ok ? pool + o * (long long)sizeof(T) + p * 16 : pool;
+      if constexpr (sizeof(T) == 4) {
+        cp_async16(dst + r * DP * 4 + ((p ^ (r & 7)) * 16), src, ok);
+      } else {
+        int4 raw = make_int4(0, 0, 0, 0);
+        if (ok) raw = *reinterpret_cast<const int4*>(src);
+        const __nv_bfloat162* e = reinterpret_cast<const __nv_bfloat162*>(&raw);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const float2 lo = __bfloat1622float2(e[2 * q]), hi = __bfloat1622float2(e[2 * q + 1]);
+          *reinterpret_cast<float4*>(dst + r * DP * 4 + (((2 * p + q) ^ (r & 7)) * 16)) =
+              make_float4(lo.x, lo.y, hi.x, hi.y);
+        }
+      }
+    }
+    cp_async_commit();
+  };
+  look_up(u0);
+  for (int x = tid; x < R * P; x += AT_THREADS) {
+    const int r = x / P, p = x - r * P;
+    const int t = r / gsub, g = hg + r - t * gsub;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (t < nt && g < a.G && p * 4 < a.c.d) {
+      const T* q = reinterpret_cast<const T*>(a.q) + (long long)(nr.off + t0 + t) * a.q_row +
+                   (long long)(h * a.G + g) * a.q_head + p * 4;
+      v = make_float4(to_f32(q[0]), to_f32(q[1]), to_f32(q[2]), to_f32(q[3]));
+    }
+    *reinterpret_cast<float4*>(Qs + r * DP * 4 + ((p ^ ((r / RT) & 7)) * 16)) = v;
+  }
+  __syncthreads();
+  if (u0 < u1) copy_rows(Ks, a.c.k, u0);
+
+  float o[RT][NC * 4], m[RT], l[RT];
+  int place[RT];  // of the row's token; below 0 also for rows that are none
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    const int r = ty * RT + i, t = r / gsub;
+    place[i] = t < nt ? i0 + t : -1;
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+#pragma unroll
+    for (int y = 0; y < NC * 4; ++y) o[i][y] = 0.f;
+  }
+  const int sw = ty & 7;
+  for (int u = u0; u < u1; ++u) {
+    cp_async_wait<0>();
+    look_up(u + 1);
+    __syncthreads();  // the keys of u are there; the values of u - 1 are done with
+    copy_rows(Vs, a.c.v, u);
+    float s[RT][4];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[i][c] = 0.f;
+#pragma unroll 2
+    for (int p = 0; p < P; ++p) {
+      float4 kv[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int r = tx + 16 * c;
+        kv[c] = *reinterpret_cast<const float4*>(Ks + r * DP * 4 + ((p ^ (r & 7)) * 16));
+      }
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const float4 qv =
+            *reinterpret_cast<const float4*>(Qs + (ty * RT + i) * DP * 4 + ((p ^ sw) * 16));
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          s[i][c] = fmaf(qv.x, kv[c].x,
+                         fmaf(qv.y, kv[c].y, fmaf(qv.z, kv[c].z, fmaf(qv.w, kv[c].w, s[i][c]))));
+      }
+    }
+    const int j0 = key0(u), j1 = key1(u);
+    // whether every row sees every key of the tile
+    const bool whole = j0 + AT_K <= j1 && j0 + AT_K - 1 <= i0 &&
+                       (a.window == 0 || i0 + nt - 1 - j0 < a.window || j0 + AT_K <= a.sinks);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int j = j0 + tx + 16 * c;
+        const bool ok = whole || (j < j1 && sees(place[i], j, a.window, a.sinks));
+        s[i][c] = ok ? s[i][c] * a.scale2 : -INFINITY;
+        mx = fmaxf(mx, s[i][c]);
+      }
+#pragma unroll
+      for (int w = 1; w < 16; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, w));
+      const float mn = fmaxf(m[i], mx), base = mn == -INFINITY ? 0.f : mn;
+      const float f = exp2_fast(m[i] - base);
+      m[i] = mn;
+      float sum = 0.f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float p = exp2_fast(s[i][c] - base);
+        sum += p;
+        const int k = tx + 16 * c;
+        *reinterpret_cast<float*>(Ps + (ty * RT + i) * AT_K * 4 + (((k >> 2) ^ sw) * 16) +
+                                  (k & 3) * 4) = p;
+      }
+      l[i] = l[i] * f + sum;
+#pragma unroll
+      for (int y = 0; y < NC * 4; ++y) o[i][y] *= f;
+    }
+    __syncthreads();  // the keys of u are done with, the weights written
+    if (u + 1 < u1) copy_rows(Ks, a.c.k, u + 1); else cp_async_commit();
+    cp_async_wait<1>();
+    __syncthreads();  // the values of u are there
+    // a weight of zero does not meet a value that is not finite: a row that does not
+    // see a key must not take a NaN from it
+    bool strange = false;
+    if (!whole) {
+      for (int x = tid; x < AT_K * P; x += AT_THREADS) {
+        const float4 v = reinterpret_cast<const float4*>(Vs)[x];
+        strange |= !(fabsf(v.x) < INFINITY && fabsf(v.y) < INFINITY && fabsf(v.z) < INFINITY &&
+                     fabsf(v.w) < INFINITY);
+      }
+      strange = __syncthreads_or(strange);
+    }
+    if (!strange)
+      times_values<RT, NC, false>(o, Ps + ty * RT * AT_K * 4, Vs, tx, sw);
+    else
+      times_values<RT, NC, true>(o, Ps + ty * RT * AT_K * 4, Vs, tx, sw);
+  }
+  cp_async_wait<0>();
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    float L = l[i];
+#pragma unroll
+    for (int w = 1; w < 16; w <<= 1) L += __shfl_xor_sync(FULL, L, w);
+    const int r = ty * RT + i, t = r / gsub, g = hg + r - t * gsub;
+    if (t >= nt || g >= a.G) continue;
+    const long long row = nr.off + t0 + t;
+    const int hq = h * a.G + g;
+    if (a.splits > 1) {
+      const long long pr = ((long long)split * a.rows + row) * a.H + hq;
+      if (tx == 0) a.ml[pr] = make_float2(m[i], L);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int x = (tx + 16 * c) * 4;
+        if (x < a.c.d)
+          *reinterpret_cast<float4*>(a.part + pr * a.c.d + x) =
+              make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
+      }
+      continue;
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    if (a.lse && tx == 0)
+      a.lse[row * a.H + hq] = L == 0.f ? -INFINITY : (m[i] + log2f(L)) * LN2;
+    T* out = reinterpret_cast<T*>(a.out) + row * a.o_row + hq * a.o_head;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int x = (tx + 16 * c) * 4 + e;
+        if (x < a.c.d) out[x] = from_f32<T>(o[i][4 * c + e] * inv);
+      }
+  }
+}
+
+// One warp a (row, query head): out = sum_s w_s part_s / sum_s w_s l_s, w_s = 2^(m_s - max m).
+template <typename T>
+__global__ void __launch_bounds__(256) k_attend_join(AttnArgs a) {
+  grid_dep_wait();
+  const int lane = threadIdx.x & 31;
+  const long long x = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (x >= (long long)a.rows * a.H) return;
+  const long long row = x / a.H;
+  const int hq = (int)(x - row * a.H);
+  const long long step = (long long)a.rows * a.H;
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (lane < a.splits) ml = a.ml[lane * step + x];
+  const float M = warp_max(ml.x), base = M == -INFINITY ? 0.f : M;
+  const float w = exp2_fast(ml.x - base);
+  const float L = warp_sum(ml.y * w);
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  if (a.lse && lane == 0) a.lse[x] = L == 0.f ? -INFINITY : (base + log2f(L)) * LN2;
+  T* out = reinterpret_cast<T*>(a.out) + row * a.o_row + hq * a.o_head;
+  for (int y0 = 0; y0 < a.c.d; y0 += 128) {
+    const int y = y0 + lane * 4;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int q = 0; q < a.splits; ++q) {
+      const float mq = __shfl_sync(FULL, ml.x, q), f = __shfl_sync(FULL, w, q);
+      if (mq == -INFINITY || y >= a.c.d) continue;  // a part without keys wrote no row
+      const float4 v = *reinterpret_cast<const float4*>(a.part + (q * step + x) * a.c.d + y);
+      s.x += f * v.x;
+      s.y += f * v.y;
+      s.z += f * v.z;
+      s.w += f * v.w;
+    }
+    if (y < a.c.d) {
+      out[y] = from_f32<T>(s.x * inv);
+      out[y + 1] = from_f32<T>(s.y * inv);
+      out[y + 2] = from_f32<T>(s.z * inv);
+      out[y + 3] = from_f32<T>(s.w * inv);
+    }
+  }
+}
+
+int simt_rows(int d) { return d > 128 ? 64 : 128; }
+
+// Parts of the key axis: where the rows' tiles leave SMs idle, as many as fill them,
+// four turns of 64 keys each at least.
+int simt_splits(const KV& c, int G, int T) {
+  const int R = simt_rows(c.d), gsub = std::min(G, R);
+  const long long ctas =
+      (long long)c.B * c.Hkv * ceil_div(G, gsub) * ceil_div(T, std::max(1, R / gsub));
+  if (ctas >= 152) return 1;
+  return (int)std::max<long long>(
+      1, std::min<long long>({152 / ctas, AT_MAX_SPLITS, ceil_div(c.cap, 4 * AT_K)}));
+}
+}  // namespace
+
+size_t attend_workspace(const KV& c, int dtype, int H, int T) {
+  const int s = simt_splits(c, H / c.Hkv, T);
+  if (s == 1) return 256;
+  const size_t rows = (size_t)c.B * T * H * s;
+  return 256 + ((rows * 8 + 255) & ~(size_t)255) + rows * c.d * 4;
+}
+
+cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t st) {
+  const unsigned grid = (unsigned)(((long long)a.rows * a.H + 7) / 8);
+  return dtype == GMC_BF16
+             ? launch_k(k_attend_join<__nv_bfloat16>, dim3(grid), dim3(256), 0, st, 1, a)
+             : launch_k(k_attend_join<float>, dim3(grid), dim3(256), 0, st, 1, a);
+}
+
+cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t st, int* launches) {
+  const int R = simt_rows(a.c.d), gsub = std::min(a.G, R), ng = ceil_div(a.G, gsub);
+  const int ntile = ceil_div(a.T, R / gsub);
+  a.splits = simt_splits(a.c, a.G, a.T);
+  if (a.splits > 1) {
+    const size_t rows = (size_t)a.c.B * a.T * a.H * a.splits;
+    a.ml = reinterpret_cast<float2*>(ws);
+    a.part = reinterpret_cast<float*>((char*)ws + ((rows * 8 + 255) & ~(size_t)255));
+  }
+  const dim3 grid((unsigned)ntile * a.splits, a.c.Hkv * ng, a.c.B);
+  cudaError_t e;
+#define GMC_AT(T, DP)                                                                     \
+  ((e = set_smem_limit((const void*)k_attend_simt<T, DP>, at_smem<DP>())) != cudaSuccess  \
+       ? e                                                                                \
+       : launch_k(k_attend_simt<T, DP>, grid, dim3(AT_THREADS), at_smem<DP>(), st, 1, a,  \
+                  gsub, ntile))
+  if (dtype == GMC_BF16)
+    e = a.c.d <= 64 ? GMC_AT(__nv_bfloat16, 64)
+                    : a.c.d <= 128 ? GMC_AT(__nv_bfloat16, 128) : GMC_AT(__nv_bfloat16, 256);
+  else
+    e = a.c.d <= 64 ? GMC_AT(float, 64)
+                    : a.c.d <= 128 ? GMC_AT(float, 128) : GMC_AT(float, 256);
+#undef GMC_AT
+  if (e != cudaSuccess) return e;
+  ++*launches;
+  if (a.splits > 1) {
+    if ((e = launch_attend_join(a, dtype, st)) != cudaSuccess) return e;
+    ++*launches;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace gmc

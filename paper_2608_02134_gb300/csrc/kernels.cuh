@@ -247,6 +247,7 @@ namespace gmc {
 // Raise a kernel's dynamic shared-memory limit when a launch needs more than
 // the 48 KB default (idempotent; remembers the largest value set per kernel).
 cudaError_t set_smem_limit(const void* func, size_t bytes);
+void count_launches(int n);  // adds to gmc_launch_count()
 }  // namespace gmc
 
 namespace gmc {

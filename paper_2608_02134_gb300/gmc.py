@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_PKG, "libgmc.so")
 GMC_OK, GMC_ERR_ARG, GMC_ERR_UNSUPPORTED, GMC_ERR_WORKSPACE, GMC_ERR_CUDA = range(5)
 GMC_F32, GMC_BF16 = 0, 1
 STATUS_NONFINITE, STATUS_TIMEOUT, STATUS_TEXT_LEN, STATUS_INTERNAL = 0x1, 0x2, 0x4, 0x8
+STATUS_CACHE = 0x10
 
 EXPORTS = (
     "gmc_default_params", "gmc_workspace_size", "gmc_compress", "gmc_get_trace_layout",
@@ -29,7 +30,8 @@ EXPORTS = (
     "gmc_transport_noalloc", "gmc_cosine_workspace_size", "gmc_cosine",
     "gmc_workspace_size_views", "gmc_compress_views", "gmc_clients", "gmc_selftest_bounded_wait",
     "gmc_compress_ex", "gmc_workspace_size_long", "gmc_compress_long", "gmc_clients_long",
-    "gmc_compress_host",
+    "gmc_compress_host", "gmc_cache_append", "gmc_attend_workspace_size", "gmc_attend",
+    "gmc_decode_workspace_size", "gmc_decode", "gmc_evict_workspace_size", "gmc_evict",
 )
 MAX_VIEWS = 4
 MAX_PREFIX_LAYERS = 64
@@ -83,6 +85,25 @@ class PrefixKV(ctypes.Structure):
 class LongPrefix(ctypes.Structure):
     _fields_ = [("rank", ctypes.c_int), ("max_clients", ctypes.c_int),
                 ("rademacher", ctypes.c_void_p)]
+
+
+class CacheStruct(ctypes.Structure):
+    """gmc_kv_cache."""
+    _fields_ = [("B", ctypes.c_int), ("Hkv", ctypes.c_int), ("d", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("page_size", ctypes.c_int), ("num_pages", ctypes.c_int),
+                ("max_pages", ctypes.c_int), ("max_len", ctypes.c_int),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("slot_stride", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("status", ctypes.c_void_p)]
+
+
+class Attn(ctypes.Structure):
+    """gmc_attn."""
+    _fields_ = [("H", ctypes.c_int), ("window", ctypes.c_int), ("sinks", ctypes.c_int),
+                ("scale", ctypes.c_float), ("q_row_stride", ctypes.c_int64),
+                ("q_head_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64),
+                ("out_head_stride", ctypes.c_int64)]
 
 
 class TraceHeader(ctypes.Structure):
@@ -179,6 +200,21 @@ def lib() -> ctypes.CDLL:
     L.gmc_clients_long.restype = i
     L.gmc_selftest_bounded_wait.argtypes = [ctypes.c_longlong, vp, sz, vp]
     L.gmc_selftest_bounded_wait.restype = i
+    C, A, i64 = ctypes.POINTER(CacheStruct), ctypes.POINTER(Attn), ctypes.c_int64
+    L.gmc_cache_append.argtypes = [C, vp, vp, vp, i, i, vp]
+    L.gmc_cache_append.restype = i
+    L.gmc_attend_workspace_size.argtypes = [C, i, i]
+    L.gmc_attend_workspace_size.restype = sz
+    L.gmc_attend.argtypes = [C, A, vp, vp, i, i, vp, vp, vp, sz, vp]
+    L.gmc_attend.restype = i
+    L.gmc_decode_workspace_size.argtypes = [C, i]
+    L.gmc_decode_workspace_size.restype = sz
+    L.gmc_decode.argtypes = [C, A, vp, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp]
+    L.gmc_decode.restype = i
+    L.gmc_evict_workspace_size.argtypes = [C, i]
+    L.gmc_evict_workspace_size.restype = sz
+    L.gmc_evict.argtypes = [C, C, vp, i64, i, i, i, vp, vp, vp, sz, vp]
+    L.gmc_evict.restype = i
     _lib = L
     return L
 
@@ -430,6 +466,163 @@ def profile_read() -> dict:
 
 def launch_count() -> int:
     return int(lib().gmc_launch_count())
+
+
+# ---------------------------------------------------------------------------
+# The key-value cache after the boundary (include/gmc.h, gmc_kv_cache)
+# ---------------------------------------------------------------------------
+_DTYPES = {torch.float32: GMC_F32, torch.bfloat16: GMC_BF16}
+
+
+class KVCache:
+    """A paged key-value cache: pools k, v [pages, Hkv, page_size, d] (any strides with
+    unit-stride rows, the same for both: a permuted view of [pages, page_size, Hkv, d]
+    pools will do), page_table int32 [B, max_pages], lens int32 [B], on the device.
+    max_len bounds the lengths (0: the table's room); status: an int32 device word that
+    calls set STATUS_CACHE in, or None.  Holds the tensors; reads nothing."""
+
+    def __init__(self, k, v, page_table, lens, max_len=0, status=None):
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1 \
+                or k.dtype != v.dtype or k.dtype not in _DTYPES:
+            raise GMCError("cache pools: two [pages, Hkv, page_size, d] tensors alike, fp32 or "
+                           "bf16, with unit-stride rows")
+        if page_table.dim() != 2 or page_table.dtype != torch.int32 \
+                or lens.dtype != torch.int32 or lens.numel() != page_table.shape[0] \
+                or not page_table.is_contiguous() or not lens.is_contiguous():
+            raise GMCError("cache: page_table int32 [B, max_pages] and lens int32 [B], dense")
+        if status is not None and status.element_size() != 4:
+            raise GMCError("cache: status is one 32-bit device word")
+        if any(not t.is_cuda for t in (k, v, page_table, lens)):
+            raise GMCError("cache: every tensor lies on the device")
+        self.k, self.v, self.page_table, self.lens, self.status = k, v, page_table, lens, status
+        self.B, self.max_pages = page_table.shape
+        self.num_pages, self.Hkv, self.page_size, self.d = k.shape
+        self.max_len, self.dtype = max_len, k.dtype
+        self.struct = CacheStruct(
+            self.B, self.Hkv, self.d, _DTYPES[k.dtype], self.page_size, self.num_pages,
+            self.max_pages, max_len, k.stride(0), k.stride(1), k.stride(2), k.data_ptr(),
+            v.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
+            None if status is None else status.data_ptr())
+        self.ref = ctypes.byref(self.struct)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _stream_handle(stream):
+    return stream.cuda_stream if stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+def _check_int32(t, n, what):
+    if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n):
+        raise GMCError(what)
+
+
+def _check_f32(t, n, what):
+    if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n):
+        raise GMCError(what)
+
+
+def _check_scores(cache, t):
+    if t.dtype != torch.float32 or t.dim() != 3 or t.shape[0] != cache.B \
+            or t.shape[1] != cache.Hkv or not t.is_contiguous():
+        raise GMCError("scores: dense fp32 [B, Hkv, places]")
+
+
+def _attn(cache, q, out, window, sinks, scale):
+    if q.dim() != 3 or q.shape != out.shape or q.dtype != cache.dtype or out.dtype != cache.dtype \
+            or q.shape[2] != cache.d or q.stride(2) != 1 or out.stride(2) != 1:
+        raise GMCError("queries and outputs: [rows, H, d] of the cache's type, unit-stride rows")
+    return Attn(q.shape[1], window, sinks, scale or 0.0, q.stride(0), q.stride(1), out.stride(0),
+                out.stride(1))
+
+
+def cache_append(cache: KVCache, k_new, v_new, T, offsets=None, stream=None):
+    """gmc_cache_append: k_new, v_new [rows, Hkv, d], T new rows a sequence (the most of a
+    ragged call, whose offsets is int32 [B+1]); v_new None: k_new is laid out as
+    gmc_compress's out_kv, [2 * rows, Hkv, d]."""
+    rows = k_new.shape[0] if v_new is not None else k_new.shape[0] // 2
+    for t in (k_new, v_new):
+        if t is not None and (t.dtype != cache.dtype or t.dim() != 3 or not t.is_contiguous()
+                              or tuple(t.shape[1:]) != (cache.Hkv, cache.d)):
+            raise GMCError("new rows: dense [rows, Hkv, d] of the cache's type")
+    if v_new is not None and v_new.shape[0] != rows:
+        raise GMCError("new rows: as many values as keys")
+    _check_int32(offsets, cache.B + 1, "offsets: dense int32 [B + 1]")
+    _check(lib().gmc_cache_append(cache.ref, _addr(k_new), _addr(v_new), _addr(offsets), rows, T,
+                                  _stream_handle(stream)))
+
+
+def attend_workspace_size(cache: KVCache, H, T) -> int:
+    return int(lib().gmc_attend_workspace_size(cache.ref, H, T))
+
+
+def attend(cache: KVCache, q, out, T, q_offsets=None, window=0, sinks=0, scale=None, lse=None,
+           workspace=None, stream=None):
+    """gmc_attend: causal attention of the new tokens q [rows, H, d] into out (and lse fp32
+    [rows, H]); T new tokens a sequence (the most of a ragged call, whose q_offsets is
+    int32 [B+1]).  scale None: 1 / sqrt(d)."""
+    a = _attn(cache, q, out, window, sinks, scale)
+    rows = q.shape[0]
+    _check_int32(q_offsets, cache.B + 1, "q_offsets: dense int32 [B + 1]")
+    _check_f32(lse, rows * a.H, "lse: dense fp32 [rows, H]")
+    if workspace is None:
+        workspace = alloc_workspace(attend_workspace_size(cache, a.H, T), q.device)
+    _check(lib().gmc_attend(cache.ref, ctypes.byref(a), q.data_ptr(), _addr(q_offsets), rows, T,
+                            out.data_ptr(), _addr(lse), workspace.data_ptr(), workspace.numel(),
+                            _stream_handle(stream)))
+
+
+def decode_workspace_size(cache: KVCache, H) -> int:
+    return int(lib().gmc_decode_workspace_size(cache.ref, H))
+
+
+def decode(cache: KVCache, q, out, k_new=None, v_new=None, window=0, sinks=0, scale=None, lse=None,
+           scores=None, out_scores=None, workspace=None, stream=None):
+    """gmc_decode: one new token a sequence, q [B, H, d] into out (and lse fp32 [B, H]).
+    k_new, v_new [B, Hkv, d]: appended at place lens - 1 on the way.  scores, out_scores
+    fp32 [B, Hkv, places]: out_scores = scores + the weight every key received (the
+    same tensor will do)."""
+    a = _attn(cache, q, out, window, sinks, scale)
+    if q.shape[0] != cache.B:
+        raise GMCError("decode: one query row a sequence")
+    for t in (k_new, v_new):
+        if t is not None and (t.dtype != cache.dtype or not t.is_contiguous()
+                              or tuple(t.shape) != (cache.B, cache.Hkv, cache.d)):
+            raise GMCError("new rows: dense [B, Hkv, d] of the cache's type")
+    _check_f32(lse, cache.B * a.H, "lse: dense fp32 [B, H]")
+    places = 0
+    if scores is not None:
+        _check_scores(cache, scores)
+        if out_scores is None or out_scores.shape != scores.shape:
+            raise GMCError("decode: scores and out_scores alike")
+        _check_scores(cache, out_scores)
+        places = scores.shape[2]
+    if workspace is None:
+        workspace = alloc_workspace(decode_workspace_size(cache, a.H), q.device)
+    _check(lib().gmc_decode(cache.ref, ctypes.byref(a), q.data_ptr(), _addr(k_new), _addr(v_new),
+                            out.data_ptr(), _addr(lse), _addr(scores), _addr(out_scores), places,
+                            workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+
+
+def evict_workspace_size(cache: KVCache, keep) -> int:
+    return int(lib().gmc_evict_workspace_size(cache.ref, keep))
+
+
+def evict(src: KVCache, dst: KVCache, scores, keep, out_idx, out_scores=None, sinks=0, recent=0,
+          workspace=None, stream=None):
+    """gmc_evict: every key head keeps its `keep` best-scored rows (the first `sinks` and
+    the last `recent` always), moved to the pages of dst in ascending order; out_idx
+    int32 [B, Hkv, keep], out_scores fp32 [B, Hkv, keep] or None.  Writes dst.lens."""
+    _check_scores(src, scores)
+    _check_int32(out_idx, src.B * src.Hkv * keep, "out_idx: dense int32 [B, Hkv, keep]")
+    _check_f32(out_scores, src.B * src.Hkv * keep, "out_scores: dense fp32 [B, Hkv, keep]")
+    if workspace is None:
+        workspace = alloc_workspace(evict_workspace_size(src, keep), scores.device)
+    _check(lib().gmc_evict(src.ref, dst.ref, scores.data_ptr(), scores.shape[2], keep, sinks,
+                           recent, out_idx.data_ptr(), _addr(out_scores), workspace.data_ptr(),
+                           workspace.numel(), _stream_handle(stream)))
 
 
 # ---------------------------------------------------------------------------
