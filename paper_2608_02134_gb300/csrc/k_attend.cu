@@ -311,7 +311,8 @@ int simt_splits(const KV& c, int G, int T) {
 }  // namespace
 
 size_t attend_workspace(const KV& c, int dtype, int H, int T) {
-  const int s = simt_splits(c, H / c.Hkv, T);
+  const int G = H / c.Hkv;
+  const int s = attend_tc_takes(c, dtype, G) ? attend_tc_splits(c, G, T) : simt_splits(c, G, T);
   if (s == 1) return 256;
   const size_t rows = (size_t)c.B * T * H * s;
   return 256 + ((rows * 8 + 255) & ~(size_t)255) + rows * c.d * 4;
@@ -327,7 +328,8 @@ cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t st) {
 cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t st, int* launches) {
   const int R = simt_rows(a.c.d), gsub = std::min(a.G, R), ng = ceil_div(a.G, gsub);
   const int ntile = ceil_div(a.T, R / gsub);
-  a.splits = simt_splits(a.c, a.G, a.T);
+  const bool tensor = attend_tc_takes(a.c, dtype, a.G);
+  a.splits = tensor ? attend_tc_splits(a.c, a.G, a.T) : simt_splits(a.c, a.G, a.T);
   if (a.splits > 1) {
     const size_t rows = (size_t)a.c.B * a.T * a.H * a.splits;
     a.ml = reinterpret_cast<float2*>(ws);
@@ -340,7 +342,9 @@ cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t st, int*
        ? e                                                                                \
        : launch_k(k_attend_simt<T, DP>, grid, dim3(AT_THREADS), at_smem<DP>(), st, 1, a,  \
                   gsub, ntile))
-  if (dtype == GMC_BF16)
+  if (tensor)
+    e = launch_attend_tc(a, st);
+  else if (dtype == GMC_BF16)
     e = a.c.d <= 64 ? GMC_AT(__nv_bfloat16, 64)
                     : a.c.d <= 128 ? GMC_AT(__nv_bfloat16, 128) : GMC_AT(__nv_bfloat16, 256);
   else

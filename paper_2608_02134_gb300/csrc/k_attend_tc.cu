@@ -1,0 +1,672 @@
+// Causal attention of new tokens over a paged key-value cache on the tcgen05 tensor
+// cores: bf16 caches with d <= 128.
+//
+// A CTA takes two tiles of up to 128 rows, a row being one query head of one token:
+// the G query heads of a key head and 128 / G consecutive tokens make a tile, so each
+// key and value is read once for all of them.  It walks the seen keys 128 at a time
+// (whole pages where they are smaller).  One warp copies keys and values by TMA into a
+// ring of five 128-row slots, one thread issues the products
+//     S = Q K^T   (128 x 128, fp32 in tensor memory)
+//     O += P V    (P bf16 in tensor memory over S's columns, V as the MN-major operand)
+// and a warpgroup a tile turns S into P: a thread holds a row's 128 logits, so maxima
+// and sums need no exchange.  The two tiles alternate: while one's logits become
+// weights the tensor cores work for the other.  The maximum that weights are taken
+// against follows the running one only when it has grown by 2^8 (weights up to 256
+// lose nothing in bf16 or fp32), so the output in tensor memory is hardly ever
+// rescaled.
+//
+// Weights are rounded to bf16 for their product with V (relative 2^-8, the same as the
+// output's own rounding); sums, maxima and products are fp32.
+//
+// Rows of a tile that do not see a key give it the weight 0.  Slots past the sequence's
+// end are zeroed in shared memory before the product reads them; where a tile of keys
+// is seen by some rows only, its values are looked over, and if one is not finite
+// (0 x NaN would reach rows that do not see it) the CTA computes its rows again one by
+// one, each from the keys that it sees.
+//
+// Every wait is bounded (about two seconds); on timeout GMC_STATUS_TIMEOUT is set in
+// the cache's status word, copies and products in flight are drained and tensor memory
+// is freed.
+#include <algorithm>
+
+#include "cache.cuh"
+#include "tc.cuh"
+
+namespace gmc {
+
+namespace {
+constexpr int TM = 128;                 // rows of a tile, keys of a turn
+constexpr int T_THREADS = 320;          // 2 x 4 softmax warps, a copying and an issuing one
+constexpr long long T_WAIT = 4000000000LL;
+constexpr float GROWN = 8.f;            // powers of two the maximum may fall behind
+
+template <int DP> constexpr int t_slots() { return DP == 128 ? 5 : 8; }
+
+struct TCtl {
+  uint64_t full[8], empty[8], qfull, sfull[2], pfull[2], drained;
+  uint32_t tmem;
+  volatile int abort;
+  int strange;
+};
+
+template <int DP> constexpr size_t t_smem() {
+  return 1024 + (size_t)(2 + t_slots<DP>()) * TM * DP * 2 + sizeof(TCtl);
+}
+
+// Turns of keys: pages of up to 128 slots are taken as many as fit whole, larger ones
+// in pieces of 128 (the last one short).
+struct Turns {
+  int ps, kt, ppt, tpp;
+  __device__ __forceinline__ int of(int j) const {  // the turn that holds place j
+    if (ps <= TM) return j / kt;
+    const int p = j / ps;
+    return p * tpp + (j - p * ps) / TM;
+  }
+  __device__ __forceinline__ int first(int u) const {
+    if (ps <= TM) return u * kt;
+    const int p = u / tpp;
+    return p * ps + (u - p * tpp) * TM;
+  }
+  __device__ __forceinline__ int rows(int u) const {
+    if (ps <= TM) return kt;
+    return min(TM, ps - (u - u / tpp * tpp) * TM);
+  }
+};
+
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  if (tc::mbar_try_wait(bar, parity)) return true;
+  const long long end = clock64() + T_WAIT;
+  while (!tc::mbar_try_wait(bar, parity)) {
+    if (*abort || clock64() > end) {
+      *abort = 1;
+      return false;
+    }
+  }
+  return true;
+}
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z,
+                                            uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(tc::smem_u32(dst)),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(tc::smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z,
+                                            int w, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(tc::smem_u32(dst)),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(tc::smem_u32(bar))
+      : "memory");
+}
+
+// D[tmem] (+)= A[tmem] * B[smem], bf16 inputs, fp32 accumulate.
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// MN-major operand stored as rows of 64 elements (128 bytes, 128-byte swizzle), one row
+// a k: 8-row groups 1024 bytes apart along k, 64-element blocks `block` bytes apart.
+__device__ __forceinline__ uint64_t desc_sw128_mnmajor(uint32_t addr, uint32_t block) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(block >> 4) << 16;   // leading byte offset: between 64-element blocks
+  d |= (uint64_t)(1024 >> 4) << 32;    // stride byte offset: between groups of 8 k
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+// 64 consecutive fp32 columns of this warp's lanes (one row a thread), waited for.
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
+        "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]),
+        "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]),
+        "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]),
+        "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]),
+        "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr)
+      : "memory");
+}
+// 32 columns of 32 bits, without the wait.
+__device__ __forceinline__ void tmem_st32_async(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(
+          taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+      "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+      "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() {
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// One row from the keys that it sees alone, a warp a row: the CTAs whose values hold
+// infinities or NaN that some of their rows do not see.
+__device__ __noinline__ void row_alone(const AttnArgs& a, int b, int h, long long row, int hq,
+                                       int place, int j0, int j1, float* m_, float* l_,
+                                       float o[4]) {
+  const int lane = threadIdx.x & 31, x = lane * 4;
+  float q[4] = {0.f, 0.f, 0.f, 0.f};
+  if (x < a.c.d) {
+    const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(a.q) + row * a.q_row +
+                             (long long)hq * a.q_head + x;
+    for (int e = 0; e < 4; ++e) q[e] = to_f32(p[e]);
+  }
+  float m = *m_, l = *l_;
+  for (int j = j0; j < j1; ++j) {
+    if (!sees(place, j, a.window, a.sinks)) continue;
+    const long long off = kv_row(a.c, b, h, j);
+    if (off < 0) continue;
+    float s = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (x < a.c.d) {
+      const __nv_bfloat16* kp = reinterpret_cast<const __nv_bfloat16*>(a.c.k) + off + x;
+      const __nv_bfloat16* vp = reinterpret_cast<const __nv_bfloat16*>(a.c.v) + off + x;
+      for (int e = 0; e < 4; ++e) {
+        s = fmaf(q[e], to_f32(kp[e]), s);
+        v[e] = to_f32(vp[e]);
+      }
+    }
+    s = warp_sum(s) * a.scale2;
+    const float mn = fmaxf(m, s), base = mn == -INFINITY ? 0.f : mn;
+    const float f = exp2_fast(m - base), p = exp2_fast(s - base);
+    l = l * f + p;
+    for (int e = 0; e < 4; ++e) o[e] = o[e] * f + p * v[e];
+    m = mn;
+  }
+  *m_ = m;
+  *l_ = l;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(T_THREADS, 1)
+    k_attend_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+                const __grid_constant__ CUtensorMap vmap, AttnArgs a, int npair, int tiles) {
+  constexpr int NS = t_slots<DP>(), SLOT = TM * DP * 2, HALF = TM * 128, NH = DP / 64;
+  extern __shared__ char raw[];
+  char* smem = reinterpret_cast<char*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+  char* Qs = smem;
+  char* ring = Qs + 2 * SLOT;
+  TCtl* ctl = reinterpret_cast<TCtl*>(ring + NS * SLOT);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+  Turns tn;
+  tn.ps = a.c.ps;
+  tn.ppt = tn.ps <= TM ? TM / tn.ps : 1;
+  tn.kt = tn.ps <= TM ? tn.ppt * tn.ps : TM;
+  tn.tpp = ceil_div(tn.ps, TM);
+
+  if (tid == 0) {
+    for (int s = 0; s < NS; ++s) {
+      tc::mbar_init(&ctl->full[s], 1);
+      tc::mbar_init(&ctl->empty[s], 1);
+    }
+    tc::mbar_init(&ctl->qfull, 1);
+    tc::mbar_init(&ctl->drained, 1);
+    for (int x = 0; x < 2; ++x) {
+      tc::mbar_init(&ctl->sfull[x], 1);
+      tc::mbar_init(&ctl->pfull[x], 4);
+    }
+    ctl->abort = 0;
+    ctl->strange = 0;
+    tc::fence_mbar_init();
+  }
+  if (warp == 8 && lane == 0) {
+    tc::prefetch_tmap(&qmap);
+    tc::prefetch_tmap(&kmap);
+    tc::prefetch_tmap(&vmap);
+  }
+  if (tn.kt < TM) {  // rows of a slot that no copy writes
+    const int per = (TM - tn.kt) * 8;
+    for (int x = tid; x < NS * NH * per; x += T_THREADS) {
+      const int s = x / per, y = x - s * per;
+      *reinterpret_cast<int4*>(ring + s * HALF + tn.kt * 128 + y * 16) = make_int4(0, 0, 0, 0);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 9) {
+    tc::tmem_alloc(&ctl->tmem, 512);
+    tc::tmem_relinquish();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem = ctl->tmem;
+  grid_dep_wait();
+
+  const int b = blockIdx.z, h = blockIdx.y;
+  const int split = blockIdx.x % a.splits;
+  const int tpt = TM / a.G;  // tokens of a tile
+  const NewRows nr = new_rows(a.q_offsets, b, a.rows, a.T, a.c.status);
+  // the last tokens see the most keys: they go first
+  const int t0 = (npair - 1 - (int)blockIdx.x / a.splits) * tpt * tiles;
+  const int nt = min(tpt * tiles, nr.T - t0);  // tokens of this CTA
+  const int n = kv_len(a.c, b);
+  const int i0 = n - nr.T + t0;
+  const int two = nt > tpt ? 2 : 1;
+  int turns = 0, na = 0, ub0 = 0, x0 = 0;
+  if (nt > 0) {
+    const Seen seen = seen_keys(i0, i0 + nt - 1, a.window, a.sinks);
+    if (seen.b1 > 0) {
+      ub0 = tn.of(min(seen.b0, seen.b1 - 1));
+      na = seen.a > 0 ? min(tn.of(seen.a - 1) + 1, ub0) : 0;
+      const int all = na + tn.of(seen.b1 - 1) + 1 - ub0;
+      const int per = ceil_div(all, a.splits);
+      x0 = min(all, split * per);
+      turns = min(all, x0 + per) - x0;
+    }
+  }
+  auto turn_at = [&](int x) { return x0 + x < na ? x0 + x : ub0 + x0 + x - na; };
+
+  int issued = 0;  // copies started (copying warp)
+  if (turns > 0 && warp == 8) {
+    // ---- copies ---------------------------------------------------------------------
+    if (lane == 0) {
+      tc::mbar_arrive_expect_tx(&ctl->qfull, two * tpt * a.G * DP * 2);
+      for (int t = 0; t < two; ++t)
+        for (int c = 0; c < NH; ++c)
+          tma_load_3d(Qs + t * SLOT + c * HALF, &qmap, c * 64, h * a.G, nr.off + t0 + t * tpt,
+                      &ctl->qfull);
+    }
+    const int box = tn.ps <= TM ? tn.ps : TM;  // rows of a copy
+    const int half = lane % NH, pg = lane / NH;
+    // this lane's page of turn x; num_pages (past the pool, zeros) where there is none
+    auto look_up = [&](int x, int* slot) {
+      *slot = 0;
+      if (pg >= tn.ppt || x >= turns) return a.c.num_pages;
+      const int u = turn_at(x), j = tn.first(u) + pg * tn.ps;
+      if (j >= n) return a.c.num_pages;
+      const int p = j / tn.ps;
+      *slot = j - p * tn.ps;
+      const int page = a.c.table[(long long)b * a.c.max_pages + p];
+      if ((unsigned)page < (unsigned)a.c.num_pages) return page;
+      set_status(a.c.status, CACHE_BAD);
+      return a.c.num_pages;
+    };
+    int slot, page = look_up(0, &slot);
+    bool ok = true;
+    for (int x = 0; x < turns && ok; ++x) {
+      int nslot;
+      const int npage = look_up(x + 1, &nslot);
+      for (int kv = 0; kv < 2 && ok; ++kv) {
+        const int s = issued % NS;
+        ok = wait_for(&ctl->empty[s], ((uint32_t)(issued / NS) & 1u) ^ 1u, &ctl->abort);
+        ok = __all_sync(FULL, ok);
+        if (!ok) break;
+        if (lane == 0) tc::mbar_arrive_expect_tx(&ctl->full[s], tn.ppt * box * DP * 2);
+        __syncwarp();
+        if (pg < tn.ppt)
+          tma_load_4d(ring + s * SLOT + half * HALF + pg * tn.ps * 128, kv ? &vmap : &kmap,
+                      half * 64, slot, h, page, &ctl->full[s]);
+        ++issued;
+      }
+      page = npage;
+      slot = nslot;
+    }
+  } else if (turns > 0 && warp == 9) {
+    // ---- products -------------------------------------------------------------------
+    if (lane == 0) {
+      constexpr uint32_t sdesc = tc::idesc_bf16_f32(TM, TM);
+      constexpr uint32_t odesc = tc::idesc_bf16_f32(TM, DP) | (1u << 16);  // B is MN-major
+      auto logits = [&](int t, int s) {
+        const char *qa = Qs + t * SLOT, *kb = ring + s * SLOT;
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k) {
+          const int o = (k >> 2) * HALF + (k & 3) * 32;
+          tc::mma_bf16(tmem + t * TM, tc::desc_sw128_kmajor(qa + o), tc::desc_sw128_kmajor(kb + o),
+                       sdesc, k > 0);
+        }
+        tc::mma_commit(&ctl->sfull[t]);
+      };
+      bool ok = wait_for(&ctl->qfull, 0, &ctl->abort) && wait_for(&ctl->full[0], 0, &ctl->abort);
+      tc::fence_after_sync();
+      if (ok) {
+        for (int t = 0; t < two; ++t) logits(t, 0);
+        tc::mma_commit(&ctl->empty[0]);
+      }
+      for (int x = 0; x < turns && ok; ++x) {
+        const int vi = 2 * x + 1, ki = 2 * x + 2;
+        for (int t = 0; t < two && ok; ++t) {
+          ok = wait_for(&ctl->pfull[t], x & 1, &ctl->abort) &&
+               (t > 0 || wait_for(&ctl->full[vi % NS], (vi / NS) & 1, &ctl->abort));
+          if (!ok) break;
+          tc::fence_after_sync();
+          const uint32_t vb = tc::smem_u32(ring + (vi % NS) * SLOT);
+#pragma unroll
+          for (int k = 0; k < TM / 16; ++k)
+            mma_bf16_ts(tmem + 2 * TM + t * TM, tmem + t * TM + k * 8,
+                        desc_sw128_mnmajor(vb + k * 2048, HALF), odesc, x > 0 || k > 0);
+          if (t == two - 1) tc::mma_commit(&ctl->empty[vi % NS]);
+          if (x + 1 < turns) {
+            ok = t > 0 || wait_for(&ctl->full[ki % NS], (ki / NS) & 1, &ctl->abort);
+            if (!ok) break;
+            tc::fence_after_sync();
+            logits(t, ki % NS);
+            if (t == two - 1) tc::mma_commit(&ctl->empty[ki % NS]);
+          } else {
+            tc::mma_commit(&ctl->sfull[t]);  // the output is complete
+          }
+        }
+      }
+      if (!ok) {  // products in flight end before tensor memory is freed
+        tc::mma_commit(&ctl->drained);
+        const long long end = clock64() + T_WAIT;
+        while (!tc::mbar_try_wait(&ctl->drained, 0) && clock64() < end) {}
+      }
+    }
+    __syncwarp();
+  } else if (warp < 8 && nt > 0) {
+    // ---- weights --------------------------------------------------------------------
+    const int t = warp >> 2, r = tid & (TM - 1);
+    const int tok = r / a.G, g = r - tok * a.G;
+    const int mine = min(tpt, nt - t * tpt);  // tokens of this tile
+    const bool valid = tok < mine;
+    const int ti0 = i0 + t * tpt, i = ti0 + tok;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's lane quarter
+    const uint32_t sa = tmem + lanes + t * TM, oa = tmem + lanes + 2 * TM + t * TM;
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    if (mine > 0) {
+      for (int x = 0; x < turns; ++x) {
+        const int u = turn_at(x), j0 = tn.first(u), cnt = tn.rows(u);
+        ok = wait_for(&ctl->sfull[t], x & 1, &ctl->abort);
+        ok = __all_sync(FULL, ok);
+        if (!ok) break;
+        tc::fence_after_sync();
+        float s[TM];
+        tmem_ld64(sa, s);
+        tmem_ld64(sa + 64, s + 64);
+        const bool whole =
+            cnt == TM && j0 + TM - 1 <= ti0 &&
+            (a.window == 0 || ti0 + mine - 1 - j0 < a.window || j0 + TM <= a.sinks);
+        if (!whole) {
+          const int hi = valid ? min(min(i + 1, n) - j0, cnt) : 0;  // columns before hi,
+          const int lo = a.window > 0 ? i - a.window + 1 - j0 : 0;  // from lo on
+          const int sk = a.sinks - j0;                              // or before sk
+#pragma unroll
+          for (int c = 0; c < TM; ++c)
+            if (!(c < hi && (c >= lo || c < sk))) s[c] = -INFINITY;
+        }
+        float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int c = 4; c < TM; c += 8)
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            mx[y] = fmaxf(fmaxf(mx[y], s[c + y]), c + 4 + y < TM ? s[c + 4 + y] : -INFINITY);
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale2;
+        const bool grew = top > m + GROWN || (m == -INFINITY && top > m);
+        if (__any_sync(FULL, grew)) {
+          const float mn = grew ? top : m;
+          const float f = m == -INFINITY || !grew ? 1.f : exp2_fast(m - mn);
+          l *= f;
+          m = mn;
+          if (x > 0 && __any_sync(FULL, f != 1.f)) {
+#pragma unroll
+            for (int c = 0; c < DP; c += 32) {
+              float o[32];
+              tc::tmem_ld32(oa + c, o);
+#pragma unroll
+              for (int y = 0; y < 32; ++y) o[y] *= f;
+              tmem_st32_async(oa + c, reinterpret_cast<const uint32_t*>(o));
+            }
+          }
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < TM; c += 64) {
+          uint32_t p[32];
+#pragma unroll
+          for (int y = 0; y < 32; ++y) {
+            const float e0 = exp2_fast(fmaf(s[c + 2 * y], a.scale2, -base));
+            const float e1 = exp2_fast(fmaf(s[c + 2 * y + 1], a.scale2, -base));
+            sum[(2 * y) & 3] += e0;
+            sum[(2 * y + 1) & 3] += e1;
+            p[y] = pack2(e0, e1);
+          }
+          tmem_st32_async(sa + c / 2, p);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        // values of a turn that not every row of the CTA sees
+        if (t == 0 && !(cnt == TM && j0 + TM - 1 <= i0 &&
+                        (a.window == 0 || i0 + nt - 1 - j0 < a.window || j0 + TM <= a.sinks))) {
+          const int vi = 2 * x + 1;
+          ok = wait_for(&ctl->full[vi % NS], (vi / NS) & 1, &ctl->abort);
+          ok = __all_sync(FULL, ok);
+          if (!ok) break;
+          char* vrow = ring + (vi % NS) * SLOT + r * 128;
+          if (r < cnt && j0 + r < n) {
+            __nv_bfloat162 bad = __float2bfloat162_rn(0.f);
+            const __nv_bfloat162 zero = bad;
+#pragma unroll
+            for (int c = 0; c < NH * 8; ++c) {
+              const int4 w =
+                  *reinterpret_cast<const int4*>(vrow + (c >> 3) * HALF + (((c ^ lane) & 7) * 16));
+              const __nv_bfloat162* e = reinterpret_cast<const __nv_bfloat162*>(&w);
+#pragma unroll
+              for (int y = 0; y < 4; ++y) bad = __hfma2(e[y], zero, bad);
+            }
+            if (__hisnan(bad.x) || __hisnan(bad.y)) ctl->strange = 1;
+          } else {
+#pragma unroll
+            for (int c = 0; c < NH * 8; ++c)
+              *reinterpret_cast<int4*>(vrow + (c >> 3) * HALF + (((c ^ lane) & 7) * 16)) =
+                  make_int4(0, 0, 0, 0);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          }
+        }
+        tmem_wait_st();
+        tc::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&ctl->pfull[t]);
+      }
+      if (ok && turns > 0) {
+        ok = wait_for(&ctl->sfull[t], turns & 1, &ctl->abort);
+        ok = __all_sync(FULL, ok);
+        tc::fence_after_sync();
+      }
+      const int hq = h * a.G + g;
+      const long long row = nr.off + t0 + t * tpt + tok;
+      if (a.splits > 1) {
+        const long long pr = ((long long)split * a.rows + row) * a.H + hq;
+        if (valid) a.ml[pr] = ok ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
+        if (ok && turns > 0)
+#pragma unroll
+          for (int c = 0; c < DP; c += 32) {
+            float o[32];
+            tc::tmem_ld32(oa + c, o);
+            if (valid)
+#pragma unroll
+              for (int y = 0; y < 32; y += 4)
+                if (c + y < a.c.d)
+                  *reinterpret_cast<float4*>(a.part + pr * a.c.d + c + y) =
+                      make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+          }
+      } else {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        if (valid && a.lse)
+          a.lse[row * a.H + hq] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+        // 32 rows a warp through its part of the queries' tile, whole rows stored
+        char* st = Qs + t * SLOT + (warp & 3) * 32 * DP * 2;
+#pragma unroll
+        for (int c = 0; c < DP; c += 32) {
+          float o[32];
+          if (ok && turns > 0) {
+            tc::tmem_ld32(oa + c, o);
+          } else {
+#pragma unroll
+            for (int y = 0; y < 32; ++y) o[y] = 0.f;
+          }
+#pragma unroll
+          for (int y = 0; y < 32; y += 8) {
+            const int pc = (c + y) / 8;
+            *reinterpret_cast<int4*>(st + lane * DP * 2 + ((pc ^ (lane & 7)) * 16)) = make_int4(
+                pack2(o[y] * inv, o[y + 1] * inv), pack2(o[y + 2] * inv, o[y + 3] * inv),
+                pack2(o[y + 4] * inv, o[y + 5] * inv), pack2(o[y + 6] * inv, o[y + 7] * inv));
+          }
+        }
+        __syncwarp();
+        constexpr int PC = DP / 8, RPI = 32 / PC;
+        for (int y = lane / PC; y < 32; y += RPI) {
+          const int rr = (warp & 3) * 32 + y, tk = rr / a.G, gg = rr - tk * a.G, pc = lane % PC;
+          if (tk < mine && pc * 8 < a.c.d) {
+            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) +
+                                 (nr.off + t0 + t * tpt + tk) * a.o_row +
+                                 (long long)(h * a.G + gg) * a.o_head + pc * 8;
+            *reinterpret_cast<int4*>(out) =
+                *reinterpret_cast<const int4*>(st + y * DP * 2 + ((pc ^ (y & 7)) * 16));
+          }
+        }
+      }
+    }
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  if (warp == 9) tc::tmem_dealloc(tmem, 512);
+  if (ctl->abort) {
+    if (tid == 0) set_status(a.c.status, GMC_STATUS_TIMEOUT);
+    if (warp == 8) {  // copies in flight land before shared memory is given back
+      const long long end = clock64() + T_WAIT;
+      for (int q = issued > NS ? issued - NS : 0; q < issued; ++q)
+        while (!tc::mbar_try_wait(&ctl->full[q % NS], (q / NS) & 1) && clock64() < end) {}
+    }
+    return;
+  }
+  if (ctl->strange) {
+    for (int rr = warp; rr < nt * a.G; rr += T_THREADS / 32) {
+      const int tk = rr / a.G, g = rr - tk * a.G, hq = h * a.G + g;
+      const long long row = nr.off + t0 + tk;
+      float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int x = 0; x < turns; ++x) {
+        const int u = turn_at(x), f = tn.first(u);
+        row_alone(a, b, h, row, hq, i0 + tk, f, min(n, f + tn.rows(u)), &m, &l, o);
+      }
+      const int y = lane * 4;
+      if (a.splits > 1) {
+        const long long pr = ((long long)split * a.rows + row) * a.H + hq;
+        if (lane == 0) a.ml[pr] = make_float2(m, l);
+        if (y < a.c.d)
+          *reinterpret_cast<float4*>(a.part + pr * a.c.d + y) = make_float4(o[0], o[1], o[2], o[3]);
+      } else {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        if (lane == 0 && a.lse)
+          a.lse[row * a.H + hq] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+        if (y < a.c.d)
+          for (int e = 0; e < 4; ++e)
+            reinterpret_cast<__nv_bfloat16*>(
+                a.out)[row * a.o_row + (long long)hq * a.o_head + y + e] =
+                __float2bfloat16_rn(o[e] * inv);
+      }
+    }
+  }
+}
+
+// [dims] of bf16 elements, 128-byte swizzle, box of 64 elements.
+cudaError_t make_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims,
+                     const cuuint64_t* strides, const cuuint32_t* box) {
+  typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                             const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  Encode fn = reinterpret_cast<Encode>(tensor_map_encoder());
+  if (!fn) return cudaErrorNotSupported;
+  const cuuint32_t ones[4] = {1, 1, 1, 1};
+  const CUresult r =
+      fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box,
+         ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+// CTAs without a split, and turns of the longest key axis.
+long long tc_ctas(const KV& c, int G, int T, int tiles) {
+  return (long long)c.B * c.Hkv * ceil_div(T, TM / G * tiles);
+}
+}  // namespace
+
+// One tile a CTA where two would leave SMs idle.
+int attend_tc_tiles(const KV& c, int G, int T) {
+  return T > TM / G && tc_ctas(c, G, T, 2) >= 152 ? 2 : 1;
+}
+// Parts of the key axis: as many as fill the SMs, two turns each at least.
+int attend_tc_splits(const KV& c, int G, int T) {
+  const long long ctas = tc_ctas(c, G, T, attend_tc_tiles(c, G, T));
+  if (ctas >= 152) return 1;
+  return (int)std::max<long long>(1, std::min<long long>({152 / ctas, 32, c.cap / (2 * TM)}));
+}
+
+bool attend_tc_takes(const KV& c, int dtype, int G) {
+  // whole swizzle atoms of 8 slots a page; strides that a tensor map can hold
+  auto fits = [](long long s, int n) { return n == 1 || (s > 0 && s * 2 < (1LL << 40)); };
+  return dtype == GMC_BF16 && c.d <= 128 && G <= TM && c.ps % 8 == 0 &&
+         fits(c.page_stride, c.num_pages) && fits(c.head_stride, c.Hkv) &&
+         fits(c.slot_stride, c.ps);
+}
+
+cudaError_t launch_attend_tc(const AttnArgs& a, cudaStream_t st) {
+  const int tpt = TM / a.G, NHd = a.c.d <= 64 ? 1 : 2, tiles = attend_tc_tiles(a.c, a.G, a.T);
+  CUtensorMap qm, km, vm;
+  auto stride = [&](long long s, int n) {
+    return n == 1 ? (cuuint64_t)a.c.d * 2 : (cuuint64_t)s * 2;
+  };
+  cudaError_t e;
+  {
+    const cuuint64_t dims[3] = {(cuuint64_t)a.c.d, (cuuint64_t)a.H, (cuuint64_t)a.rows};
+    const cuuint64_t strides[2] = {stride(a.q_head, a.H), stride(a.q_row, a.rows)};
+    const cuuint32_t box[3] = {64, (cuuint32_t)a.G, (cuuint32_t)tpt};
+    if ((e = make_map(&qm, a.q, 3, dims, strides, box)) != cudaSuccess) return e;
+  }
+  {
+    const cuuint64_t dims[4] = {(cuuint64_t)a.c.d, (cuuint64_t)a.c.ps, (cuuint64_t)a.c.Hkv,
+                                (cuuint64_t)a.c.num_pages};
+    const cuuint64_t strides[3] = {stride(a.c.slot_stride, a.c.ps),
+                                   stride(a.c.head_stride, a.c.Hkv),
+                                   stride(a.c.page_stride, a.c.num_pages)};
+    const cuuint32_t box[4] = {64, (cuuint32_t)std::min(a.c.ps, TM), 1, 1};
+    if ((e = make_map(&km, a.c.k, 4, dims, strides, box)) != cudaSuccess) return e;
+    if ((e = make_map(&vm, a.c.v, 4, dims, strides, box)) != cudaSuccess) return e;
+  }
+  const int npair = ceil_div(a.T, tpt * tiles);
+  const dim3 grid((unsigned)npair * a.splits, a.c.Hkv, a.c.B);
+  if (NHd == 1) {
+    if ((e = set_smem_limit((const void*)k_attend_tc<64>, t_smem<64>())) != cudaSuccess) return e;
+    return launch_k(k_attend_tc<64>, grid, dim3(T_THREADS), t_smem<64>(), st, 1, qm, km, vm, a,
+                    npair, tiles);
+  }
+  if ((e = set_smem_limit((const void*)k_attend_tc<128>, t_smem<128>())) != cudaSuccess) return e;
+  return launch_k(k_attend_tc<128>, grid, dim3(T_THREADS), t_smem<128>(), st, 1, qm, km, vm, a,
+                  npair, tiles);
+}
+
+}  // namespace gmc

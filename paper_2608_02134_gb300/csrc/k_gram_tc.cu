@@ -238,6 +238,8 @@ static EncodeTiledFn encode_fn() {
   return fn;
 }
 
+void* tensor_map_encoder() { return reinterpret_cast<void*>(encode_fn()); }
+
 // 2-D bf16 tensor map: rows of `row_elems` elements, `rows` rows, row pitch
 // `pitch_elems`; box = 64 elements x `box_rows` rows, 128-byte swizzle.
 cudaError_t make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t row_elems, uint64_t rows,
