@@ -6,6 +6,12 @@
 
 namespace gmc {
 
+// Lets the next kernel on the stream be set up while this one runs (it waits in its
+// own grid_dep_wait before it touches memory).
+__device__ __forceinline__ void grid_dep_launch() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 constexpr uint32_t CACHE_BAD = GMC_STATUS_CACHE;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -132,12 +138,17 @@ struct DecodeArgs {
   long long q_row, q_head, o_row, o_head;
   int H, G, window, sinks;
   float scale2;
-  int h0;          // first query head of its key head in this launch
-  bool fresh;      // the appended key's score starts from 0
-  int chunk;       // seen keys of a split
-  float* logits;   // [B][Hkv][splits][heads][chunk] or NULL: kept in shared memory
-  int chunk_smem;
+  int h0, heads;      // query heads of a key head in this launch: from h0 on
+  bool fresh;         // the appended key's score starts from 0
+  // workspace, see k_decode.cu
+  float2* ml;                  // [part][heads] maxima and sums
+  float* part;                 // [part][heads][DP] outputs, unnormalised
+  float* logits;               // [B][Hkv][places][hs]
+  int places, hs;
+  int warps;  // of the launch
+  unsigned page16, head16, slot16;  // strides in pieces of 16 bytes
 };
+int sm_count();  // of the current device
 size_t decode_workspace(const KV&, int dtype, int H);
 cudaError_t launch_decode(DecodeArgs a, int dtype, void* ws, cudaStream_t, int* launches);
 

@@ -28,6 +28,9 @@ int check_shape(const gmc_kv_cache* c) {
   if ((long long)c->page_size * c->max_pages > 0x40000000LL || c->B > 65535 || c->Hkv > 65535)
     return GMC_ERR_UNSUPPORTED;
   if (c->max_len > c->page_size * c->max_pages) return GMC_ERR_ARG;
+  // turns of 16 keys over all sequences and key heads are counted in 32 bits
+  if ((long long)c->B * c->Hkv * (c->page_size * (long long)c->max_pages / 16 + 1) > 0x40000000LL)
+    return GMC_ERR_UNSUPPORTED;
   if (c->d > GMC_MAX_CACHE_D || c->d % (16 / esize_of(c->dtype)) != 0) return GMC_ERR_UNSUPPORTED;
   return GMC_OK;
 }

@@ -66,6 +66,7 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_simt(AttnArgs a, int gsub
   char* Ps = Vs + AT_K * DP * 4;
   long long* offs = reinterpret_cast<long long*>(Ps + R * AT_K * 4);  // [2][AT_K]
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  grid_dep_launch();
   grid_dep_wait();
   const int b = blockIdx.z;
   const int ng = ceil_div(a.G, gsub);
@@ -260,6 +261,7 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_simt(AttnArgs a, int gsub
 // One warp a (row, query head): out = sum_s w_s part_s / sum_s w_s l_s, w_s = 2^(m_s - max m).
 template <typename T>
 __global__ void __launch_bounds__(256) k_attend_join(AttnArgs a) {
+  grid_dep_launch();
   grid_dep_wait();
   const int lane = threadIdx.x & 31;
   const long long x = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);

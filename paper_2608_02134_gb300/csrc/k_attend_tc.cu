@@ -263,6 +263,7 @@ __global__ void __launch_bounds__(T_THREADS, 1)
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = ctl->tmem;
+  grid_dep_launch();
   grid_dep_wait();
 
   const int b = blockIdx.z, h = blockIdx.y;

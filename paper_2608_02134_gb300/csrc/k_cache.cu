@@ -18,6 +18,7 @@ __global__ void __launch_bounds__(AP_THREADS)
     k_cache_append(KV c, const char* __restrict__ k_new, const char* __restrict__ v_new,
                    const int32_t* __restrict__ offsets, int rows, int T, int esize, int tile) {
   __shared__ long long at[AP_ROWS];
+  grid_dep_launch();
   grid_dep_wait();
   const int b = blockIdx.y, t0 = blockIdx.x * tile;
   const NewRows nr = new_rows(offsets, b, rows, T, c.status);
@@ -100,6 +101,7 @@ __global__ void __launch_bounds__(EV_THREADS) k_evict(EvictArgs a, int esize) {
   const int C = (int)cluster.num_blocks(), r = (int)cluster.block_rank();
   const int h = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  grid_dep_launch();
   grid_dep_wait();
   const int n = kv_len(a.src, b);
   const int k = min(a.keep, n);
@@ -266,6 +268,16 @@ __global__ void __launch_bounds__(EV_THREADS) k_evict(EvictArgs a, int esize) {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 }  // namespace
+
+int sm_count() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return 152;
+  }
+  return sms;
+}
 
 cudaError_t launch_cache_append(const KV& c, int dtype, const void* k_new, const void* v_new,
                                 const int32_t* offsets, int rows, int T, cudaStream_t st) {

@@ -497,21 +497,56 @@ class KVCache:
         self.k, self.v, self.page_table, self.lens, self.status = k, v, page_table, lens, status
         self.B, self.max_pages = page_table.shape
         self.num_pages, self.Hkv, self.page_size, self.d = k.shape
-        self.max_len, self.dtype = max_len, k.dtype
+        self.max_len, self.dtype, self.device_index = max_len, k.dtype, k.get_device()
         self.struct = CacheStruct(
             self.B, self.Hkv, self.d, _DTYPES[k.dtype], self.page_size, self.num_pages,
             self.max_pages, max_len, k.stride(0), k.stride(1), k.stride(2), k.data_ptr(),
             v.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
             None if status is None else status.data_ptr())
         self.ref = ctypes.byref(self.struct)
+        self._row_shape = (self.Hkv, self.d)        # of new rows
+        self._new_shape = (self.B, self.Hkv, self.d)
+        self._attn = {}                             # gmc_attn of dense queries and outputs
+
+    def attn(self, q, out, window, sinks, scale):
+        """gmc_attn of these queries and outputs, and their head count."""
+        shape = q.shape
+        if len(shape) != 3 or shape != out.shape or q.dtype != self.dtype \
+                or out.dtype != self.dtype or shape[2] != self.d:
+            raise GMCError("queries and outputs: [rows, H, d] of the cache's type")
+        H = shape[1]
+        if q.is_contiguous() and out.is_contiguous():
+            key = (H, window, sinks, scale)
+            a = self._attn.get(key)
+            if a is None:
+                a = ctypes.byref(Attn(H, window, sinks, scale or 0.0, 0, 0, 0, 0))
+                self._attn[key] = a
+            return a, H
+        if q.stride(2) != 1 or out.stride(2) != 1 or \
+                (shape[0] > 1 and 0 in (q.stride(0), out.stride(0))) or \
+                (H > 1 and 0 in (q.stride(1), out.stride(1))):
+            raise GMCError("queries and outputs: unit-stride rows, none of them shared")
+        # the stride of a dimension of one is anything: none is passed
+        rs = [t.stride(0) if shape[0] > 1 else H * self.d for t in (q, out)]
+        hs = [t.stride(1) if H > 1 else self.d for t in (q, out)]
+        return ctypes.byref(Attn(H, window, sinks, scale or 0.0, rs[0], hs[0], rs[1], hs[1])), H
+
+    def stream(self, stream):
+        """Handle of `stream`, or of the current stream of the cache's device."""
+        if stream is not None:
+            return stream.cuda_stream
+        return torch._C._cuda_getCurrentRawStream(self.device_index)
+
+    def workspace(self, nbytes, stream):
+        """A workspace for one call on `stream`."""
+        w = alloc_workspace(nbytes, self.k.device)
+        if stream is not None:
+            w.record_stream(stream)
+        return w
 
 
 def _addr(t):
     return None if t is None else t.data_ptr()
-
-
-def _stream_handle(stream):
-    return stream.cuda_stream if stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _check_int32(t, n, what):
@@ -525,33 +560,29 @@ def _check_f32(t, n, what):
 
 
 def _check_scores(cache, t):
-    if t.dtype != torch.float32 or t.dim() != 3 or t.shape[0] != cache.B \
-            or t.shape[1] != cache.Hkv or not t.is_contiguous():
+    shape = t.shape
+    if t.dtype != torch.float32 or len(shape) != 3 or shape[0] != cache.B \
+            or shape[1] != cache.Hkv or not t.is_contiguous():
         raise GMCError("scores: dense fp32 [B, Hkv, places]")
-
-
-def _attn(cache, q, out, window, sinks, scale):
-    if q.dim() != 3 or q.shape != out.shape or q.dtype != cache.dtype or out.dtype != cache.dtype \
-            or q.shape[2] != cache.d or q.stride(2) != 1 or out.stride(2) != 1:
-        raise GMCError("queries and outputs: [rows, H, d] of the cache's type, unit-stride rows")
-    return Attn(q.shape[1], window, sinks, scale or 0.0, q.stride(0), q.stride(1), out.stride(0),
-                out.stride(1))
+    return shape
 
 
 def cache_append(cache: KVCache, k_new, v_new, T, offsets=None, stream=None):
     """gmc_cache_append: k_new, v_new [rows, Hkv, d], T new rows a sequence (the most of a
     ragged call, whose offsets is int32 [B+1]); v_new None: k_new is laid out as
     gmc_compress's out_kv, [2 * rows, Hkv, d]."""
-    rows = k_new.shape[0] if v_new is not None else k_new.shape[0] // 2
-    for t in (k_new, v_new):
-        if t is not None and (t.dtype != cache.dtype or t.dim() != 3 or not t.is_contiguous()
-                              or tuple(t.shape[1:]) != (cache.Hkv, cache.d)):
-            raise GMCError("new rows: dense [rows, Hkv, d] of the cache's type")
-    if v_new is not None and v_new.shape[0] != rows:
+    shape = k_new.shape
+    rows = shape[0] if v_new is not None else shape[0] // 2
+    if shape[1:] != cache._row_shape or k_new.dtype != cache.dtype or not k_new.is_contiguous():
+        raise GMCError("new rows: dense [rows, Hkv, d] of the cache's type")
+    if v_new is not None and (v_new.shape != shape or v_new.dtype != cache.dtype
+                              or not v_new.is_contiguous()):
         raise GMCError("new rows: as many values as keys")
     _check_int32(offsets, cache.B + 1, "offsets: dense int32 [B + 1]")
-    _check(lib().gmc_cache_append(cache.ref, _addr(k_new), _addr(v_new), _addr(offsets), rows, T,
-                                  _stream_handle(stream)))
+    rc = lib().gmc_cache_append(cache.ref, k_new.data_ptr(), _addr(v_new), _addr(offsets), rows, T,
+                                cache.stream(stream))
+    if rc:
+        _check(rc)
 
 
 def attend_workspace_size(cache: KVCache, H, T) -> int:
@@ -563,15 +594,17 @@ def attend(cache: KVCache, q, out, T, q_offsets=None, window=0, sinks=0, scale=N
     """gmc_attend: causal attention of the new tokens q [rows, H, d] into out (and lse fp32
     [rows, H]); T new tokens a sequence (the most of a ragged call, whose q_offsets is
     int32 [B+1]).  scale None: 1 / sqrt(d)."""
-    a = _attn(cache, q, out, window, sinks, scale)
+    a, H = cache.attn(q, out, window, sinks, scale)
     rows = q.shape[0]
     _check_int32(q_offsets, cache.B + 1, "q_offsets: dense int32 [B + 1]")
-    _check_f32(lse, rows * a.H, "lse: dense fp32 [rows, H]")
+    _check_f32(lse, rows * H, "lse: dense fp32 [rows, H]")
     if workspace is None:
-        workspace = alloc_workspace(attend_workspace_size(cache, a.H, T), q.device)
-    _check(lib().gmc_attend(cache.ref, ctypes.byref(a), q.data_ptr(), _addr(q_offsets), rows, T,
-                            out.data_ptr(), _addr(lse), workspace.data_ptr(), workspace.numel(),
-                            _stream_handle(stream)))
+        workspace = cache.workspace(attend_workspace_size(cache, H, T), stream)
+    rc = lib().gmc_attend(cache.ref, a, q.data_ptr(), _addr(q_offsets), rows, T, out.data_ptr(),
+                          _addr(lse), workspace.data_ptr(), workspace.numel(),
+                          cache.stream(stream))
+    if rc:
+        _check(rc)
 
 
 def decode_workspace_size(cache: KVCache, H) -> int:
@@ -584,26 +617,28 @@ def decode(cache: KVCache, q, out, k_new=None, v_new=None, window=0, sinks=0, sc
     k_new, v_new [B, Hkv, d]: appended at place lens - 1 on the way.  scores, out_scores
     fp32 [B, Hkv, places]: out_scores = scores + the weight every key received (the
     same tensor will do)."""
-    a = _attn(cache, q, out, window, sinks, scale)
+    a, H = cache.attn(q, out, window, sinks, scale)
     if q.shape[0] != cache.B:
         raise GMCError("decode: one query row a sequence")
     for t in (k_new, v_new):
-        if t is not None and (t.dtype != cache.dtype or not t.is_contiguous()
-                              or tuple(t.shape) != (cache.B, cache.Hkv, cache.d)):
+        if t is not None and (t.shape != cache._new_shape or t.dtype != cache.dtype
+                              or not t.is_contiguous()):
             raise GMCError("new rows: dense [B, Hkv, d] of the cache's type")
-    _check_f32(lse, cache.B * a.H, "lse: dense fp32 [B, H]")
+    _check_f32(lse, cache.B * H, "lse: dense fp32 [B, H]")
     places = 0
     if scores is not None:
-        _check_scores(cache, scores)
-        if out_scores is None or out_scores.shape != scores.shape:
+        shape = _check_scores(cache, scores)
+        if out_scores is not scores and (out_scores is None
+                                         or _check_scores(cache, out_scores) != shape):
             raise GMCError("decode: scores and out_scores alike")
-        _check_scores(cache, out_scores)
-        places = scores.shape[2]
+        places = shape[2]
     if workspace is None:
-        workspace = alloc_workspace(decode_workspace_size(cache, a.H), q.device)
-    _check(lib().gmc_decode(cache.ref, ctypes.byref(a), q.data_ptr(), _addr(k_new), _addr(v_new),
-                            out.data_ptr(), _addr(lse), _addr(scores), _addr(out_scores), places,
-                            workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+        workspace = cache.workspace(decode_workspace_size(cache, H), stream)
+    rc = lib().gmc_decode(cache.ref, a, q.data_ptr(), _addr(k_new), _addr(v_new), out.data_ptr(),
+                          _addr(lse), _addr(scores), _addr(out_scores), places,
+                          workspace.data_ptr(), workspace.numel(), cache.stream(stream))
+    if rc:
+        _check(rc)
 
 
 def evict_workspace_size(cache: KVCache, keep) -> int:
@@ -619,10 +654,12 @@ def evict(src: KVCache, dst: KVCache, scores, keep, out_idx, out_scores=None, si
     _check_int32(out_idx, src.B * src.Hkv * keep, "out_idx: dense int32 [B, Hkv, keep]")
     _check_f32(out_scores, src.B * src.Hkv * keep, "out_scores: dense fp32 [B, Hkv, keep]")
     if workspace is None:
-        workspace = alloc_workspace(evict_workspace_size(src, keep), scores.device)
-    _check(lib().gmc_evict(src.ref, dst.ref, scores.data_ptr(), scores.shape[2], keep, sinks,
-                           recent, out_idx.data_ptr(), _addr(out_scores), workspace.data_ptr(),
-                           workspace.numel(), _stream_handle(stream)))
+        workspace = src.workspace(evict_workspace_size(src, keep), stream)
+    rc = lib().gmc_evict(src.ref, dst.ref, scores.data_ptr(), scores.shape[2], keep, sinks, recent,
+                         out_idx.data_ptr(), _addr(out_scores), workspace.data_ptr(),
+                         workspace.numel(), src.stream(stream))
+    if rc:
+        _check(rc)
 
 
 # ---------------------------------------------------------------------------
