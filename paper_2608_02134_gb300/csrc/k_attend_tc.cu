@@ -43,7 +43,7 @@ constexpr float GROWN = 8.f;            // powers of two the maximum may fall be
 template <int DP> constexpr int t_slots() { return DP == 128 ? 5 : 8; }
 
 struct TCtl {
-  uint64_t full[8], empty[8], qfull, sfull[2], pfull[2], drained;
+  uint64_t full[8], empty[8], qfull, sfull[2], pfull[2][2], drained;
   uint32_t tmem;
   volatile int abort;
   int strange;
@@ -102,14 +102,46 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
       : "memory");
 }
 
-// D[tmem] (+)= A[tmem] * B[smem], bf16 inputs, fp32 accumulate.
-__device__ __forceinline__ void mma_bf16_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc,
-                                            uint32_t accumulate) {
+// The issuing warp runs as a whole, so that addresses and descriptors stay in uniform
+// registers; the one thread whose `go` is set issues.
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t p;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(p));
+  return p;
+}
+// D[tmem] (+)= A[smem] * B[smem]^T, bf16 inputs, fp32 accumulate.
+__device__ __forceinline__ void mma_ss(uint32_t go, uint32_t d, uint64_t adesc, uint64_t bdesc,
+                                       uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(go)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem].
+__device__ __forceinline__ void mma_ts(uint32_t go, uint32_t d, uint32_t a, uint64_t bdesc,
+                                       uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(go)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t go, uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(
+          tc::smem_u32(bar)),
+      "r"(go)
       : "memory");
 }
 
@@ -167,6 +199,34 @@ __device__ __forceinline__ void tmem_wait_st() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
+// Two fp32 at a time.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+  f32x2 d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ float2 unpair(f32x2 v) {
+  float2 d;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(v));
+  return d;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
@@ -209,6 +269,38 @@ __device__ __noinline__ void row_alone(const AttnArgs& a, int b, int h, long lon
   *l_ = l;
 }
 
+// The values of a turn that some rows of the CTA do not see, a row a thread of the first
+// tile's warps: slots past the end become zeros, others are looked over for infinities
+// and NaN.  false: the copy did not come.
+template <int DP>
+__device__ __forceinline__ bool look_over(TCtl* ctl, char* slot, int s, uint32_t parity, int r,
+                                          bool there) {
+  const int lane = threadIdx.x & 31;
+  const bool ok = wait_for(&ctl->full[s], parity, &ctl->abort);
+  if (!__all_sync(FULL, ok)) return false;
+  char* row = slot + r * 128;
+  if (there) {
+    const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
+    __nv_bfloat162 bad = zero;
+#pragma unroll
+    for (int c = 0; c < DP / 8; ++c) {
+      const int4 w =
+          *reinterpret_cast<const int4*>(row + (c >> 3) * TM * 128 + (((c ^ lane) & 7) * 16));
+      const __nv_bfloat162* e = reinterpret_cast<const __nv_bfloat162*>(&w);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) bad = __hfma2(e[y], zero, bad);
+    }
+    if (__hisnan(bad.x) || __hisnan(bad.y)) ctl->strange = 1;
+  } else {
+#pragma unroll
+    for (int c = 0; c < DP / 8; ++c)
+      *reinterpret_cast<int4*>(row + (c >> 3) * TM * 128 + (((c ^ lane) & 7) * 16)) =
+          make_int4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  return true;
+}
+
 template <int DP>
 __global__ void __launch_bounds__(T_THREADS, 1)
     k_attend_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
@@ -236,7 +328,8 @@ __global__ void __launch_bounds__(T_THREADS, 1)
     tc::mbar_init(&ctl->drained, 1);
     for (int x = 0; x < 2; ++x) {
       tc::mbar_init(&ctl->sfull[x], 1);
-      tc::mbar_init(&ctl->pfull[x], 4);
+      tc::mbar_init(&ctl->pfull[x][0], 4);
+      tc::mbar_init(&ctl->pfull[x][1], 4);
     }
     ctl->abort = 0;
     ctl->strange = 0;
@@ -255,6 +348,17 @@ __global__ void __launch_bounds__(T_THREADS, 1)
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  grid_dep_launch();
+  grid_dep_wait();
+  const int b = blockIdx.z, h = blockIdx.y;
+  const int split = blockIdx.x % a.splits;
+  const int tpt = TM / a.G;  // tokens of a tile
+  const NewRows nr = new_rows(a.q_offsets, b, a.rows, a.T, a.c.status);
+  const int n = kv_len(a.c, b);
+  // the last tokens see the most keys: they go first
+  const int t0 = (npair - 1 - (int)blockIdx.x / a.splits) * tpt * tiles;
+  const int nt = min(tpt * tiles, nr.T - t0);  // tokens of this CTA
+  if (nt <= 0) return;
   if (warp == 9) {
     tc::tmem_alloc(&ctl->tmem, 512);
     tc::tmem_relinquish();
@@ -263,21 +367,10 @@ __global__ void __launch_bounds__(T_THREADS, 1)
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = ctl->tmem;
-  grid_dep_launch();
-  grid_dep_wait();
-
-  const int b = blockIdx.z, h = blockIdx.y;
-  const int split = blockIdx.x % a.splits;
-  const int tpt = TM / a.G;  // tokens of a tile
-  const NewRows nr = new_rows(a.q_offsets, b, a.rows, a.T, a.c.status);
-  // the last tokens see the most keys: they go first
-  const int t0 = (npair - 1 - (int)blockIdx.x / a.splits) * tpt * tiles;
-  const int nt = min(tpt * tiles, nr.T - t0);  // tokens of this CTA
-  const int n = kv_len(a.c, b);
   const int i0 = n - nr.T + t0;
   const int two = nt > tpt ? 2 : 1;
   int turns = 0, na = 0, ub0 = 0, x0 = 0;
-  if (nt > 0) {
+  {
     const Seen seen = seen_keys(i0, i0 + nt - 1, a.window, a.sinks);
     if (seen.b1 > 0) {
       ub0 = tn.of(min(seen.b0, seen.b1 - 1));
@@ -337,57 +430,80 @@ __global__ void __launch_bounds__(T_THREADS, 1)
     }
   } else if (turns > 0 && warp == 9) {
     // ---- products -------------------------------------------------------------------
-    if (lane == 0) {
-      constexpr uint32_t sdesc = tc::idesc_bf16_f32(TM, TM);
-      constexpr uint32_t odesc = tc::idesc_bf16_f32(TM, DP) | (1u << 16);  // B is MN-major
-      auto logits = [&](int t, int s) {
-        const char *qa = Qs + t * SLOT, *kb = ring + s * SLOT;
+    constexpr uint32_t sdesc = tc::idesc_bf16_f32(TM, TM);
+    constexpr uint32_t odesc = tc::idesc_bf16_f32(TM, DP) | (1u << 16);  // B is MN-major
+    const uint32_t go = elect_one();
+    // advancing an address by x bytes adds x / 16 to its descriptor
+    const uint64_t qd = tc::desc_sw128_kmajor(Qs), kd = tc::desc_sw128_kmajor(ring),
+                   vd = desc_sw128_mnmajor(tc::smem_u32(ring), HALF);
+    auto logits = [&](int t, int slot) {
+      const uint64_t qa = qd + t * (SLOT / 16), kb = kd + slot * (SLOT / 16);
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k) {
-          const int o = (k >> 2) * HALF + (k & 3) * 32;
-          tc::mma_bf16(tmem + t * TM, tc::desc_sw128_kmajor(qa + o), tc::desc_sw128_kmajor(kb + o),
-                       sdesc, k > 0);
-        }
-        tc::mma_commit(&ctl->sfull[t]);
-      };
-      bool ok = wait_for(&ctl->qfull, 0, &ctl->abort) && wait_for(&ctl->full[0], 0, &ctl->abort);
-      tc::fence_after_sync();
-      if (ok) {
-        for (int t = 0; t < two; ++t) logits(t, 0);
-        tc::mma_commit(&ctl->empty[0]);
+      for (int k = 0; k < DP / 16; ++k) {
+        const int o = ((k >> 2) * HALF + (k & 3) * 32) / 16;
+        mma_ss(go, tmem + t * TM, qa + o, kb + o, sdesc, k > 0);
       }
-      for (int x = 0; x < turns && ok; ++x) {
-        const int vi = 2 * x + 1, ki = 2 * x + 2;
-        for (int t = 0; t < two && ok; ++t) {
-          ok = wait_for(&ctl->pfull[t], x & 1, &ctl->abort) &&
-               (t > 0 || wait_for(&ctl->full[vi % NS], (vi / NS) & 1, &ctl->abort));
+      commit(go, &ctl->sfull[t]);
+    };
+    auto ready = [&](uint64_t* bar, uint32_t parity) {
+      const bool ok = wait_for(bar, parity, &ctl->abort);
+      return __all_sync(FULL, ok) != 0;
+    };
+    bool ok = ready(&ctl->qfull, 0) && ready(&ctl->full[0], 0);
+    tc::fence_after_sync();
+    if (ok) {
+      for (int t = 0; t < two; ++t) logits(t, 0);
+      commit(go, &ctl->empty[0]);
+    }
+    int vs = 1, ks = 2 % NS;        // slots of this turn's values and the next one's keys
+    uint32_t vp = 0, kp = 2 / NS;   // and their parities
+#pragma unroll 1
+    for (int x = 0; x < turns && ok; ++x) {
+#pragma unroll 1
+      for (int t = 0; t < two; ++t) {
+        const uint64_t vb = vd + vs * (SLOT / 16);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {  // 64 keys' weights at a time
+          ok = ok && ready(&ctl->pfull[t][half], x & 1);
+          if (half == 0 && t == 0) ok = ok && ready(&ctl->full[vs], vp);
           if (!ok) break;
           tc::fence_after_sync();
-          const uint32_t vb = tc::smem_u32(ring + (vi % NS) * SLOT);
 #pragma unroll
-          for (int k = 0; k < TM / 16; ++k)
-            mma_bf16_ts(tmem + 2 * TM + t * TM, tmem + t * TM + k * 8,
-                        desc_sw128_mnmajor(vb + k * 2048, HALF), odesc, x > 0 || k > 0);
-          if (t == two - 1) tc::mma_commit(&ctl->empty[vi % NS]);
-          if (x + 1 < turns) {
-            ok = t > 0 || wait_for(&ctl->full[ki % NS], (ki / NS) & 1, &ctl->abort);
-            if (!ok) break;
-            tc::fence_after_sync();
-            logits(t, ki % NS);
-            if (t == two - 1) tc::mma_commit(&ctl->empty[ki % NS]);
-          } else {
-            tc::mma_commit(&ctl->sfull[t]);  // the output is complete
-          }
+          for (int k = half * (TM / 32); k < (half + 1) * (TM / 32); ++k)
+            mma_ts(go, tmem + 2 * TM + t * TM, tmem + t * TM + k * 8, vb + k * (2048 / 16), odesc,
+                   x > 0 || k > 0);
+        }
+        if (!ok) break;
+        if (t == two - 1) commit(go, &ctl->empty[vs]);
+        if (x + 1 < turns) {
+          if (t == 0) ok = ready(&ctl->full[ks], kp);
+          if (!ok) break;
+          tc::fence_after_sync();
+          logits(t, ks);
+          if (t == two - 1) commit(go, &ctl->empty[ks]);
+        } else {
+          commit(go, &ctl->sfull[t]);  // the output is complete
         }
       }
-      if (!ok) {  // products in flight end before tensor memory is freed
-        tc::mma_commit(&ctl->drained);
-        const long long end = clock64() + T_WAIT;
-        while (!tc::mbar_try_wait(&ctl->drained, 0) && clock64() < end) {}
+      vs += 2;
+      if (vs >= NS) {
+        vs -= NS;
+        vp ^= 1;
+      }
+      ks += 2;
+      if (ks >= NS) {
+        ks -= NS;
+        kp ^= 1;
+      }
+    }
+    if (!ok) {  // products in flight end before tensor memory is freed
+      commit(go, &ctl->drained);
+      const long long end = clock64() + T_WAIT;
+      while (!tc::mbar_try_wait(&ctl->drained, 0) && clock64() < end) {
       }
     }
     __syncwarp();
-  } else if (warp < 8 && nt > 0) {
+  } else if (warp < 8) {
     // ---- weights --------------------------------------------------------------------
     const int t = warp >> 2, r = tid & (TM - 1);
     const int tok = r / a.G, g = r - tok * a.G;
@@ -421,10 +537,11 @@ __global__ void __launch_bounds__(T_THREADS, 1)
         }
         float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-        for (int c = 4; c < TM; c += 8)
+        for (int c = 4; c + 8 <= TM; c += 8)
 #pragma unroll
-          for (int y = 0; y < 4; ++y)
-            mx[y] = fmaxf(fmaxf(mx[y], s[c + y]), c + 4 + y < TM ? s[c + 4 + y] : -INFINITY);
+          for (int y = 0; y < 4; ++y) mx[y] = max3(mx[y], s[c + y], s[c + 4 + y]);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) mx[y] = fmaxf(mx[y], s[TM - 4 + y]);
         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale2;
         const bool grew = top > m + GROWN || (m == -INFINITY && top > m);
         if (__any_sync(FULL, grew)) {
@@ -444,53 +561,33 @@ __global__ void __launch_bounds__(T_THREADS, 1)
           }
         }
         const float base = m == -INFINITY ? 0.f : m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        // values of a turn that not every row of the CTA sees, before the first product
+        if (t == 0 && !(cnt == TM && j0 + TM - 1 <= i0 &&
+                        (a.window == 0 || i0 + nt - 1 - j0 < a.window || j0 + TM <= a.sinks))) {
+          ok = look_over<DP>(ctl, ring + (2 * x + 1) % NS * SLOT, (2 * x + 1) % NS,
+                             ((2 * x + 1) / NS) & 1, r, r < cnt && j0 + r < n);
+          if (!ok) break;
+        }
+        const f32x2 scale = pair(a.scale2, a.scale2), off = pair(-base, -base);
+        f32x2 sum[2] = {0ull, 0ull};
 #pragma unroll
         for (int c = 0; c < TM; c += 64) {
           uint32_t p[32];
 #pragma unroll
           for (int y = 0; y < 32; ++y) {
-            const float e0 = exp2_fast(fmaf(s[c + 2 * y], a.scale2, -base));
-            const float e1 = exp2_fast(fmaf(s[c + 2 * y + 1], a.scale2, -base));
-            sum[(2 * y) & 3] += e0;
-            sum[(2 * y + 1) & 3] += e1;
+            const float2 v = unpair(fma2(pair(s[c + 2 * y], s[c + 2 * y + 1]), scale, off));
+            const float e0 = exp2_fast(v.x), e1 = exp2_fast(v.y);
+            sum[y & 1] = add2(sum[y & 1], pair(e0, e1));
             p[y] = pack2(e0, e1);
           }
           tmem_st32_async(sa + c / 2, p);
+          tmem_wait_st();
+          tc::fence_before_sync();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&ctl->pfull[t][c / 64]);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        // values of a turn that not every row of the CTA sees
-        if (t == 0 && !(cnt == TM && j0 + TM - 1 <= i0 &&
-                        (a.window == 0 || i0 + nt - 1 - j0 < a.window || j0 + TM <= a.sinks))) {
-          const int vi = 2 * x + 1;
-          ok = wait_for(&ctl->full[vi % NS], (vi / NS) & 1, &ctl->abort);
-          ok = __all_sync(FULL, ok);
-          if (!ok) break;
-          char* vrow = ring + (vi % NS) * SLOT + r * 128;
-          if (r < cnt && j0 + r < n) {
-            __nv_bfloat162 bad = __float2bfloat162_rn(0.f);
-            const __nv_bfloat162 zero = bad;
-#pragma unroll
-            for (int c = 0; c < NH * 8; ++c) {
-              const int4 w =
-                  *reinterpret_cast<const int4*>(vrow + (c >> 3) * HALF + (((c ^ lane) & 7) * 16));
-              const __nv_bfloat162* e = reinterpret_cast<const __nv_bfloat162*>(&w);
-#pragma unroll
-              for (int y = 0; y < 4; ++y) bad = __hfma2(e[y], zero, bad);
-            }
-            if (__hisnan(bad.x) || __hisnan(bad.y)) ctl->strange = 1;
-          } else {
-#pragma unroll
-            for (int c = 0; c < NH * 8; ++c)
-              *reinterpret_cast<int4*>(vrow + (c >> 3) * HALF + (((c ^ lane) & 7) * 16)) =
-                  make_int4(0, 0, 0, 0);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          }
-        }
-        tmem_wait_st();
-        tc::fence_before_sync();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&ctl->pfull[t]);
+        const float2 both = unpair(add2(sum[0], sum[1]));
+        l += both.x + both.y;
       }
       if (ok && turns > 0) {
         ok = wait_for(&ctl->sfull[t], turns & 1, &ctl->abort);
