@@ -121,7 +121,6 @@ size_t attend_workspace(const KV&, int dtype, int H, int T);
 // The join of a split key axis (AttnArgs::part, ml).
 void* tensor_map_encoder();  // cuTensorMapEncodeTiled, or NULL
 bool attend_tc_takes(const KV&, int dtype, int G);
-int attend_tc_tiles(const KV&, int G, int T);
 int attend_tc_splits(const KV&, int G, int T);
 cudaError_t launch_attend_tc(const AttnArgs&, cudaStream_t);
 cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t);

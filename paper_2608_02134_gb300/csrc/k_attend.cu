@@ -16,12 +16,13 @@
 namespace gmc {
 
 namespace {
-constexpr int AT_THREADS = 256, AT_K = 64;
+constexpr int AT_K = 64;
 constexpr int AT_MAX_SPLITS = 32;
 
-template <int DP> constexpr int at_rows() { return DP > 128 ? 64 : 128; }
+constexpr int AT_ROWS = 64;
+template <int DP> constexpr int at_threads() { return DP > 128 ? 256 : 128; }
 template <int DP> constexpr size_t at_smem() {
-  return (size_t)at_rows<DP>() * DP * 4 + 2 * (size_t)AT_K * DP * 4 + at_rows<DP>() * AT_K * 4 +
+  return (size_t)AT_ROWS * DP * 4 + 2 * (size_t)AT_K * DP * 4 + AT_ROWS * AT_K * 4 +
          2 * AT_K * 8;
 }
 
@@ -57,8 +58,8 @@ __device__ __forceinline__ void times_values(float (&o)[RT][NC * 4], const char*
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(AT_THREADS) k_attend_simt(AttnArgs a, int gsub, int ntile) {
-  constexpr int R = at_rows<DP>(), RT = R / 16, P = DP / 4, NC = DP / 64, E = 16 / sizeof(T);
+__global__ void __launch_bounds__(at_threads<DP>(), DP > 128 ? 1 : 2) k_attend_simt(AttnArgs a, int gsub, int ntile) {
+  constexpr int R = AT_ROWS, AT_THREADS = at_threads<DP>(), RT = R * 16 / AT_THREADS, P = DP / 4, NC = DP / 64, E = 16 / sizeof(T);
   extern __shared__ __align__(128) char smem[];
   char* Qs = smem;
   char* Ks = Qs + R * DP * 4;
@@ -152,7 +153,7 @@ __global__ void __launch_bounds__(AT_THREADS) k_attend_simt(AttnArgs a, int gsub
     for (int i = 0; i < RT; ++i)
 #pragma unroll
       for (int c = 0; c < 4; ++c) s[i][c] = 0.f;
-#pragma unroll 2
+#pragma unroll 4
     for (int p = 0; p < P; ++p) {
       float4 kv[4];
 #pragma unroll
@@ -298,17 +299,16 @@ __global__ void __launch_bounds__(256) k_attend_join(AttnArgs a) {
   }
 }
 
-int simt_rows(int d) { return d > 128 ? 64 : 128; }
-
 // Parts of the key axis: where the rows' tiles leave SMs idle, as many as fill them,
 // four turns of 64 keys each at least.
 int simt_splits(const KV& c, int G, int T) {
-  const int R = simt_rows(c.d), gsub = std::min(G, R);
+  const int R = AT_ROWS, gsub = std::min(G, R);
   const long long ctas =
       (long long)c.B * c.Hkv * ceil_div(G, gsub) * ceil_div(T, std::max(1, R / gsub));
-  if (ctas >= 152) return 1;
+  const int fill = (c.d > 128 ? 1 : 2) * sm_count();
+  if (ctas >= fill / 2) return 1;
   return (int)std::max<long long>(
-      1, std::min<long long>({152 / ctas, AT_MAX_SPLITS, ceil_div(c.cap, 4 * AT_K)}));
+      1, std::min<long long>({fill / ctas, AT_MAX_SPLITS, ceil_div(c.cap, 4 * AT_K)}));
 }
 }  // namespace
 
@@ -328,7 +328,7 @@ cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t st) {
 }
 
 cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t st, int* launches) {
-  const int R = simt_rows(a.c.d), gsub = std::min(a.G, R), ng = ceil_div(a.G, gsub);
+  const int R = AT_ROWS, gsub = std::min(a.G, R), ng = ceil_div(a.G, gsub);
   const int ntile = ceil_div(a.T, R / gsub);
   const bool tensor = attend_tc_takes(a.c, dtype, a.G);
   a.splits = tensor ? attend_tc_splits(a.c, a.G, a.T) : simt_splits(a.c, a.G, a.T);
@@ -342,7 +342,7 @@ cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t st, int*
 #define GMC_AT(T, DP)                                                                     \
   ((e = set_smem_limit((const void*)k_attend_simt<T, DP>, at_smem<DP>())) != cudaSuccess  \
        ? e                                                                                \
-       : launch_k(k_attend_simt<T, DP>, grid, dim3(AT_THREADS), at_smem<DP>(), st, 1, a,  \
+       : launch_k(k_attend_simt<T, DP>, grid, dim3(at_threads<DP>()), at_smem<DP>(), st, 1, a,  \
                   gsub, ntile))
   if (tensor)
     e = launch_attend_tc(a, st);

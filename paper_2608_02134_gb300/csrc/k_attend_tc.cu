@@ -36,11 +36,15 @@ namespace gmc {
 
 namespace {
 constexpr int TM = 128;                 // rows of a tile, keys of a turn
-constexpr int T_THREADS = 320;          // 2 x 4 softmax warps, a copying and an issuing one
 constexpr long long T_WAIT = 4000000000LL;
 constexpr float GROWN = 8.f;            // powers of two the maximum may fall behind
 
-template <int DP> constexpr int t_slots() { return DP == 128 ? 5 : 8; }
+// 128-row slots of the ring: what shared memory holds beside the queries, for one CTA of
+// two tiles an SM or two CTAs of one.
+template <int DP, int TILES> constexpr int t_slots() {
+  return TILES == 2 ? (DP == 128 ? 5 : 8) : (DP == 128 ? 2 : 4);
+}
+template <int TILES> constexpr int t_threads() { return TILES * 128 + 64; }
 
 struct TCtl {
   uint64_t full[8], empty[8], qfull, sfull[2], pfull[2][2], drained;
@@ -49,29 +53,64 @@ struct TCtl {
   int strange;
 };
 
-template <int DP> constexpr size_t t_smem() {
-  return 1024 + (size_t)(2 + t_slots<DP>()) * TM * DP * 2 + sizeof(TCtl);
+template <int DP, int TILES> constexpr size_t t_smem() {
+  return 1024 + (size_t)(TILES + t_slots<DP, TILES>()) * TM * DP * 2 + sizeof(TCtl);
+}
+
+// Division by a number that the host knows: n / d = (n * mul) >> (32 + shift), exact for
+// 0 <= n < 2^31 (mul = ceil(2^(32 + shift) / d) with 2^shift >= d / 2).
+struct Div {
+  unsigned mul, shift, d;
+  __device__ __forceinline__ int of(int n) const {
+    return d == 1 ? n : (int)(__umulhi((unsigned)n, mul) >> shift);
+  }
+};
+Div make_div(int d) {
+  Div v;
+  v.d = (unsigned)d;
+  v.shift = 0;
+  while ((2ull << v.shift) < (unsigned long long)d) ++v.shift;
+  v.mul = (unsigned)(((1ull << (32 + v.shift)) + d - 1) / d);
+  return v;
 }
 
 // Turns of keys: pages of up to 128 slots are taken as many as fit whole, larger ones
 // in pieces of 128 (the last one short).
 struct Turns {
   int ps, kt, ppt, tpp;
+  Div by_ps, by_kt, by_tpp, by_g;
   __device__ __forceinline__ int of(int j) const {  // the turn that holds place j
-    if (ps <= TM) return j / kt;
-    const int p = j / ps;
+    if (ps <= TM) return by_kt.of(j);
+    const int p = by_ps.of(j);
     return p * tpp + (j - p * ps) / TM;
   }
   __device__ __forceinline__ int first(int u) const {
     if (ps <= TM) return u * kt;
-    const int p = u / tpp;
+    const int p = by_tpp.of(u);
     return p * ps + (u - p * tpp) * TM;
   }
   __device__ __forceinline__ int rows(int u) const {
     if (ps <= TM) return kt;
-    return min(TM, ps - (u - u / tpp * tpp) * TM);
+    return min(TM, ps - (u - by_tpp.of(u) * tpp) * TM);
   }
 };
+Turns make_turns(int ps, int G) {
+  Turns t;
+  t.ps = ps;
+  t.ppt = ps <= TM ? TM / ps : 1;
+  t.kt = ps <= TM ? t.ppt * ps : TM;
+  t.tpp = ceil_div(ps, TM);
+  t.by_ps = make_div(ps);
+  t.by_kt = make_div(t.kt);
+  t.by_tpp = make_div(t.tpp);
+  t.by_g = make_div(G);
+  return t;
+}
+
+// Bits 0 .. n - 1 of a word.
+__device__ __forceinline__ uint32_t below(int n) {
+  return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1;
+}
 
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile int* abort) {
   if (tc::mbar_try_wait(bar, parity)) return true;
@@ -301,24 +340,79 @@ __device__ __forceinline__ bool look_over(TCtl* ctl, char* slot, int s, uint32_t
   return true;
 }
 
-template <int DP>
-__global__ void __launch_bounds__(T_THREADS, 1)
+// The sequence and the tile of it (`tokens` new tokens each) that is number c of all.
+__device__ __forceinline__ bool find_tile(const AttnArgs& a, int c, int tokens, int* b, int* tile,
+                                          NewRows* nr, int* n) {
+  if (!a.q_offsets) {
+    const int each = ceil_div(a.T, tokens);
+    *b = c / each;
+    *tile = c - *b * each;
+    if (*b >= a.c.B) return false;
+    *nr = new_rows(a.q_offsets, *b, a.rows, a.T, a.c.status);
+    *n = kv_len(a.c, *b);
+    return true;
+  }
+  // each lane counts the tiles of some consecutive sequences
+  const int lane = threadIdx.x & 31, cs = ceil_div(a.c.B, 32);
+  const int b0 = min(a.c.B, lane * cs), b1 = min(a.c.B, b0 + cs);
+  int mine = 0, len = 0;
+  NewRows last = {0, 0};
+#pragma unroll 4
+  for (int x = b0; x < b1; ++x) {
+    last = new_rows(a.q_offsets, x, a.rows, a.T, a.c.status);
+    len = kv_len(a.c, x);
+    mine += ceil_div(last.T, tokens);
+  }
+  int sum = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(FULL, sum, o);
+    if (lane >= o) sum += y;
+  }
+  if (c >= __shfl_sync(FULL, sum, 31)) return false;
+  const int lo = __popc(__ballot_sync(FULL, sum - mine <= c)) - 1;
+  int u = c - __shfl_sync(FULL, sum - mine, lo);
+  last.off = __shfl_sync(FULL, last.off, lo);
+  last.T = __shfl_sync(FULL, last.T, lo);
+  len = __shfl_sync(FULL, len, lo);
+  if (cs == 1) {
+    *b = lo;
+    *tile = u;
+    *nr = last;
+    *n = len;
+    return true;
+  }
+  for (int x = lo * cs;; ++x) {
+    *nr = new_rows(a.q_offsets, x, a.rows, a.T, a.c.status);
+    const int here = ceil_div(nr->T, tokens);
+    if (u < here) {
+      *b = x;
+      *tile = u;
+      *n = kv_len(a.c, x);
+      return true;
+    }
+    u -= here;
+  }
+}
+
+template <int DP, int TILES>
+__global__ void __launch_bounds__(t_threads<TILES>(), 3 - TILES)
     k_attend_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
-                const __grid_constant__ CUtensorMap vmap, AttnArgs a, int npair, int tiles) {
-  constexpr int NS = t_slots<DP>(), SLOT = TM * DP * 2, HALF = TM * 128, NH = DP / 64;
+                const __grid_constant__ CUtensorMap vmap, AttnArgs a, Turns tn) {
+  constexpr int NS = t_slots<DP, TILES>(), THREADS = t_threads<TILES>(), COPY = 4 * TILES,
+                ISSUE = COPY + 1, SLOT = TM * DP * 2, HALF = TM * 128, NH = DP / 64;
   extern __shared__ char raw[];
   char* smem = reinterpret_cast<char*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   char* Qs = smem;
-  char* ring = Qs + 2 * SLOT;
+  char* ring = Qs + TILES * SLOT;
   TCtl* ctl = reinterpret_cast<TCtl*>(ring + NS * SLOT);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
-  Turns tn;
-  tn.ps = a.c.ps;
-  tn.ppt = tn.ps <= TM ? TM / tn.ps : 1;
-  tn.kt = tn.ps <= TM ? tn.ppt * tn.ps : TM;
-  tn.tpp = ceil_div(tn.ps, TM);
-
+  if (warp == COPY && lane == 0) {
+    tc::prefetch_tmap(&qmap);
+    tc::prefetch_tmap(&kmap);
+    tc::prefetch_tmap(&vmap);
+  }
   if (tid == 0) {
     for (int s = 0; s < NS; ++s) {
       tc::mbar_init(&ctl->full[s], 1);
@@ -326,7 +420,7 @@ __global__ void __launch_bounds__(T_THREADS, 1)
     }
     tc::mbar_init(&ctl->qfull, 1);
     tc::mbar_init(&ctl->drained, 1);
-    for (int x = 0; x < 2; ++x) {
+    for (int x = 0; x < TILES; ++x) {
       tc::mbar_init(&ctl->sfull[x], 1);
       tc::mbar_init(&ctl->pfull[x][0], 4);
       tc::mbar_init(&ctl->pfull[x][1], 4);
@@ -335,32 +429,26 @@ __global__ void __launch_bounds__(T_THREADS, 1)
     ctl->strange = 0;
     tc::fence_mbar_init();
   }
-  if (warp == 8 && lane == 0) {
-    tc::prefetch_tmap(&qmap);
-    tc::prefetch_tmap(&kmap);
-    tc::prefetch_tmap(&vmap);
-  }
+  grid_dep_launch();
+  grid_dep_wait();
+  const int h = blockIdx.y, split = blockIdx.x % a.splits;
+  const int tpt = TM / a.G;  // tokens of a tile
+  int b, tile, n;
+  NewRows nr;
+  if (!find_tile(a, blockIdx.x / a.splits, tpt * TILES, &b, &tile, &nr, &n)) return;
+  // the last tokens see the most keys: they go first
+  const int t0 = (ceil_div(nr.T, tpt * TILES) - 1 - tile) * tpt * TILES;
+  const int nt = min(tpt * TILES, nr.T - t0);  // tokens of this CTA
   if (tn.kt < TM) {  // rows of a slot that no copy writes
     const int per = (TM - tn.kt) * 8;
-    for (int x = tid; x < NS * NH * per; x += T_THREADS) {
+    for (int x = tid; x < NS * NH * per; x += THREADS) {
       const int s = x / per, y = x - s * per;
       *reinterpret_cast<int4*>(ring + s * HALF + tn.kt * 128 + y * 16) = make_int4(0, 0, 0, 0);
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  grid_dep_launch();
-  grid_dep_wait();
-  const int b = blockIdx.z, h = blockIdx.y;
-  const int split = blockIdx.x % a.splits;
-  const int tpt = TM / a.G;  // tokens of a tile
-  const NewRows nr = new_rows(a.q_offsets, b, a.rows, a.T, a.c.status);
-  const int n = kv_len(a.c, b);
-  // the last tokens see the most keys: they go first
-  const int t0 = (npair - 1 - (int)blockIdx.x / a.splits) * tpt * tiles;
-  const int nt = min(tpt * tiles, nr.T - t0);  // tokens of this CTA
-  if (nt <= 0) return;
-  if (warp == 9) {
-    tc::tmem_alloc(&ctl->tmem, 512);
+  if (warp == ISSUE) {
+    tc::tmem_alloc(&ctl->tmem, 256 * TILES);
     tc::tmem_relinquish();
   }
   tc::fence_before_sync();
@@ -368,7 +456,7 @@ __global__ void __launch_bounds__(T_THREADS, 1)
   tc::fence_after_sync();
   const uint32_t tmem = ctl->tmem;
   const int i0 = n - nr.T + t0;
-  const int two = nt > tpt ? 2 : 1;
+  const int two = TILES == 2 && nt > tpt ? 2 : 1;
   int turns = 0, na = 0, ub0 = 0, x0 = 0;
   {
     const Seen seen = seen_keys(i0, i0 + nt - 1, a.window, a.sinks);
@@ -384,7 +472,7 @@ __global__ void __launch_bounds__(T_THREADS, 1)
   auto turn_at = [&](int x) { return x0 + x < na ? x0 + x : ub0 + x0 + x - na; };
 
   int issued = 0;  // copies started (copying warp)
-  if (turns > 0 && warp == 8) {
+  if (turns > 0 && warp == COPY) {
     // ---- copies ---------------------------------------------------------------------
     if (lane == 0) {
       tc::mbar_arrive_expect_tx(&ctl->qfull, two * tpt * a.G * DP * 2);
@@ -401,7 +489,7 @@ __global__ void __launch_bounds__(T_THREADS, 1)
       if (pg >= tn.ppt || x >= turns) return a.c.num_pages;
       const int u = turn_at(x), j = tn.first(u) + pg * tn.ps;
       if (j >= n) return a.c.num_pages;
-      const int p = j / tn.ps;
+      const int p = tn.by_ps.of(j);
       *slot = j - p * tn.ps;
       const int page = a.c.table[(long long)b * a.c.max_pages + p];
       if ((unsigned)page < (unsigned)a.c.num_pages) return page;
@@ -428,7 +516,7 @@ __global__ void __launch_bounds__(T_THREADS, 1)
       page = npage;
       slot = nslot;
     }
-  } else if (turns > 0 && warp == 9) {
+  } else if (turns > 0 && warp == ISSUE) {
     // ---- products -------------------------------------------------------------------
     constexpr uint32_t sdesc = tc::idesc_bf16_f32(TM, TM);
     constexpr uint32_t odesc = tc::idesc_bf16_f32(TM, DP) | (1u << 16);  // B is MN-major
@@ -455,8 +543,8 @@ __global__ void __launch_bounds__(T_THREADS, 1)
       for (int t = 0; t < two; ++t) logits(t, 0);
       commit(go, &ctl->empty[0]);
     }
-    int vs = 1, ks = 2 % NS;        // slots of this turn's values and the next one's keys
-    uint32_t vp = 0, kp = 2 / NS;   // and their parities
+    int vs = 1, ks = 2 % NS;       // slots of this turn's values and the next one's keys
+    uint32_t vp = 0, kp = 2 / NS;  // and their parities
 #pragma unroll 1
     for (int x = 0; x < turns && ok; ++x) {
 #pragma unroll 1
@@ -470,7 +558,7 @@ __global__ void __launch_bounds__(T_THREADS, 1)
           tc::fence_after_sync();
 #pragma unroll
           for (int k = half * (TM / 32); k < (half + 1) * (TM / 32); ++k)
-            mma_ts(go, tmem + 2 * TM + t * TM, tmem + t * TM + k * 8, vb + k * (2048 / 16), odesc,
+            mma_ts(go, tmem + TILES * TM + t * TM, tmem + t * TM + k * 8, vb + k * (2048 / 16), odesc,
                    x > 0 || k > 0);
         }
         if (!ok) break;
@@ -503,15 +591,15 @@ __global__ void __launch_bounds__(T_THREADS, 1)
       }
     }
     __syncwarp();
-  } else if (warp < 8) {
+  } else if (warp < COPY) {
     // ---- weights --------------------------------------------------------------------
     const int t = warp >> 2, r = tid & (TM - 1);
-    const int tok = r / a.G, g = r - tok * a.G;
+    const int tok = tn.by_g.of(r), g = r - tok * a.G;
     const int mine = min(tpt, nt - t * tpt);  // tokens of this tile
     const bool valid = tok < mine;
     const int ti0 = i0 + t * tpt, i = ti0 + tok;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's lane quarter
-    const uint32_t sa = tmem + lanes + t * TM, oa = tmem + lanes + 2 * TM + t * TM;
+    const uint32_t sa = tmem + lanes + t * TM, oa = tmem + lanes + TILES * TM + t * TM;
     float m = -INFINITY, l = 0.f;
     bool ok = true;
     if (mine > 0) {
@@ -532,8 +620,12 @@ __global__ void __launch_bounds__(T_THREADS, 1)
           const int lo = a.window > 0 ? i - a.window + 1 - j0 : 0;  // from lo on
           const int sk = a.sinks - j0;                              // or before sk
 #pragma unroll
-          for (int c = 0; c < TM; ++c)
-            if (!(c < hi && (c >= lo || c < sk))) s[c] = -INFINITY;
+          for (int c = 0; c < TM; c += 32) {
+            const uint32_t in = below(hi - c) & (~below(lo - c) | below(sk - c));
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+              if (!(in >> y & 1)) s[c + y] = -INFINITY;
+          }
         }
         float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
@@ -600,7 +692,7 @@ __global__ void __launch_bounds__(T_THREADS, 1)
         const long long pr = ((long long)split * a.rows + row) * a.H + hq;
         if (valid) a.ml[pr] = ok ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
         if (ok && turns > 0)
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < DP; c += 32) {
             float o[32];
             tc::tmem_ld32(oa + c, o);
@@ -615,9 +707,10 @@ __global__ void __launch_bounds__(T_THREADS, 1)
         const float inv = l == 0.f ? 0.f : 1.f / l;
         if (valid && a.lse)
           a.lse[row * a.H + hq] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+        const long long mine_at = valid ? row * a.o_row + (long long)hq * a.o_head : -1;
         // 32 rows a warp through its part of the queries' tile, whole rows stored
         char* st = Qs + t * SLOT + (warp & 3) * 32 * DP * 2;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < DP; c += 32) {
           float o[32];
           if (ok && turns > 0) {
@@ -636,25 +729,25 @@ __global__ void __launch_bounds__(T_THREADS, 1)
         }
         __syncwarp();
         constexpr int PC = DP / 8, RPI = 32 / PC;
-        for (int y = lane / PC; y < 32; y += RPI) {
-          const int rr = (warp & 3) * 32 + y, tk = rr / a.G, gg = rr - tk * a.G, pc = lane % PC;
-          if (tk < mine && pc * 8 < a.c.d) {
-            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) +
-                                 (nr.off + t0 + t * tpt + tk) * a.o_row +
-                                 (long long)(h * a.G + gg) * a.o_head + pc * 8;
-            *reinterpret_cast<int4*>(out) =
+        const int pc = lane % PC;
+#pragma unroll 8
+        for (int y0 = 0; y0 < 32; y0 += RPI) {
+          const int y = y0 + lane / PC;
+          // the row's place in the output, from the thread that holds it
+          const long long at = __shfl_sync(FULL, mine_at, y);
+          if (at >= 0 && pc * 8 < a.c.d)
+            *reinterpret_cast<int4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at + pc * 8) =
                 *reinterpret_cast<const int4*>(st + y * DP * 2 + ((pc ^ (y & 7)) * 16));
-          }
         }
       }
     }
   }
   tc::fence_before_sync();
   __syncthreads();
-  if (warp == 9) tc::tmem_dealloc(tmem, 512);
+  if (warp == ISSUE) tc::tmem_dealloc(tmem, 256 * TILES);
   if (ctl->abort) {
     if (tid == 0) set_status(a.c.status, GMC_STATUS_TIMEOUT);
-    if (warp == 8) {  // copies in flight land before shared memory is given back
+    if (warp == COPY) {  // copies in flight land before shared memory is given back
       const long long end = clock64() + T_WAIT;
       for (int q = issued > NS ? issued - NS : 0; q < issued; ++q)
         while (!tc::mbar_try_wait(&ctl->full[q % NS], (q / NS) & 1) && clock64() < end) {}
@@ -662,7 +755,7 @@ __global__ void __launch_bounds__(T_THREADS, 1)
     return;
   }
   if (ctl->strange) {
-    for (int rr = warp; rr < nt * a.G; rr += T_THREADS / 32) {
+    for (int rr = warp; rr < nt * a.G; rr += THREADS / 32) {
       const int tk = rr / a.G, g = rr - tk * a.G, hq = h * a.G + g;
       const long long row = nr.off + t0 + tk;
       float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
@@ -707,21 +800,30 @@ cudaError_t make_map(CUtensorMap* map, const void* base, int rank, const cuuint6
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-// CTAs without a split, and turns of the longest key axis.
-long long tc_ctas(const KV& c, int G, int T, int tiles) {
-  return (long long)c.B * c.Hkv * ceil_div(T, TM / G * tiles);
+// CTAs without a split: at most this many tiles of `tiles` x (128 / G) tokens.
+long long tc_ctas(const KV& c, int G, long long rows, int T, int tiles) {
+  const int tokens = TM / G * tiles;
+  const long long each = (long long)c.B * ceil_div(T, tokens);
+  return c.Hkv * std::min(each, rows / tokens + c.B);
+}
+// One tile a CTA and two CTAs an SM where the key axis is short and the CTAs are more than
+// a wave: one's first copies and last stores (3 us each) hide behind the other's products
+// (32 questions of 16 to 256 tokens on up to 513 keys: two tiles 56.6 us, one 52.7; 8 x
+// 512 tokens on 2,048: 122 and 117); on longer axes two tiles share each key's copy
+// (4,096 tokens: 112 and 124; 1,024 tokens, less than a wave: 21.3 and 21.7).
+int tc_tiles(const AttnArgs& a) {
+  long long most = a.c.cap;
+  if (a.window > 0) most = std::min(most, (long long)a.window + a.sinks + a.T);
+  return most <= 18 * TM && tc_ctas(a.c, a.G, a.rows, a.T, 2) > sm_count() ? 1 : 2;
 }
 }  // namespace
 
-// One tile a CTA where two would leave SMs idle.
-int attend_tc_tiles(const KV& c, int G, int T) {
-  return T > TM / G && tc_ctas(c, G, T, 2) >= 152 ? 2 : 1;
-}
 // Parts of the key axis: as many as fill the SMs, two turns each at least.
 int attend_tc_splits(const KV& c, int G, int T) {
-  const long long ctas = tc_ctas(c, G, T, attend_tc_tiles(c, G, T));
-  if (ctas >= 152) return 1;
-  return (int)std::max<long long>(1, std::min<long long>({152 / ctas, 32, c.cap / (2 * TM)}));
+  const long long rows = (long long)c.B * T, ctas = tc_ctas(c, G, rows, T, 1);
+  const long long fill = 2LL * sm_count();
+  if (ctas >= fill / 2) return 1;
+  return (int)std::max<long long>(1, std::min<long long>({fill / ctas, 32, c.cap / (2 * TM)}));
 }
 
 bool attend_tc_takes(const KV& c, int dtype, int G) {
@@ -732,8 +834,22 @@ bool attend_tc_takes(const KV& c, int dtype, int G) {
          fits(c.slot_stride, c.ps);
 }
 
+namespace {
+template <int DP, int TILES>
+cudaError_t tc_launch(const AttnArgs& a, const CUtensorMap& qm, const CUtensorMap& km,
+                      const CUtensorMap& vm, cudaStream_t st) {
+  constexpr size_t smem = t_smem<DP, TILES>();
+  const cudaError_t e = set_smem_limit((const void*)k_attend_tc<DP, TILES>, smem);
+  if (e != cudaSuccess) return e;
+  const long long tiles = tc_ctas(a.c, a.G, a.rows, a.T, TILES) / a.c.Hkv;
+  return launch_k(k_attend_tc<DP, TILES>, dim3((unsigned)(tiles * a.splits), a.c.Hkv),
+                  dim3(t_threads<TILES>()), smem, st, 1, qm, km, vm, a,
+                  make_turns(a.c.ps, a.G));
+}
+}  // namespace
+
 cudaError_t launch_attend_tc(const AttnArgs& a, cudaStream_t st) {
-  const int tpt = TM / a.G, NHd = a.c.d <= 64 ? 1 : 2, tiles = attend_tc_tiles(a.c, a.G, a.T);
+  const int tpt = TM / a.G;
   CUtensorMap qm, km, vm;
   auto stride = [&](long long s, int n) {
     return n == 1 ? (cuuint64_t)a.c.d * 2 : (cuuint64_t)s * 2;
@@ -755,16 +871,10 @@ cudaError_t launch_attend_tc(const AttnArgs& a, cudaStream_t st) {
     if ((e = make_map(&km, a.c.k, 4, dims, strides, box)) != cudaSuccess) return e;
     if ((e = make_map(&vm, a.c.v, 4, dims, strides, box)) != cudaSuccess) return e;
   }
-  const int npair = ceil_div(a.T, tpt * tiles);
-  const dim3 grid((unsigned)npair * a.splits, a.c.Hkv, a.c.B);
-  if (NHd == 1) {
-    if ((e = set_smem_limit((const void*)k_attend_tc<64>, t_smem<64>())) != cudaSuccess) return e;
-    return launch_k(k_attend_tc<64>, grid, dim3(T_THREADS), t_smem<64>(), st, 1, qm, km, vm, a,
-                    npair, tiles);
-  }
-  if ((e = set_smem_limit((const void*)k_attend_tc<128>, t_smem<128>())) != cudaSuccess) return e;
-  return launch_k(k_attend_tc<128>, grid, dim3(T_THREADS), t_smem<128>(), st, 1, qm, km, vm, a,
-                  npair, tiles);
+  const bool one = a.splits > 1 || tc_tiles(a) == 1;
+  if (a.c.d <= 64)
+    return one ? tc_launch<64, 1>(a, qm, km, vm, st) : tc_launch<64, 2>(a, qm, km, vm, st);
+  return one ? tc_launch<128, 1>(a, qm, km, vm, st) : tc_launch<128, 2>(a, qm, km, vm, st);
 }
 
 }  // namespace gmc
