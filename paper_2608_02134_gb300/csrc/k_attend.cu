@@ -28,7 +28,7 @@ template <int DP> constexpr size_t at_smem() {
 
 // o += weights x values of one tile; SKIP: zero weights are left out.
 template <int RT, int NC, bool SKIP>
-__device__ __forceinline__ void times_values(float (&o)[RT][NC * 4], const char* Pr,
+__device__ __forceinline__ void times_values(f32x2 (&o)[RT][NC * 2], const char* Pr,
                                              const char* Vs, int tx, int sw) {
 #pragma unroll 1
   for (int k4 = 0; k4 < AT_K / 4; ++k4) {
@@ -39,18 +39,20 @@ __device__ __forceinline__ void times_values(float (&o)[RT][NC * 4], const char*
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int k = k4 * 4 + e;
+      ulonglong2 vv[NC];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const float4 vv = *reinterpret_cast<const float4*>(Vs + k * (NC * 256) +
-                                                           (((tx + 16 * c) ^ (k & 7)) * 16));
+      for (int c = 0; c < NC; ++c)
+        vv[c] = *reinterpret_cast<const ulonglong2*>(Vs + k * (NC * 256) +
+                                                     (((tx + 16 * c) ^ (k & 7)) * 16));
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-          const float p = e == 0 ? pv[i].x : e == 1 ? pv[i].y : e == 2 ? pv[i].z : pv[i].w;
-          if (SKIP && p == 0.f) continue;
-          o[i][4 * c + 0] = fmaf(p, vv.x, o[i][4 * c + 0]);
-          o[i][4 * c + 1] = fmaf(p, vv.y, o[i][4 * c + 1]);
-          o[i][4 * c + 2] = fmaf(p, vv.z, o[i][4 * c + 2]);
-          o[i][4 * c + 3] = fmaf(p, vv.w, o[i][4 * c + 3]);
+      for (int i = 0; i < RT; ++i) {
+        const float p = e == 0 ? pv[i].x : e == 1 ? pv[i].y : e == 2 ? pv[i].z : pv[i].w;
+        if (SKIP && p == 0.f) continue;
+        const f32x2 pp = pair(p, p);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          o[i][2 * c] = fma2(pp, vv[c].x, o[i][2 * c]);
+          o[i][2 * c + 1] = fma2(pp, vv[c].y, o[i][2 * c + 1]);
         }
       }
     }
@@ -131,7 +133,8 @@ __global__ void __launch_bounds__(at_threads<DP>(), DP > 128 ? 1 : 2) k_attend_s
   __syncthreads();
   if (u0 < u1) copy_rows(Ks, a.c.k, u0);
 
-  float o[RT][NC * 4], m[RT], l[RT];
+  f32x2 o[RT][NC * 2];  // columns in pairs
+  float m[RT], l[RT];
   int place[RT];  // of the row's token; below 0 also for rows that are none
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
@@ -140,7 +143,7 @@ __global__ void __launch_bounds__(at_threads<DP>(), DP > 128 ? 1 : 2) k_attend_s
     m[i] = -INFINITY;
     l[i] = 0.f;
 #pragma unroll
-    for (int y = 0; y < NC * 4; ++y) o[i][y] = 0.f;
+    for (int y = 0; y < NC * 2; ++y) o[i][y] = 0ull;
   }
   const int sw = ty & 7;
   for (int u = u0; u < u1; ++u) {
@@ -149,27 +152,35 @@ __global__ void __launch_bounds__(at_threads<DP>(), DP > 128 ? 1 : 2) k_attend_s
     __syncthreads();  // the keys of u are there; the values of u - 1 are done with
     copy_rows(Vs, a.c.v, u);
     float s[RT][4];
+    {
+      f32x2 z[RT][4];  // sums over even and odd columns
 #pragma unroll
-    for (int i = 0; i < RT; ++i)
+      for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[i][c] = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < P; ++p) {
-      float4 kv[4];
+        for (int c = 0; c < 4; ++c) z[i][c] = 0ull;
+#pragma unroll 2
+      for (int p = 0; p < P; ++p) {
+        ulonglong2 kv[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int r = tx + 16 * c;
-        kv[c] = *reinterpret_cast<const float4*>(Ks + r * DP * 4 + ((p ^ (r & 7)) * 16));
+        for (int c = 0; c < 4; ++c) {
+          const int r = tx + 16 * c;
+          kv[c] = *reinterpret_cast<const ulonglong2*>(Ks + r * DP * 4 + ((p ^ (r & 7)) * 16));
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          const ulonglong2 qv =
+              *reinterpret_cast<const ulonglong2*>(Qs + (ty * RT + i) * DP * 4 + ((p ^ sw) * 16));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) z[i][c] = fma2(qv.y, kv[c].y, fma2(qv.x, kv[c].x, z[i][c]));
+        }
       }
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        const float4 qv =
-            *reinterpret_cast<const float4*>(Qs + (ty * RT + i) * DP * 4 + ((p ^ sw) * 16));
+      for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          s[i][c] = fmaf(qv.x, kv[c].x,
-                         fmaf(qv.y, kv[c].y, fmaf(qv.z, kv[c].z, fmaf(qv.w, kv[c].w, s[i][c]))));
-      }
+        for (int c = 0; c < 4; ++c) {
+          const float2 v = unpair(z[i][c]);
+          s[i][c] = v.x + v.y;
+        }
     }
     const int j0 = key0(u), j1 = key1(u);
     // whether every row sees every key of the tile
@@ -200,8 +211,11 @@ __global__ void __launch_bounds__(at_threads<DP>(), DP > 128 ? 1 : 2) k_attend_s
                                   (k & 3) * 4) = p;
       }
       l[i] = l[i] * f + sum;
+      if (f != 1.f) {
+        const f32x2 ff = pair(f, f);
 #pragma unroll
-      for (int y = 0; y < NC * 4; ++y) o[i][y] *= f;
+        for (int y = 0; y < NC * 2; ++y) o[i][y] = mul2(o[i][y], ff);
+      }
     }
     __syncthreads();  // the keys of u are done with, the weights written
     if (u + 1 < u1) copy_rows(Ks, a.c.k, u + 1); else cp_async_commit();
@@ -239,9 +253,10 @@ __global__ void __launch_bounds__(at_threads<DP>(), DP > 128 ? 1 : 2) k_attend_s
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const int x = (tx + 16 * c) * 4;
+        const float2 lo = unpair(o[i][2 * c]), hi = unpair(o[i][2 * c + 1]);
         if (x < a.c.d)
           *reinterpret_cast<float4*>(a.part + pr * a.c.d + x) =
-              make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
+              make_float4(lo.x, lo.y, hi.x, hi.y);
       }
       continue;
     }
@@ -250,12 +265,15 @@ __global__ void __launch_bounds__(at_threads<DP>(), DP > 128 ? 1 : 2) k_attend_s
       a.lse[row * a.H + hq] = L == 0.f ? -INFINITY : (m[i] + log2f(L)) * LN2;
     T* out = reinterpret_cast<T*>(a.out) + row * a.o_row + hq * a.o_head;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int x = (tx + 16 * c) * 4 + e;
-        if (x < a.c.d) out[x] = from_f32<T>(o[i][4 * c + e] * inv);
-      }
+    for (int c = 0; c < NC; ++c) {
+      const int x = (tx + 16 * c) * 4;
+      if (x >= a.c.d) continue;
+      const float2 lo = unpair(o[i][2 * c]), hi = unpair(o[i][2 * c + 1]);
+      out[x] = from_f32<T>(lo.x * inv);
+      out[x + 1] = from_f32<T>(lo.y * inv);
+      out[x + 2] = from_f32<T>(hi.x * inv);
+      out[x + 3] = from_f32<T>(hi.y * inv);
+    }
   }
 }
 
