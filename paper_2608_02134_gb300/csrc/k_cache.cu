@@ -1,10 +1,8 @@
 // The key-value cache's own kernels: new rows written to their pages, and the
 // best-scored rows of a sequence moved to fresh pages.
-#include <cooperative_groups.h>
+#include <algorithm>
 
 #include "cache.cuh"
-
-namespace cg = cooperative_groups;
 
 namespace gmc {
 
@@ -67,24 +65,29 @@ __global__ void __launch_bounds__(AP_THREADS)
 }
 
 // ---------------------------------------------------------------------------
-// Eviction: one cluster per (sequence, key head), CTA r owning the r-th share of
-// the sequence's places.  The keep-th largest score is found by a radix search
-// over the scores' order-preserving 32-bit keys, eight bits a pass: every CTA
-// counts its share, the counts meet through distributed shared memory.  Keys
-// equal to the threshold are taken from the lowest place on.  Then each CTA
-// writes its kept places in order and copies their rows.
+// Eviction: S CTAs a (sequence, key head), each of which finds the same threshold from
+// all of the pair's scores (they are a hundredth of the rows' bytes; finding it once and
+// telling the others took a cluster's barriers, 17.4 us for 4 x 16,004 places where this
+// takes 14.9), and then writes and copies an equal part of the kept places.
+//
+// The threshold, the keep-th largest of the scores' order-preserving 32-bit keys, is
+// found in three passes of 11, 11 and 10 bits over a histogram in shared memory; keys
+// equal to it are taken from the lowest place on.  A thread holds up to 16 consecutive
+// keys in registers, through all passes where the sequence has no more than 16,384 places,
+// so one scan over the threads' counts numbers the kept places.
 // ---------------------------------------------------------------------------
-constexpr int EV_THREADS = 512, EV_WARPS = EV_THREADS / 32;
-constexpr int EV_KEYS = 8192;  // keys of a share held in shared memory; the others are read again
+constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32;
+constexpr int EV_EACH = 16;
+constexpr int EV_BINS = 2048, EV_COPIES = 4;  // copies by lane: fewer meet at one address
+constexpr int EV_LIST = 8192;                 // kept places of a CTA held in shared memory
 
 struct EvSmem {
-  int hist[2][256];
-  int wgt[EV_WARPS], weq[EV_WARPS];
-  int tot_gt, tot_eq;
+  int hist[EV_BINS * EV_COPIES];
+  int list[EV_LIST];
+  long long src[EV_THREADS], dst[EV_THREADS];
+  int wsum[2][EV_WARPS];
   uint32_t prefix;
   int need;
-  long long src[EV_THREADS], dst[EV_THREADS];
-  uint32_t key[EV_KEYS];
 };
 
 // Larger score, larger key; -0 equals 0, a NaN is below every number's key.
@@ -94,19 +97,68 @@ __device__ __forceinline__ uint32_t score_key(float s) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-__global__ void __launch_bounds__(EV_THREADS) k_evict(EvictArgs a, int esize) {
+// One more in a shared word, without a branch around it.
+__device__ __forceinline__ void count_if(uint32_t addr, bool yes) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "@p red.shared.add.u32 [%0], 1;\n\t}" ::"r"(addr),
+      "r"((uint32_t)yes)
+      : "memory");
+}
+
+// Exclusive sums over the warp's lanes.
+__device__ __forceinline__ int lanes_before(int v) {
+  const int lane = threadIdx.x & 31;
+  int sum = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(FULL, sum, o);
+    if (lane >= o) sum += y;
+  }
+  return sum - v;
+}
+
+__global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize, int vec, int E) {
   extern __shared__ __align__(16) char ev_raw[];
   EvSmem* s = reinterpret_cast<EvSmem*>(ev_raw);
-  cg::cluster_group cluster = cg::this_cluster();
-  const int C = (int)cluster.num_blocks(), r = (int)cluster.block_rank();
-  const int h = blockIdx.y, b = blockIdx.z;
+  const int r = blockIdx.x, S = gridDim.x, h = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t hist = (uint32_t)__cvta_generic_to_shared(s->hist);
   grid_dep_launch();
   grid_dep_wait();
-  const int n = kv_len(a.src, b);
-  const int k = min(a.keep, n);
   const long long pair = (long long)b * a.src.Hkv + h;
   const float* sc = a.scores + pair * a.score_stride;
+  // this thread's places of a chunk: E from `at` on.  A row holds cap scores, so they are
+  // on their way before the sequence's length is known
+  const int chunk = EV_THREADS * E;
+  float v[EV_EACH];
+  uint32_t key[EV_EACH];
+  int at;
+  auto fetch = [&](int c) {
+    at = c * chunk + tid * E;
+    if (vec && at + E <= a.src.cap) {
+#pragma unroll
+      for (int x = 0; x < EV_EACH; x += 4)
+        if (x < E)
+          *reinterpret_cast<float4*>(v + x) = *reinterpret_cast<const float4*>(sc + at + x);
+    } else {
+#pragma unroll
+      for (int x = 0; x < EV_EACH; ++x)
+        v[x] = x < E && at + x < a.src.cap ? sc[at + x] : 0.f;
+    }
+  };
+  fetch(0);
+  const int n = kv_len(a.src, b);
+  const int k = min(a.keep, n), tail = n - a.recent;
+  auto to_keys = [&]() {  // 0 is no key's value
+#pragma unroll
+    for (int x = 0; x < EV_EACH; ++x) {
+      const int j = at + x;
+      key[x] = x >= E || j >= n ? 0u
+               : j < a.sinks || j >= tail ? 0xffffffffu : score_key(v[x]);
+    }
+  };
   int32_t* oi = a.out_idx + pair * a.keep;
   float* os = a.out_scores ? a.out_scores + pair * a.keep : nullptr;
   if (r == 0) {
@@ -116,54 +168,52 @@ __global__ void __launch_bounds__(EV_THREADS) k_evict(EvictArgs a, int esize) {
       if (os) os[x] = 0.f;
     }
   }
-  // this CTA's places [j0, j0 + m), whole warps' worth each
-  const int share = (ceil_div(n, C) + 31) & ~31;
-  const int j0 = min(n, r * share), m = min(share, n - j0);
-  const int tail = n - a.recent;
-  auto fresh_key = [&](int x) -> uint32_t {
-    const int j = j0 + x;
-    return (j < a.sinks || j >= tail) ? 0xffffffffu : score_key(sc[j]);
-  };
-  auto key_at = [&](int x) -> uint32_t { return x < EV_KEYS ? s->key[x] : fresh_key(x); };
-  for (int x = tid; x < min(m, EV_KEYS); x += EV_THREADS) s->key[x] = fresh_key(x);
-  uint32_t thr = 0;
-  int need = 0;       // keys equal to the threshold to take; all larger ones are
+  // this CTA's part of the kept places
+  const int each = ceil_div(k, S), p0 = min(k, r * each), p1 = min(k, p0 + each);
+  if (p0 >= p1) return;
+  const int chunks = ceil_div(n, chunk);
+  to_keys();
+  uint32_t thr = 0;  // k == n: every key is larger
+  int need = 0;      // keys equal to the threshold to take; all larger ones are
   if (k < n) {
     uint32_t prefix = 0;
     need = k;
-    for (int p = 0; p < 4; ++p) {
-      int* hist = s->hist[p & 1];
-      for (int x = tid; x < 256; x += EV_THREADS) hist[x] = 0;
+    for (int p = 0; p < 3; ++p) {
+      const int sh = p == 0 ? 21 : p == 1 ? 10 : 0, bits = p == 2 ? 10 : 11;
+      for (int x = tid; x < EV_BINS * EV_COPIES / 4; x += EV_THREADS)
+        reinterpret_cast<int4*>(s->hist)[x] = make_int4(0, 0, 0, 0);
       __syncthreads();
-      const int sh = 24 - 8 * p;
-      for (int x0 = warp * 32; x0 < m; x0 += EV_THREADS) {
-        const int x = x0 + lane;
-        const uint32_t kx = x < m ? key_at(x) : 0;
-        const bool in = x < m && (p == 0 || ((kx ^ prefix) >> (sh + 8)) == 0);
-        const uint32_t d = in ? (kx >> sh) & 255u : 256u;
-        const uint32_t same = __match_any_sync(FULL, d);
-        if (in && lane == __ffs(same) - 1) atomicAdd(&hist[d], __popc(same));
-      }
-      cluster.sync();
-      int cnt = 0;
-      if (tid < 256)
-        for (int q = 0; q < C; ++q) cnt += cluster.map_shared_rank(hist, q)[tid];
-      // the digit whose keys reach the need-th from above
-      int suf = cnt;  // counts of this digit and the larger ones of its warp
-      if (tid < 256) {
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int y = __shfl_down_sync(FULL, suf, o);
-          if (lane + o < 32) suf += y;
+      for (int c = 0; c < chunks; ++c) {
+        if (chunks > 1) {
+          fetch(c);
+          to_keys();
         }
-        if (lane == 0) s->wgt[warp] = suf;
+#pragma unroll
+        for (int x = 0; x < EV_EACH; ++x) {
+          if (x >= E) break;
+          count_if(hist + (((key[x] >> sh) & ((1u << bits) - 1)) * EV_COPIES + (lane & 3)) * 4,
+                   key[x] != 0 && (p == 0 || ((key[x] ^ prefix) >> (sh + bits)) == 0));
+        }
       }
       __syncthreads();
-      if (tid < 256) {
-        for (int w = warp + 1; w < 8; ++w) suf += s->wgt[w];
-        if (suf >= need && suf - cnt < need) {
-          s->prefix = prefix | ((uint32_t)tid << sh);
-          s->need = need - (suf - cnt);
+      // bins from the largest on, two a thread: the one whose keys reach the need-th
+      int c[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int4 v = reinterpret_cast<const int4*>(s->hist)[EV_BINS - 1 - 2 * tid - y];
+        c[y] = v.x + v.y + v.z + v.w;
+      }
+      const int here = __reduce_add_sync(FULL, c[0] + c[1]);
+      if (lane == 0) s->wsum[0][warp] = here;
+      __syncthreads();
+      const int w = s->wsum[0][lane];  // EV_WARPS == 32 totals
+      int before = __shfl_sync(FULL, lanes_before(w), warp);
+      if (before < need && before + here >= need) {  // it is one of this warp's
+        before += lanes_before(c[0] + c[1]);
+        if (before < need && before + c[0] + c[1] >= need) {
+          const int y = before + c[0] >= need ? 0 : 1;
+          s->prefix = prefix | ((uint32_t)(EV_BINS - 1 - 2 * tid - y) << sh);
+          s->need = need - before - (y ? c[0] : 0);
         }
       }
       __syncthreads();
@@ -172,66 +222,58 @@ __global__ void __launch_bounds__(EV_THREADS) k_evict(EvictArgs a, int esize) {
     }
     thr = prefix;
   }
-  // what this CTA keeps: warp w counts the places of its own run of the share
-  const int run = ceil_div(ceil_div(m, 32), EV_WARPS) * 32;
-  const int x0 = min(m, warp * run), x1 = min(m, x0 + run);
-  int gt = 0, eq = 0;
-  for (int x = x0; x < x1; x += 32) {
-    const uint32_t kx = x + lane < x1 ? key_at(x + lane) : 0;
-    const bool in = x + lane < x1;
-    gt += __popc(__ballot_sync(FULL, in && (k == n || kx > thr)));
-    eq += __popc(__ballot_sync(FULL, in && k < n && kx == thr));
-  }
-  if (lane == 0) {
-    s->wgt[warp] = gt;
-    s->weq[warp] = eq;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    int g = 0, e = 0;
-    for (int w = 0; w < EV_WARPS; ++w) {
-      g += s->wgt[w];
-      e += s->weq[w];
+  // the kept places in order: larger keys and equal ones before this thread's
+  int g0 = 0, e0 = 0;
+  for (int c = 0; c < chunks; ++c) {
+    if (chunks > 1) {
+      fetch(c);
+      to_keys();
     }
-    s->tot_gt = g;
-    s->tot_eq = e;
-  }
-  cluster.sync();
-  int g0 = 0, e0 = 0;  // larger and equal keys before this CTA
-  for (int q = 0; q < r; ++q) {
-    g0 += *cluster.map_shared_rank(&s->tot_gt, q);
-    e0 += *cluster.map_shared_rank(&s->tot_eq, q);
-  }
-  const int p0 = g0 + min(e0, need);
-  const int p1 = g0 + s->tot_gt + min(e0 + s->tot_eq, need);
-  // no CTA leaves while another may read its counts; the copies need no more of them
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  for (int w = 0; w < warp; ++w) {
-    g0 += s->wgt[w];
-    e0 += s->weq[w];
-  }
-  for (int x = x0; x < x1; x += 32) {
-    const bool in = x + lane < x1;
-    const uint32_t kx = in ? key_at(x + lane) : 0;
-    const bool isg = in && (k == n || kx > thr), ise = in && k < n && kx == thr;
-    const uint32_t mg = __ballot_sync(FULL, isg), me = __ballot_sync(FULL, ise);
-    const uint32_t below = (1u << lane) - 1;
-    const int e = e0 + __popc(me & below);
-    if (isg || (ise && e < need)) {
-      const int pos = g0 + __popc(mg & below) + min(e, need);
-      oi[pos] = j0 + x + lane;
-      if (os) os[pos] = sc[j0 + x + lane];
+    int gt = 0, eq = 0;
+#pragma unroll
+    for (int x = 0; x < EV_EACH; ++x) {
+      if (x >= E) break;
+      gt += key[x] > thr;
+      eq += key[x] == thr && thr != 0;
     }
-    g0 += __popc(mg);
-    e0 += __popc(me);
+    const int both = (gt << 16) + eq;  // at most 16,384 each over the block
+    const int here = __reduce_add_sync(FULL, both);
+    int* ws = s->wsum[c & 1];
+    if (lane == 0) ws[warp] = here;
+    __syncthreads();
+    const int w = ws[lane];
+    const int before = __shfl_sync(FULL, lanes_before(w), warp) + lanes_before(both);
+    const int total = __reduce_add_sync(FULL, w);
+    int g = g0 + (before >> 16), e = e0 + (before & 0xffff);
+    if (g + min(e, need) < p1 && g + gt + min(e + eq, need) > p0) {
+#pragma unroll
+      for (int x = 0; x < EV_EACH; ++x) {
+        if (x >= E) break;
+        const bool isg = key[x] > thr, ise = key[x] == thr && thr != 0;
+        const int pos = g + min(e, need);
+        if ((isg || (ise && e < need)) && pos >= p0 && pos < p1) {
+          if (pos - p0 < EV_LIST)
+            s->list[pos - p0] = at + x;
+          else
+            oi[pos] = at + x;
+        }
+        g += isg;
+        e += ise;
+      }
+    }
+    g0 += total >> 16;
+    e0 += total & 0xffff;
   }
   __syncthreads();  // this CTA's places are written
   const int rc = a.src.d * esize / 16;
   for (int q0 = p0; q0 < p1; q0 += EV_THREADS) {
     const int nr = min(EV_THREADS, p1 - q0);
     if (tid < nr) {
-      const long long so = kv_row(a.src, b, h, oi[q0 + tid]);
-      const long long dto = kv_row(a.dst, b, h, q0 + tid);
+      const int q = q0 + tid, j = q - p0 < EV_LIST ? s->list[q - p0] : oi[q];
+      oi[q] = j;
+      if (os) os[q] = sc[j];
+      const long long so = kv_row(a.src, b, h, j);
+      const long long dto = kv_row(a.dst, b, h, q);
       s->src[tid] = so < 0 || dto < 0 ? -1 : so * esize;
       s->dst[tid] = dto * esize;
     }
@@ -240,32 +282,29 @@ __global__ void __launch_bounds__(EV_THREADS) k_evict(EvictArgs a, int esize) {
     constexpr int U = 4;
     for (int x = tid; x < total; x += EV_THREADS * U) {
       int4 kv[U], vv[U];
+      long long at[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int y = x + u * EV_THREADS;
+        at[u] = -1;
         if (y < total) {
           const int row = y / rc, z = (y - row * rc) * 16;
           if (s->src[row] >= 0) {
+            at[u] = s->dst[row] + z;
             kv[u] = *(const int4*)(a.src.k + s->src[row] + z);
             vv[u] = *(const int4*)(a.src.v + s->src[row] + z);
           }
         }
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int y = x + u * EV_THREADS;
-        if (y < total) {
-          const int row = y / rc, z = (y - row * rc) * 16;
-          if (s->src[row] >= 0) {
-            *(int4*)(a.dst.k + s->dst[row] + z) = kv[u];
-            *(int4*)(a.dst.v + s->dst[row] + z) = vv[u];
-          }
+      for (int u = 0; u < U; ++u)
+        if (at[u] >= 0) {
+          *(int4*)(a.dst.k + at[u]) = kv[u];
+          *(int4*)(a.dst.v + at[u]) = vv[u];
         }
-      }
     }
     __syncthreads();
   }
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 }  // namespace
 
@@ -290,17 +329,18 @@ cudaError_t launch_cache_append(const KV& c, int dtype, const void* k_new, const
 
 cudaError_t launch_evict(const EvictArgs& a, int dtype, cudaStream_t st) {
   const int esize = dtype == GMC_BF16 ? 2 : 4;
-  // CTAs of a cluster: as many as fill the GPU, a few hundred places each at least
-  int C = 1;
-  while (C < 16 && (long long)a.src.B * a.src.Hkv * C < 152 && a.src.cap > 256 * C) C *= 2;
-  cudaError_t e = set_smem_limit((const void*)k_evict, sizeof(EvSmem));
+  // CTAs of a pair: as many as fill the GPU, 32 kept rows each at least
+  const long long pairs = (long long)a.src.B * a.src.Hkv;
+  const int S = (int)std::max<long long>(
+      1, std::min<long long>(sm_count() / pairs, ceil_div(a.keep, 32)));
+  const cudaError_t e = set_smem_limit((const void*)k_evict, sizeof(EvSmem));
   if (e != cudaSuccess) return e;
-  if (C > 8) {
-    e = cudaFuncSetAttribute(k_evict, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return e;
-  }
-  return launch_k(k_evict, dim3(C, a.src.Hkv, a.src.B), dim3(EV_THREADS), sizeof(EvSmem), st, C, a,
-                  esize);
+  const int vec = (uintptr_t)a.scores % 16 == 0 && a.score_stride % 4 == 0;
+  // keys of a thread: as few as hold the longest sequence, whole vectors from four on
+  int E = std::min(EV_EACH, ceil_div(a.src.cap, EV_THREADS));
+  if (E >= 4) E = ceil_div(E, 4) * 4;
+  return launch_k(k_evict, dim3(S, a.src.Hkv, a.src.B), dim3(EV_THREADS), sizeof(EvSmem), st, 1, a,
+                  esize, (int)(vec && E >= 4), E);
 }
 
 }  // namespace gmc
