@@ -582,8 +582,11 @@ int gmc_cache_append(const gmc_kv_cache* cache, const void* k_new, const void* v
  * appended) over its cached keys, whole or through a window with sinks.
  *   q        [rows][H][d] (strides in attn), sequence after sequence as q_offsets says
  *   out      as q;  lse  fp32 [rows][H] or NULL
- * q_offsets, rows, T: as offsets, rows, T of gmc_cache_append.  q and out
- * 16-byte aligned, their strides multiples of 16 bytes.
+ * q_offsets, rows, T: as offsets, rows, T of gmc_cache_append; rows of no
+ * sequence are left alone.  q and out 16-byte aligned, their strides multiples
+ * of 16 bytes.  bf16 caches with d <= 128 and pages of a multiple of 8 slots run
+ * on the tcgen05 tensor cores, others on the CUDA cores.  One launch, or two
+ * where the key axis is split.
  */
 size_t gmc_attend_workspace_size(const gmc_kv_cache* cache, int H, int T);
 int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
@@ -594,14 +597,16 @@ int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
  * gmc_decode -- one new token a sequence: its attention over the cached keys,
  * the key at place lens[b] - 1 being its own.
  *   q           [B][H][d] (strides in attn);  out as q;  lse fp32 [B][H] or NULL
- *   k_new,v_new [B][Hkv][d]: appended at place lens[b] - 1 in the same launch
- *               (and read from here); both NULL: the cache holds them already
+ *   k_new,v_new [B][Hkv][d]: appended at place lens[b] - 1 by the same call (and
+ *               read from here); both NULL: the cache holds them already
  *   scores      fp32 [B][Hkv][score_stride] or NULL: what every key has gathered so far
  *   out_scores  out_scores[b][g][j] = scores[b][g][j] + the weight that key j
  *               received, summed over the H / Hkv query heads of key head g, for
  *               j < lens[b] (later entries are left alone); unseen keys receive
  *               nothing, and a key appended by this call starts from 0.  May be
  *               `scores` itself; both or neither are NULL.
+ * Two launches (for every 16 query heads of a key head with bf16, 8 with fp32).
+ * A page's rows must lie within 64 GB (GMC_ERR_UNSUPPORTED).
  */
 size_t gmc_decode_workspace_size(const gmc_kv_cache* cache, int H);
 int gmc_decode(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q, const void* k_new,
@@ -619,7 +624,8 @@ int gmc_decode(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q, c
  *   out_idx     int32 [B][Hkv][keep]: the places kept, -1 after the last
  *   out_scores  fp32 [B][Hkv][keep]: their scores, 0 after the last; may be NULL
  * src and dst: the same B, Hkv, d and dtype; sinks + recent <= keep; dst must
- * have room for `keep` tokens a sequence (GMC_ERR_ARG).  One launch.
+ * have room for `keep` tokens a sequence (GMC_ERR_ARG).  One launch; the
+ * workspace is not used yet.
  */
 size_t gmc_evict_workspace_size(const gmc_kv_cache* src, int keep);
 int gmc_evict(const gmc_kv_cache* src, const gmc_kv_cache* dst, const float* scores,

@@ -135,11 +135,15 @@ struct AttnArgs {
   long long q_row, q_head, o_row, o_head;  // elements
   int H, G, window, sinks, rows, T;
   float scale2;  // scale * log2(e): softmax in powers of two
-  // a long key axis split over CTAs: partial sums [split][row][H][d], maxima and sums
+  // a long key axis split over CTAs: partial sums [split][B][T][H][d], maxima and sums
   int splits;
   float* part;
-  float2* ml;  // [split][row][H]
+  float2* ml;  // [split][B][T][H]
 };
+// Row of a split's part of new token t of sequence b.
+__device__ __forceinline__ long long part_row(const AttnArgs& a, int split, int b, int t) {
+  return ((long long)split * a.c.B + b) * a.T + t;
+}
 
 cudaError_t launch_cache_append(const KV&, int dtype, const void* k_new, const void* v_new,
                                 const int32_t* offsets, int rows, int T, cudaStream_t);

@@ -174,6 +174,9 @@ int gmc_decode(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q, c
     return GMC_ERR_ARG;
   DecodeArgs a{};
   a.c = view(cache);
+  // offsets inside a page are kept as 32-bit numbers of 16 bytes
+  const long long page = a.c.head_stride / 8 * (a.c.Hkv - 1) + a.c.slot_stride / 8 * (a.c.ps - 1);
+  if (page * esize_of(cache->dtype) / 2 > 0xffff0000LL) return GMC_ERR_UNSUPPORTED;
   if (scores && score_stride < a.c.cap) return GMC_ERR_ARG;
   if (ws_bytes < decode_workspace(a.c, cache->dtype, attn->H)) return GMC_ERR_WORKSPACE;
   a.q = (const char*)q;

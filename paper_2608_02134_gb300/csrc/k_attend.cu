@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(at_threads<DP>(), DP > 128 ? 1 : 2) k_attend_s
     const long long row = nr.off + t0 + t;
     const int hq = h * a.G + g;
     if (a.splits > 1) {
-      const long long pr = ((long long)split * a.rows + row) * a.H + hq;
+      const long long pr = part_row(a, split, b, t0 + t) * a.H + hq;
       if (tx == 0) a.ml[pr] = make_float2(m[i], L);
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
@@ -277,24 +277,29 @@ __global__ void __launch_bounds__(at_threads<DP>(), DP > 128 ? 1 : 2) k_attend_s
   }
 }
 
-// One warp a (row, query head): out = sum_s w_s part_s / sum_s w_s l_s, w_s = 2^(m_s - max m).
+// One warp a (new token, query head): out = sum_s w_s part_s / sum_s w_s l_s,
+// w_s = 2^(m_s - max m).
 template <typename T>
 __global__ void __launch_bounds__(256) k_attend_join(AttnArgs a) {
   grid_dep_launch();
   grid_dep_wait();
   const int lane = threadIdx.x & 31;
+  const long long step = part_row(a, 1, 0, 0) * a.H;
   const long long x = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (x >= (long long)a.rows * a.H) return;
-  const long long row = x / a.H;
-  const int hq = (int)(x - row * a.H);
-  const long long step = (long long)a.rows * a.H;
+  if (x >= step) return;
+  const long long token = x / a.H;
+  const int hq = (int)(x - token * a.H), b = (int)(token / a.T), t = (int)(token - (long long)b * a.T);
+  const NewRows nr = new_rows(a.q_offsets, b, a.rows, a.T, a.c.status);
+  if (t >= nr.T) return;
+  const long long row = nr.off + t;
   float2 ml = make_float2(-INFINITY, 0.f);
   if (lane < a.splits) ml = a.ml[lane * step + x];
   const float M = warp_max(ml.x), base = M == -INFINITY ? 0.f : M;
   const float w = exp2_fast(ml.x - base);
   const float L = warp_sum(ml.y * w);
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  if (a.lse && lane == 0) a.lse[x] = L == 0.f ? -INFINITY : (base + log2f(L)) * LN2;
+  if (a.lse && lane == 0)
+    a.lse[row * a.H + hq] = L == 0.f ? -INFINITY : (base + log2f(L)) * LN2;
   T* out = reinterpret_cast<T*>(a.out) + row * a.o_row + hq * a.o_head;
   for (int y0 = 0; y0 < a.c.d; y0 += 128) {
     const int y = y0 + lane * 4;
@@ -339,7 +344,7 @@ size_t attend_workspace(const KV& c, int dtype, int H, int T) {
 }
 
 cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t st) {
-  const unsigned grid = (unsigned)(((long long)a.rows * a.H + 7) / 8);
+  const unsigned grid = (unsigned)(((long long)a.c.B * a.T * a.H + 7) / 8);
   return dtype == GMC_BF16
              ? launch_k(k_attend_join<__nv_bfloat16>, dim3(grid), dim3(256), 0, st, 1, a)
              : launch_k(k_attend_join<float>, dim3(grid), dim3(256), 0, st, 1, a);

@@ -667,7 +667,7 @@ __global__ void __launch_bounds__(t_threads<TILES>(), 3 - TILES)
       const int hq = h * a.G + g;
       const long long row = nr.off + t0 + t * tpt + tok;
       if (a.splits > 1) {
-        const long long pr = ((long long)split * a.rows + row) * a.H + hq;
+        const long long pr = part_row(a, split, b, t0 + t * tpt + tok) * a.H + hq;
         if (valid) a.ml[pr] = ok ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
         if (ok && turns > 0)
 #pragma unroll 1
@@ -743,7 +743,7 @@ __global__ void __launch_bounds__(t_threads<TILES>(), 3 - TILES)
       }
       const int y = lane * 4;
       if (a.splits > 1) {
-        const long long pr = ((long long)split * a.rows + row) * a.H + hq;
+        const long long pr = part_row(a, split, b, t0 + tk) * a.H + hq;
         if (lane == 0) a.ml[pr] = make_float2(m, l);
         if (y < a.c.d)
           *reinterpret_cast<float4*>(a.part + pr * a.c.d + y) = make_float4(o[0], o[1], o[2], o[3]);

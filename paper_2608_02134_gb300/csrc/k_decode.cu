@@ -828,7 +828,8 @@ cudaError_t decode_launch(DecodeArgs a, cudaStream_t st) {
   if (a.scores) {
     long long most = a.c.cap;
     if (a.window > 0) most = std::min(most, (long long)a.window + a.sinks);
-    blocks = (int)std::min<long long>((most + JN_PLACES - 1) / JN_PLACES, 1024);
+    blocks = (int)std::min<long long>({(most + JN_PLACES - 1) / JN_PLACES, 1024,
+                                       std::max(1, 0x3fffffff / pairs)});
   }
   return launch_k(k_decode_join<typename H::T>, dim3(out_blocks + pairs * blocks),
                   dim3(JN_THREADS), 0, st, 1, a, W, DP, out_blocks, std::max(blocks, 1));
@@ -856,9 +857,8 @@ cudaError_t launch_decode(DecodeArgs a, int dtype, void* ws, cudaStream_t st, in
   const long long esize = dtype == GMC_BF16 ? 2 : 4;
   const long long page16 = a.c.page_stride * esize / 16, head16 = a.c.head_stride * esize / 16,
                   slot16 = a.c.slot_stride * esize / 16;
-  // pieces of 16 bytes from the pools' start: inside a page always below 2^32 here, over
-  // the pool in all but the largest (page16 = 0: 64-bit offsets)
-  if (head16 * (a.c.Hkv - 1) + slot16 * (a.c.ps - 1) > 0xffff0000LL) return cudaErrorNotSupported;
+  // pieces of 16 bytes from the pools' start: inside a page below 2^32 (gmc_decode checks
+  // it), over the pool in all but the largest (page16 = 0: 64-bit offsets)
   a.head16 = (unsigned)head16;
   a.slot16 = (unsigned)slot16;
   a.page16 = page16 * (a.c.num_pages - 1) + head16 * (a.c.Hkv - 1) + slot16 * a.c.ps + 64 <=

@@ -512,7 +512,8 @@ class KVCache:
         """gmc_attn of these queries and outputs, and their head count."""
         shape = q.shape
         if len(shape) != 3 or shape != out.shape or q.dtype != self.dtype \
-                or out.dtype != self.dtype or shape[2] != self.d:
+                or out.dtype != self.dtype or shape[2] != self.d or not q.is_cuda \
+                or not out.is_cuda:
             raise GMCError("queries and outputs: [rows, H, d] of the cache's type")
         H = shape[1]
         if q.is_contiguous() and out.is_contiguous():
@@ -538,11 +539,11 @@ class KVCache:
         return torch._C._cuda_getCurrentRawStream(self.device_index)
 
     def workspace(self, nbytes, stream):
-        """A workspace for one call on `stream`."""
-        w = alloc_workspace(nbytes, self.k.device)
-        if stream is not None:
-            w.record_stream(stream)
-        return w
+        """A workspace for one call on `stream`, from that stream's memory."""
+        if stream is None:
+            return alloc_workspace(nbytes, self.k.device)
+        with torch.cuda.stream(stream):
+            return alloc_workspace(nbytes, self.k.device)
 
 
 def _addr(t):
@@ -550,20 +551,22 @@ def _addr(t):
 
 
 def _check_int32(t, n, what):
-    if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n):
+    if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n
+                          or not t.is_cuda):
         raise GMCError(what)
 
 
 def _check_f32(t, n, what):
-    if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n):
+    if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n
+                          or not t.is_cuda):
         raise GMCError(what)
 
 
 def _check_scores(cache, t):
     shape = t.shape
     if t.dtype != torch.float32 or len(shape) != 3 or shape[0] != cache.B \
-            or shape[1] != cache.Hkv or not t.is_contiguous():
-        raise GMCError("scores: dense fp32 [B, Hkv, places]")
+            or shape[1] != cache.Hkv or not t.is_contiguous() or not t.is_cuda:
+        raise GMCError("scores: dense fp32 [B, Hkv, places] on the device")
     return shape
 
 
@@ -573,10 +576,11 @@ def cache_append(cache: KVCache, k_new, v_new, T, offsets=None, stream=None):
     gmc_compress's out_kv, [2 * rows, Hkv, d]."""
     shape = k_new.shape
     rows = shape[0] if v_new is not None else shape[0] // 2
-    if shape[1:] != cache._row_shape or k_new.dtype != cache.dtype or not k_new.is_contiguous():
+    if shape[1:] != cache._row_shape or k_new.dtype != cache.dtype \
+            or not k_new.is_contiguous() or not k_new.is_cuda:
         raise GMCError("new rows: dense [rows, Hkv, d] of the cache's type")
     if v_new is not None and (v_new.shape != shape or v_new.dtype != cache.dtype
-                              or not v_new.is_contiguous()):
+                              or not v_new.is_contiguous() or not v_new.is_cuda):
         raise GMCError("new rows: as many values as keys")
     _check_int32(offsets, cache.B + 1, "offsets: dense int32 [B + 1]")
     rc = lib().gmc_cache_append(cache.ref, k_new.data_ptr(), _addr(v_new), _addr(offsets), rows, T,
@@ -622,7 +626,7 @@ def decode(cache: KVCache, q, out, k_new=None, v_new=None, window=0, sinks=0, sc
         raise GMCError("decode: one query row a sequence")
     for t in (k_new, v_new):
         if t is not None and (t.shape != cache._new_shape or t.dtype != cache.dtype
-                              or not t.is_contiguous()):
+                              or not t.is_contiguous() or not t.is_cuda):
             raise GMCError("new rows: dense [B, Hkv, d] of the cache's type")
     _check_f32(lse, cache.B * H, "lse: dense fp32 [B, H]")
     places = 0
