@@ -554,6 +554,10 @@ __device__ __forceinline__ void write_lse(const DecodeArgs& a, int b, int h, int
     a.lse[(long long)b * a.H + h * a.G + a.h0 + g] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
 }
 
+__device__ __forceinline__ void fetch_l1(const void* p) {
+  asm volatile("prefetch.global.L1 [%0];" ::"l"(p));
+}
+
 // out_scores of a pair's places x0, x0 + step, .. from its logits and final maxima and sums.
 __device__ __forceinline__ void add_scores(const DecodeArgs& a, const Walk& w, const float2* ml,
                                            int x0, int step) {
@@ -741,32 +745,43 @@ __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W,
     }
     const Parts p(row, W, u, w.turns, pair);
     if (p.whole) return;
-    const float2 v = join_ml(a, p, g, lane);
-    const float inv = final_ml(v.x, v.y).y;
     for (int y = lane * 4; y < dp; y += 128) {
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      float M = -INFINITY, L = 0.f;
       for (int q0 = 0; q0 < p.count; q0 += 8) {  // eight parts' loads in flight
         float4 z[8];
-        float f[8];
+        float2 v[8];
+        float top = M;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
           const long long at = p.place(min(q0 + q, p.count - 1)) * a.heads + g;
           z[q] = *reinterpret_cast<const float4*>(a.part + at * dp + y);
-          f[q] = q0 + q < p.count ? a.ml[at].x : -INFINITY;
+          v[q] = a.ml[at];
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          const float x = exp2_fast(f[q] - v.x);
-          if (x == 0.f) continue;
+          if (q0 + q >= p.count) v[q] = make_float2(-INFINITY, 0.f);
+          top = fmaxf(top, v[q].x);
+        }
+        const float base = top == -INFINITY ? 0.f : top, old = exp2_fast(M - base);
+        M = top;
+        L *= old;
+        o = make_float4(o.x * old, o.y * old, o.z * old, o.w * old);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const float x = exp2_fast(v[q].x - base);
+          L = fmaf(v[q].y, x, L);
+          if (q0 + q >= p.count) continue;
           o.x = fmaf(z[q].x, x, o.x);
           o.y = fmaf(z[q].y, x, o.y);
           o.z = fmaf(z[q].z, x, o.z);
           o.w = fmaf(z[q].w, x, o.w);
         }
       }
-      write_head<T>(a, b, w.h, g, y, o, inv);
+      if (M == -INFINITY) M = 0.f;
+      write_head<T>(a, b, w.h, g, y, o, final_ml(M, L).y);
+      if (y == 0) write_lse(a, b, w.h, g, M, L);
     }
-    if (lane == 0) write_lse(a, b, w.h, g, v.x, v.y);
     return;
   }
   const int x = blockIdx.x - out_blocks, pair = x / blocks, b = pair / a.c.Hkv;
@@ -774,6 +789,14 @@ __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W,
   const int u = row.first(a, b, &w) + w.h * w.turns;
   const int x0 = (x - pair * blocks) * JN_THREADS;
   if (w.turns == 0) return;
+  // this thread's logits and scores on their way while the sums are joined
+#pragma unroll
+  for (int i = 0; i < JN_PLACES / JN_THREADS; ++i) {
+    const int y = x0 + (int)threadIdx.x + i * blocks * JN_THREADS;
+    if (y >= w.nv) break;
+    fetch_l1(a.logits + ((long long)pair * a.places + y) * a.hs);
+    fetch_l1(a.scores + (long long)pair * a.score_stride + w.seen.place(y));
+  }
   const Parts p(row, W, u, w.turns, pair);
   for (int g = warp; g < a.heads; g += JN_WARPS) {
     const float2 v = join_ml(a, p, g, lane);
