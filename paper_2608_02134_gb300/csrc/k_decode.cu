@@ -395,7 +395,8 @@ template <int DP, int HM_> struct HeadsF32 {
   static constexpr int ROWB = DP * 4, P = DP / 4;
   static constexpr int NC = P >= 32 ? P / 32 : 1;  // output pieces of a lane
   static constexpr int KS = P >= 32 ? 1 : 32 / P;  // lanes that share a piece, alternate keys
-  float o[HM][NC * 4], m[HM], l[HM];
+  f32x2 o[HM][NC * 2];  // columns in pairs
+  float m[HM], l[HM];
   __device__ __forceinline__ void begin(const DecodeArgs& a, const Walk& w, char* extra,
                                         int lane) {
     float* qw = reinterpret_cast<float*>(extra);
@@ -410,7 +411,7 @@ template <int DP, int HM_> struct HeadsF32 {
       m[g] = -INFINITY;
       l[g] = 0.f;
 #pragma unroll
-      for (int x = 0; x < NC * 4; ++x) o[g][x] = 0.f;
+      for (int x = 0; x < NC * 2; ++x) o[g][x] = 0ull;
     }
     __syncwarp();
   }
@@ -421,16 +422,25 @@ template <int DP, int HM_> struct HeadsF32 {
     const char* vb = kb + DT * ROWB;
     const int key = lane & 15, half = lane >> 4;
     float s[HM];
+    {
+      f32x2 z[HM];  // sums over even and odd columns
 #pragma unroll
-    for (int g = 0; g < HM; ++g) s[g] = 0.f;
+      for (int g = 0; g < HM; ++g) z[g] = 0ull;
 #pragma unroll 4
-    for (int c = 0; c < P / 2; ++c) {
-      const int pc = half * (P / 2) + c;
-      const float4 kv = *reinterpret_cast<const float4*>(kb + key * ROWB + ((pc ^ (key & 7)) * 16));
+      for (int c = 0; c < P / 2; ++c) {
+        const int pc = half * (P / 2) + c;
+        const ulonglong2 kv =
+            *reinterpret_cast<const ulonglong2*>(kb + key * ROWB + ((pc ^ (key & 7)) * 16));
+#pragma unroll
+        for (int g = 0; g < HM; ++g) {
+          const ulonglong2 qv = *reinterpret_cast<const ulonglong2*>(qw + g * DP + pc * 4);
+          z[g] = fma2(qv.y, kv.y, fma2(qv.x, kv.x, z[g]));
+        }
+      }
 #pragma unroll
       for (int g = 0; g < HM; ++g) {
-        const float4 qv = *reinterpret_cast<const float4*>(qw + g * DP + pc * 4);
-        s[g] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, s[g]))));
+        const float2 v = unpair(z[g]);
+        s[g] = v.x + v.y;
       }
     }
     const bool in = w.t * DT + key < w.nv;
@@ -447,7 +457,7 @@ template <int DP, int HM_> struct HeadsF32 {
         const float x = exp2_fast(m[g] - base);
         l[g] *= x;
 #pragma unroll
-        for (int y = 0; y < NC * 4; ++y) o[g][y] *= x;
+        for (int y = 0; y < NC * 2; ++y) o[g][y] = mul2(o[g][y], pair(x, x));
         m[g] = mn;
       }
       const float p = exp2_fast(s[g] - base);
@@ -458,17 +468,25 @@ template <int DP, int HM_> struct HeadsF32 {
     const int piece = P >= 32 ? lane : lane % P, sub = P >= 32 ? 0 : lane / P;
 #pragma unroll 4
     for (int k = sub; k < DT; k += KS) {
+      float p[HM];
+      if constexpr (HM % 4 == 0) {
+#pragma unroll
+        for (int g = 0; g < HM; g += 4)
+          *reinterpret_cast<float4*>(p + g) = *reinterpret_cast<const float4*>(pw + k * HM + g);
+      } else {
+#pragma unroll
+        for (int g = 0; g < HM; ++g) p[g] = pw[k * HM + g];
+      }
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const int pc = piece + c * 32;
-        const float4 vv = *reinterpret_cast<const float4*>(vb + k * ROWB + ((pc ^ (k & 7)) * 16));
+        const ulonglong2 vv =
+            *reinterpret_cast<const ulonglong2*>(vb + k * ROWB + ((pc ^ (k & 7)) * 16));
 #pragma unroll
         for (int g = 0; g < HM; ++g) {
-          const float p = pw[k * HM + g];
-          o[g][4 * c + 0] = fmaf(p, vv.x, o[g][4 * c + 0]);
-          o[g][4 * c + 1] = fmaf(p, vv.y, o[g][4 * c + 1]);
-          o[g][4 * c + 2] = fmaf(p, vv.z, o[g][4 * c + 2]);
-          o[g][4 * c + 3] = fmaf(p, vv.w, o[g][4 * c + 3]);
+          const f32x2 pp = pair(p[g], p[g]);
+          o[g][2 * c] = fma2(pp, vv.x, o[g][2 * c]);
+          o[g][2 * c + 1] = fma2(pp, vv.y, o[g][2 * c + 1]);
         }
       }
     }
@@ -481,15 +499,18 @@ template <int DP, int HM_> struct HeadsF32 {
 #pragma unroll
         for (int x = P; x < 32; x <<= 1)
 #pragma unroll
-          for (int y = 0; y < NC * 4; ++y) o[g][y] += __shfl_xor_sync(FULL, o[g][y], x);
+          for (int y = 0; y < NC * 2; ++y)
+            o[g][y] = add2(o[g][y], __shfl_xor_sync(FULL, o[g][y], x));
       }
       if (g < a.heads) {
         if (lane == 0) ml[g] = make_float2(m[g], L);
         if (P >= 32 || lane < P)
 #pragma unroll
-          for (int c = 0; c < NC; ++c)
+          for (int c = 0; c < NC; ++c) {
+            const float2 lo = unpair(o[g][2 * c]), hi = unpair(o[g][2 * c + 1]);
             *reinterpret_cast<float4*>(out + g * DP + (lane + c * 32) * 4) =
-                make_float4(o[g][4 * c], o[g][4 * c + 1], o[g][4 * c + 2], o[g][4 * c + 3]);
+                make_float4(lo.x, lo.y, hi.x, hi.y);
+          }
       }
     }
   }
