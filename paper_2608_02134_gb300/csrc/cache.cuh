@@ -154,6 +154,9 @@ void* tensor_map_encoder();  // cuTensorMapEncodeTiled, or NULL
 bool attend_tc_takes(const KV&, int dtype, int G);
 int attend_tc_splits(const KV&, int G, int T);
 cudaError_t launch_attend_tc(const AttnArgs&, cudaStream_t);
+bool attend_f32_takes(const KV&, int dtype);
+int attend_f32_splits(const KV&, int G, int T);
+cudaError_t launch_attend_f32(const AttnArgs&, cudaStream_t);
 cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t);
 cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t, int* launches);
 

@@ -1,14 +1,15 @@
-// Causal attention of new tokens over a paged key-value cache on the CUDA cores: fp32
-// caches, and bf16 ones whose shape the tensor-core kernel does not take.
+// Causal attention of new tokens over a paged key-value cache on the CUDA cores: head
+// sizes above 128, and bf16 caches whose pages are not a multiple of 8 slots.
 //
-// A CTA takes R rows, the query heads of one key head of some consecutive tokens (so
+// A CTA takes 64 rows, the query heads of one key head of some consecutive tokens (so
 // each key is read once for all of them), and walks the seen keys 64 at a time with a
-// running maximum and sum for every row.  A thread holds 8 (4 at d > 128) rows x 4
-// keys of the logits and 8 x 8 of the output in registers; queries, keys, values and
-// weights are fp32 in shared memory, read four at a time: 12 loads of 16 bytes per 128
-// multiply-adds, 16 per 256, which is what bounds it.  The keys' copies run behind the
-// products with the values and the values' behind the logits.  Where the rows are too
-// few to fill the GPU the keys are split over CTAs and a second kernel joins them.
+// running maximum and sum for every row.  A thread holds 8 (4 at d > 128) rows x 4 keys
+// of the logits and 8 x 8 (4 x 16) of the output in registers; queries, keys, values and
+// weights are fp32 in shared memory, read four at a time.  Two multiply-adds go into an
+// instruction; two CTAs an SM (one at d > 128) wait for each other's loads.  The keys'
+// copies run behind the products with the values and the values' behind the logits.
+// Where the rows are too few to fill the GPU the keys are split over CTAs and a second
+// kernel joins them.
 #include <algorithm>
 
 #include "cache.cuh"
@@ -333,11 +334,16 @@ int simt_splits(const KV& c, int G, int T) {
   return (int)std::max<long long>(
       1, std::min<long long>({fill / ctas, AT_MAX_SPLITS, ceil_div(c.cap, 4 * AT_K)}));
 }
+int attend_splits(const KV& c, int dtype, int G, int T) {
+  return attend_tc_takes(c, dtype, G) ? attend_tc_splits(c, G, T)
+         : attend_f32_takes(c, dtype) ? attend_f32_splits(c, G, T)
+                                      : simt_splits(c, G, T);
+}
 }  // namespace
 
 size_t attend_workspace(const KV& c, int dtype, int H, int T) {
   const int G = H / c.Hkv;
-  const int s = attend_tc_takes(c, dtype, G) ? attend_tc_splits(c, G, T) : simt_splits(c, G, T);
+  const int s = attend_splits(c, dtype, G, T);
   if (s == 1) return 256;
   const size_t rows = (size_t)c.B * T * H * s;
   return 256 + ((rows * 8 + 255) & ~(size_t)255) + rows * c.d * 4;
@@ -353,8 +359,7 @@ cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t st) {
 cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t st, int* launches) {
   const int R = AT_ROWS, gsub = std::min(a.G, R), ng = ceil_div(a.G, gsub);
   const int ntile = ceil_div(a.T, R / gsub);
-  const bool tensor = attend_tc_takes(a.c, dtype, a.G);
-  a.splits = tensor ? attend_tc_splits(a.c, a.G, a.T) : simt_splits(a.c, a.G, a.T);
+  a.splits = attend_splits(a.c, dtype, a.G, a.T);
   if (a.splits > 1) {
     const size_t rows = (size_t)a.c.B * a.T * a.H * a.splits;
     a.ml = reinterpret_cast<float2*>(ws);
@@ -367,14 +372,15 @@ cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t st, int*
        ? e                                                                                \
        : launch_k(k_attend_simt<T, DP>, grid, dim3(at_threads<DP>()), at_smem<DP>(), st, 1, a,  \
                   gsub, ntile))
-  if (tensor)
+  if (attend_tc_takes(a.c, dtype, a.G))
     e = launch_attend_tc(a, st);
+  else if (attend_f32_takes(a.c, dtype))
+    e = launch_attend_f32(a, st);
   else if (dtype == GMC_BF16)
     e = a.c.d <= 64 ? GMC_AT(__nv_bfloat16, 64)
                     : a.c.d <= 128 ? GMC_AT(__nv_bfloat16, 128) : GMC_AT(__nv_bfloat16, 256);
   else
-    e = a.c.d <= 64 ? GMC_AT(float, 64)
-                    : a.c.d <= 128 ? GMC_AT(float, 128) : GMC_AT(float, 256);
+    e = GMC_AT(float, 256);
 #undef GMC_AT
   if (e != cudaSuccess) return e;
   ++*launches;
