@@ -305,10 +305,12 @@ __global__ void __launch_bounds__(256) k_attend_join(AttnArgs a) {
   for (int y0 = 0; y0 < a.c.d; y0 += 128) {
     const int y = y0 + lane * 4;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float* part = a.part + x * a.c.d + min(y, a.c.d - 4);
+#pragma unroll 4
     for (int q = 0; q < a.splits; ++q) {
+      float4 v = *reinterpret_cast<const float4*>(part + q * step * a.c.d);
       const float mq = __shfl_sync(FULL, ml.x, q), f = __shfl_sync(FULL, w, q);
-      if (mq == -INFINITY || y >= a.c.d) continue;  // a part without keys wrote no row
-      const float4 v = *reinterpret_cast<const float4*>(a.part + (q * step + x) * a.c.d + y);
+      if (mq == -INFINITY) v = make_float4(0.f, 0.f, 0.f, 0.f);  // without keys: wrote no row
       s.x += f * v.x;
       s.y += f * v.y;
       s.z += f * v.z;

@@ -19,11 +19,16 @@
 // for the maximum.  The maximum that weights are taken against follows the running one
 // only when it has grown by 2^8.
 //
-// Measured: 608 tokens of 32 heads 38 us, 1,000 tokens of 28 heads (4 key heads) 52 us,
-// 138 TFLOP/s of fp32 products, where fp32 multiply-adds on the CUDA cores took 170 and
-// 308 (their peak is 78 TFLOP/s).  Relative error (2-norm, against 64 bits) 5e-7, theirs
-// was 9e-7.  Bound by shared memory: of a turn's 3,900 clocks the products read 380 KB
-// through its port and the cutting writes 96 KB.
+// The queries' parts lie in tensor memory, so a product reads 2 KB of shared memory for its
+// keys alone, not 6 (which took the port's whole rate).
+//
+// Measured: 608 tokens of 32 heads 37 us, 1,000 tokens of 28 heads (4 key heads) 50 us,
+// 144 TFLOP/s of fp32 products, where fp32 multiply-adds on the CUDA cores took 170 and
+// 308 (their peak is 74 TFLOP/s).  Relative error (2-norm, against 64 bits) 5e-7, theirs
+// was 9e-7; with the output added up in tensor memory over two turns 8e-7, over four
+// 15e-7.  A turn takes 5,000 clocks; the tensor cores work for 3,100 of them, and the six
+// warps that load and cut are its longest chain (some 800 instructions, half of them
+// integer ones at half rate).
 //
 // Keys that a row does not see get the weight 0.  Slots outside the seen ranges are not
 // read; where a key or value is not finite (its parts would be NaN, and 0 x NaN would
@@ -47,7 +52,7 @@ constexpr int F_THREADS = (F_ISSUE + 1) * 32;
 constexpr int F_STAGE = 96;   // columns of a turn in tensor memory: 64 logits, then 3 x 32 of weights
 
 struct FCtl {
-  uint64_t qfull, kfull, kempty, vfull, vempty, sfull[2], pfull[2], ofull[2], drained;
+  uint64_t qfull, kfull[2], kempty[2], vfull[2], vempty[2], sfull[2], pfull[2], ofull, drained;
   float top[2][2][TM], sum[2][TM];
   uint32_t tmem;
   volatile int abort;
@@ -56,7 +61,7 @@ struct FCtl {
 
 // One CTA an SM (a second one would wait for tensor memory).
 template <int DP> constexpr size_t f_smem() {
-  const size_t need = 1024 + 3 * (size_t)(TM + 2 * FK) * DP * 2 + sizeof(FCtl);
+  const size_t need = 1024 + 12 * (size_t)FK * DP * 2 + sizeof(FCtl);
   return need > 120 * 1024 ? need : 120 * 1024;
 }
 
@@ -70,9 +75,11 @@ __device__ __forceinline__ float upper(float x) {
 // Two floats as three pairs of bf16.
 __device__ __forceinline__ void cut2(float x, float y, uint32_t* p0, uint32_t* p1, uint32_t* p2) {
   *p0 = uppers(x, y);
-  const float x1 = x - upper(x), y1 = y - upper(y);
-  *p1 = uppers(x1, y1);
-  *p2 = uppers(x1 - upper(x1), y1 - upper(y1));
+  const f32x2 minus = pair(-1.f, -1.f), one = fma2(pair(upper(x), upper(y)), minus, pair(x, y));
+  const float2 v = unpair(one);
+  *p1 = uppers(v.x, v.y);
+  const float2 w = unpair(fma2(pair(upper(v.x), upper(v.y)), minus, one));
+  *p2 = uppers(w.x, w.y);
 }
 // Eight floats into 16 bytes each of three tiles `step` bytes apart.
 __device__ __forceinline__ void cut8(char* dst, int step, const float4& a, const float4& b) {
@@ -87,14 +94,11 @@ __device__ __forceinline__ void cut8(char* dst, int step, const float4& a, const
 __device__ __forceinline__ void fence_async() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
-// 16 columns of 32 bits, without the wait.
-__device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const uint32_t* r) {
+// 8 columns of 32 bits, without the wait.
+__device__ __forceinline__ void tmem_st8_async(uint32_t taddr, const uint32_t* r) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
-      "r"(r[15])
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
       : "memory");
 }
 // The two warps of a lane quarter meet.
@@ -104,25 +108,26 @@ __device__ __forceinline__ void meet(int quarter) {
 
 template <int DP>
 __global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_g) {
-  constexpr int QT = TM * DP * 2, KT = FK * DP * 2, C = DP / 8;
+  constexpr int KT = FK * DP * 2, C = DP / 8;
+  // tensor memory: the queries' three parts, two turns of logits and weights, one of output
+  constexpr int QC = DP / 2, STAGE = 3 * QC, SUM = STAGE + 2 * F_STAGE;
   extern __shared__ char raw[];
   char* smem = reinterpret_cast<char*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-  char* Qs = smem;          // [3][DP / 64][128 rows][64]
-  char* Ks = Qs + 3 * QT;   // [3][DP / 64][64 rows][64]
-  char* Vs = Ks + 3 * KT;
-  FCtl* ctl = reinterpret_cast<FCtl*>(Vs + 3 * KT);
+  char* Ks = smem;          // [2 turns][3][DP / 64][64 rows][64]
+  char* Vs = Ks + 6 * KT;
+  FCtl* ctl = reinterpret_cast<FCtl*>(Vs + 6 * KT);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) {
     tc::mbar_init(&ctl->qfull, F_WEIGH);
-    tc::mbar_init(&ctl->kfull, F_COPY / 2);
-    tc::mbar_init(&ctl->vfull, F_COPY / 2);
-    tc::mbar_init(&ctl->kempty, 1);
-    tc::mbar_init(&ctl->vempty, 1);
+    tc::mbar_init(&ctl->ofull, 1);
     tc::mbar_init(&ctl->drained, 1);
     for (int x = 0; x < 2; ++x) {
+      tc::mbar_init(&ctl->kfull[x], F_COPY / 2);
+      tc::mbar_init(&ctl->vfull[x], F_COPY / 2);
+      tc::mbar_init(&ctl->kempty[x], 1);
+      tc::mbar_init(&ctl->vempty[x], 1);
       tc::mbar_init(&ctl->sfull[x], 1);
       tc::mbar_init(&ctl->pfull[x], F_WEIGH);
-      tc::mbar_init(&ctl->ofull[x], 1);
     }
     ctl->abort = 0;
     ctl->strange = 0;
@@ -161,20 +166,36 @@ __global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_
     const int kv = (warp - F_WEIGH) / W, w = warp - F_WEIGH - kv * W, c = lane % C, rw = lane / C;
     const char* pool = (kv ? a.c.v : a.c.k) + c * 32;
     char* tiles = kv ? Vs : Ks;
-    uint64_t *full = kv ? &ctl->vfull : &ctl->kfull, *empty = kv ? &ctl->vempty : &ctl->kempty;
+    uint64_t *full = kv ? ctl->vfull : ctl->kfull, *empty = kv ? ctl->vempty : ctl->kempty;
     const bool ok0 = c * 8 < a.c.d, ok1 = c * 8 + 4 < a.c.d;
-    // the place of the warp's row (step, rw) = (lane / RW, lane % RW)
-    auto look_up = [&](int x) {
-      const int r = (lane / RW * W + w) * RW + lane % RW, j = key0(x) + r;
-      return lane < STEPS * RW && r < FK && x < turns && j < key1(x) ? kv_row(a.c, b, h, j) : -1;
+    // the place of the warp's row (step, rw) = (lane / RW, lane % RW): its page is read a turn
+    // before it is needed, and looked at only then
+    struct Place {
+      int page, slot;
     };
-    long long next = look_up(0);
-    f32x2 bad = 0ull;
-    for (int x = 0; x < turns; ++x) {
-      float4 v[STEPS][2];
+    auto look_up = [&](int x) {
+      Place p = {0, -1};
+      const int r = (lane / RW * W + w) * RW + lane % RW, j = key0(x) + r;
+      if (lane < STEPS * RW && r < FK && x < turns && j < key1(x)) {
+        const unsigned y = (unsigned)j / (unsigned)a.c.ps;
+        p.page = a.c.table[(long long)b * a.c.max_pages + y];
+        p.slot = j - (int)y * a.c.ps;
+      }
+      return p;
+    };
+    auto row_of = [&](const Place& p) {
+      if (p.slot < 0) return -1LL;
+      if ((unsigned)p.page >= (unsigned)a.c.num_pages) {
+        set_status(a.c.status, CACHE_BAD);
+        return -1LL;
+      }
+      return p.page * a.c.page_stride + h * a.c.head_stride + p.slot * a.c.slot_stride;
+    };
+    float4 v[STEPS][2];
+    auto load = [&](long long rows) {
 #pragma unroll
       for (int k = 0; k < STEPS; ++k) {
-        const long long o = __shfl_sync(FULL, next, k * RW + rw);
+        const long long o = __shfl_sync(FULL, rows, k * RW + rw);
         v[k][0] = v[k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (o >= 0) {
           const float4* src = reinterpret_cast<const float4*>(pool + o * 4);
@@ -182,22 +203,32 @@ __global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_
           if (ok1) v[k][1] = src[1];
         }
       }
-      next = look_up(x + 1);
-      if (x > 0 && !__all_sync(FULL, wait_for(empty, (x - 1) & 1, &ctl->abort))) break;
+    };
+    f32x2 bad = 0ull;  // becomes NaN with a key or value that is not finite
+    load(row_of(look_up(0)));
+    Place next = look_up(1);
+    for (int x = 0; x < turns; ++x) {
+      if (x > 1 &&
+          !__all_sync(FULL, wait_for(&empty[x & 1], ((x >> 1) & 1) ^ 1, &ctl->abort)))
+        break;
+      char* dst = tiles + (x & 1) * 3 * KT;
+      const long long rows = row_of(next);
+      next = look_up(x + 2);
 #pragma unroll
       for (int k = 0; k < STEPS; ++k) {
         const int r = (k * W + w) * RW + rw;
-        if (r >= FK) break;
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           bad = fma2(pair(v[k][y].x, v[k][y].y), 0ull, bad);
           bad = fma2(pair(v[k][y].z, v[k][y].w), 0ull, bad);
         }
-        cut8(tiles + (c >> 3) * FK * 128 + r * 128 + (((c ^ r) & 7) * 16), KT, v[k][0], v[k][1]);
+        if (k + 1 < STEPS || r < FK)
+          cut8(dst + (c >> 3) * FK * 128 + r * 128 + (((c ^ r) & 7) * 16), KT, v[k][0], v[k][1]);
       }
       fence_async();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(full);
+      if (lane == 0) tc::mbar_arrive(&full[x & 1]);
+      load(rows);  // waited for at the next turn's stores
     }
     const float2 z = unpair(bad);
     if (!(z.x == 0.f && z.y == 0.f)) ctl->strange = 1;
@@ -206,7 +237,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_
     constexpr uint32_t sdesc = tc::idesc_bf16_f32(TM, FK);
     constexpr uint32_t odesc = tc::idesc_bf16_f32(TM, DP) | (1u << 16);  // B is MN-major
     const uint32_t go = elect_one();
-    const uint64_t qd = tc::desc_sw128_kmajor(Qs), kd = tc::desc_sw128_kmajor(Ks),
+    const uint64_t kd = tc::desc_sw128_kmajor(Ks),
                    vd = desc_sw128_mnmajor(tc::smem_u32(Vs), FK * 128);
     auto ready = [&](uint64_t* bar, uint32_t parity) {
       const bool ok = wait_for(bar, parity, &ctl->abort);
@@ -214,43 +245,45 @@ __global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_
     };
     // six products of parts, the smallest first
     auto logits = [&](int x) {
-      const uint32_t d = tmem + (x & 1) * F_STAGE;
+      const uint32_t d = tmem + STAGE + (x & 1) * F_STAGE;
+      const uint64_t kb = kd + (x & 1) * (3 * KT / 16);
 #pragma unroll
       for (int e = 0; e < 6; ++e) {
         constexpr int P[6] = {0, 2, 1, 0, 1, 0}, R[6] = {2, 0, 1, 1, 0, 0};
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k)
-          mma_ss(go, d, qd + (P[e] * QT + (k >> 2) * TM * 128 + (k & 3) * 32) / 16,
-                 kd + (R[e] * KT + (k >> 2) * FK * 128 + (k & 3) * 32) / 16, sdesc, e > 0 || k > 0);
+          mma_ts(go, d, tmem + P[e] * QC + k * 8,
+                 kb + (R[e] * KT + (k >> 2) * FK * 128 + (k & 3) * 32) / 16, sdesc, e > 0 || k > 0);
       }
       commit(go, &ctl->sfull[x & 1]);
-      commit(go, &ctl->kempty);
+      commit(go, &ctl->kempty[x & 1]);
     };
-    bool ok = ready(&ctl->qfull, 0) && ready(&ctl->kfull, 0);
+    bool ok = ready(&ctl->qfull, 0) && ready(&ctl->kfull[0], 0);
     tc::fence_after_sync();
     if (ok) logits(0);
 #pragma unroll 1
     for (int x = 0; x < turns && ok; ++x) {
       if (x + 1 < turns) {
-        ok = ready(&ctl->kfull, (x + 1) & 1);
+        ok = ready(&ctl->kfull[(x + 1) & 1], ((x + 1) >> 1) & 1);
         if (!ok) break;
         tc::fence_after_sync();
         logits(x + 1);
       }
-      ok = ready(&ctl->pfull[x & 1], (x >> 1) & 1) && ready(&ctl->vfull, x & 1);
+      ok = ready(&ctl->pfull[x & 1], (x >> 1) & 1) && ready(&ctl->vfull[x & 1], (x >> 1) & 1);
       if (!ok) break;
       tc::fence_after_sync();
-      const uint32_t p = tmem + (x & 1) * F_STAGE, d = tmem + 2 * F_STAGE + (x & 1) * DP;
+      const uint32_t p = tmem + STAGE + (x & 1) * F_STAGE, d = tmem + SUM;
+      const uint64_t vb = vd + (x & 1) * (3 * KT / 16);
 #pragma unroll
       for (int e = 0; e < 6; ++e) {
         constexpr int P[6] = {0, 2, 1, 0, 1, 0}, R[6] = {2, 0, 1, 1, 0, 0};
 #pragma unroll
         for (int k = 0; k < FK / 16; ++k)
-          mma_ts(go, d, p + P[e] * 32 + k * 8, vd + (R[e] * KT + k * 2048) / 16, odesc,
+          mma_ts(go, d, p + P[e] * 32 + k * 8, vb + (R[e] * KT + k * 2048) / 16, odesc,
                  e > 0 || k > 0);
       }
-      commit(go, &ctl->ofull[x & 1]);
-      commit(go, &ctl->vempty);
+      commit(go, &ctl->ofull);
+      commit(go, &ctl->vempty[x & 1]);
     }
     if (!ok) {  // products in flight end before tensor memory is freed
       commit(go, &ctl->drained);
@@ -261,41 +294,50 @@ __global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_
     __syncwarp();
   } else if (warp < F_WEIGH) {
     // ---- weights and output ---------------------------------------------------------------
-    if (turns > 0) {  // the queries' tile
-      for (int x = tid; x < TM * C; x += F_WEIGH * 32) {
-        const int r = x / C, c = x % C, t = by_g.of(r), g = r - t * a.G;
-        float4 lo = make_float4(0.f, 0.f, 0.f, 0.f), hi = lo;
-        if (t < nt) {
-          const float* q = reinterpret_cast<const float*>(a.q) + (nr.off + t0 + t) * a.q_row +
-                           (long long)(h * a.G + g) * a.q_head + c * 8;
-          if (c * 8 < a.c.d) lo = *reinterpret_cast<const float4*>(q);
-          if (c * 8 + 4 < a.c.d) hi = *reinterpret_cast<const float4*>(q + 4);
-        }
-        cut8(Qs + (c >> 3) * TM * 128 + r * 128 + (((c ^ r) & 7) * 16), QT, lo, hi);
-      }
-      fence_async();
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&ctl->qfull);
-    }
     constexpr int OC = DP / 2;  // columns of a thread
     const int half = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
     const int tok = by_g.of(r), g = r - tok * a.G;
     const bool valid = tok < nt;
     const int i = i0 + tok;
     const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
+    const int hq = h * a.G + g;
+    const long long row = nr.off + t0 + tok;
+    if (turns > 0) {  // the queries: half a row a thread
+      const float* q = reinterpret_cast<const float*>(a.q) + row * a.q_row +
+                       (long long)hq * a.q_head + half * OC;
+#pragma unroll
+      for (int c = 0; c < OC; c += 16) {
+        uint32_t p[3][8];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (valid && half * OC + c + 4 * y < a.c.d)
+            v = *reinterpret_cast<const float4*>(q + c + 4 * y);
+          cut2(v.x, v.y, &p[0][2 * y], &p[1][2 * y], &p[2][2 * y]);
+          cut2(v.z, v.w, &p[0][2 * y + 1], &p[1][2 * y + 1], &p[2][2 * y + 1]);
+        }
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          tmem_st8_async(lanes + e * QC + (half * OC + c) / 2, p[e]);
+      }
+      tmem_wait_st();
+      tc::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&ctl->qfull);
+    }
     float m = -INFINITY, l = 0.f;
     f32x2 o[OC / 2];
 #pragma unroll
     for (int c = 0; c < OC / 2; ++c) o[c] = 0ull;
     // adds the products of turn x
     auto add_up = [&](int x) {
-      wait_for(&ctl->ofull[x & 1], (x >> 1) & 1, &ctl->abort);
+      wait_for(&ctl->ofull, x & 1, &ctl->abort);
       __syncwarp();
       tc::fence_after_sync();
 #pragma unroll
       for (int c = 0; c < OC; c += 32) {
         float v[32];
-        tc::tmem_ld32(lanes + 2 * F_STAGE + (x & 1) * DP + half * OC + c, v);
+        tc::tmem_ld32(lanes + SUM + half * OC + c, v);
 #pragma unroll
         for (int y = 0; y < 16; ++y)
           o[c / 2 + y] = add2(o[c / 2 + y], pair(v[2 * y], v[2 * y + 1]));
@@ -303,7 +345,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_
     };
     // a wait that runs out makes the next ones return at once; all threads stay in step
     for (int x = 0; x < turns; ++x) {
-      const uint32_t at = lanes + (x & 1) * F_STAGE;
+      const uint32_t at = lanes + STAGE + (x & 1) * F_STAGE;
       const int j0 = key0(x), j1 = key1(x);
       wait_for(&ctl->sfull[x & 1], (x >> 1) & 1, &ctl->abort);
       __syncwarp();
@@ -342,24 +384,28 @@ __global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_
       const float base = m == -INFINITY ? 0.f : m;
       const f32x2 scale = pair(a.scale2, a.scale2), off = pair(-base, -base);
       f32x2 sum[2] = {0ull, 0ull};
-      uint32_t p[3][16];
 #pragma unroll
-      for (int y = 0; y < 16; ++y) {
-        const float2 v = unpair(fma2(pair(s[2 * y], s[2 * y + 1]), scale, off));
-        const float e0 = exp2_fast(v.x), e1 = exp2_fast(v.y);
-        sum[y & 1] = add2(sum[y & 1], pair(e0, e1));
-        cut2(e0, e1, &p[0][y], &p[1][y], &p[2][y]);
+      for (int c = 0; c < 16; c += 8) {
+        uint32_t p[3][8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          const int z = 2 * (c + y);
+          const float2 v = unpair(fma2(pair(s[z], s[z + 1]), scale, off));
+          const float e0 = exp2_fast(v.x), e1 = exp2_fast(v.y);
+          sum[y & 1] = add2(sum[y & 1], pair(e0, e1));
+          cut2(e0, e1, &p[0][y], &p[1][y], &p[2][y]);
+        }
+#pragma unroll
+        for (int e = 0; e < 3; ++e) tmem_st8_async(at + e * 32 + half * 16 + c, p[e]);
       }
-#pragma unroll
-      for (int e = 0; e < 3; ++e) tmem_st16_async(at + e * 32 + half * 16, p[e]);
       tmem_wait_st();
+      const float2 both = unpair(add2(sum[0], sum[1]));
+      l += both.x + both.y;
+      if (x > 0) add_up(x - 1);  // its place is free for this turn's products after that
       tc::fence_before_sync();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&ctl->pfull[x & 1]);
-      const float2 both = unpair(add2(sum[0], sum[1]));
-      l += both.x + both.y;
       if (x > 0) {
-        add_up(x - 1);
         if (__any_sync(FULL, f != 1.f)) {
           const f32x2 ff = pair(f, f);
 #pragma unroll
@@ -371,8 +417,6 @@ __global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_
     ctl->sum[half][r] = l;
     meet(quarter);
     l = ctl->sum[0][r] + ctl->sum[1][r];
-    const int hq = h * a.G + g;
-    const long long row = nr.off + t0 + tok;
     float* dst;
     long long mine_at = -1;
     float factor = 1.f;
@@ -388,9 +432,9 @@ __global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_
       dst = reinterpret_cast<float*>(a.out);
       if (valid) mine_at = row * a.o_row + (long long)hq * a.o_head;
     }
-    // 32 rows x OC columns a warp through the queries' tile, whole rows stored
+    // 32 rows x OC columns a warp through the keys' place, whole rows stored
     constexpr int PC = OC / 4, RPI = 32 / PC;
-    char* st = Qs + warp * 32 * OC * 4;
+    char* st = Ks + warp * 32 * OC * 4;
 #pragma unroll
     for (int c = 0; c < PC; ++c) {
       const float2 lo = unpair(o[2 * c]), hi = unpair(o[2 * c + 1]);
@@ -450,13 +494,13 @@ long long f32_tiles(const KV& c, int G, long long rows, int T) {
 
 bool attend_f32_takes(const KV& c, int dtype) { return dtype == GMC_F32 && c.d <= 128; }
 
-// Parts of the key axis: where the tiles leave SMs idle, as many as fill them, four turns
+// Parts of the key axis: where the tiles leave SMs idle, as many as fill them, two turns
 // each at least.
 int attend_f32_splits(const KV& c, int G, int T) {
   const long long ctas = c.Hkv * f32_tiles(c, G, (long long)c.B * T, T);
   if (ctas > sm_count() / 2) return 1;
   return (int)std::max<long long>(
-      1, std::min<long long>({sm_count() / ctas, 32, c.cap / (4 * FK)}));
+      1, std::min<long long>({sm_count() / ctas, 32, c.cap / (2 * FK)}));
 }
 
 cudaError_t launch_attend_f32(const AttnArgs& a, cudaStream_t st) {
