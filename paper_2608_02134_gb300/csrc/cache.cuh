@@ -25,9 +25,10 @@ struct KV {
   int B, Hkv, d, ps, num_pages, max_pages, cap;
 };
 
-// Tokens of sequence b, clamped to what the cache can hold.
+// Tokens of sequence b, clamped to what the cache can hold (read from L2, see
+// k_decode_join).
 __device__ __forceinline__ int kv_len(const KV& c, int b) {
-  const int n = c.lens[b];
+  const int n = __ldcg(c.lens + b);
   if (n < 0 || n > c.cap) {
     set_status(c.status, CACHE_BAD);
     return n < 0 ? 0 : c.cap;

@@ -15,7 +15,7 @@
 // What a CTA holds of a pair that others share is left as a part in the workspace, and a
 // second kernel joins the parts of every query head in the order of the row and adds the
 // scores.  (Joined by the CTA that is last instead, one launch took 18.4 us for one
-// sequence of 322 keys where the two take 9.4: a count, a fence and the joining one after
+// sequence of 322 keys where the two take 8.4: a count, a fence and the joining one after
 // another on one SM.)
 #include <algorithm>
 
@@ -623,8 +623,8 @@ __global__ void __launch_bounds__(W * 32) k_decode(DecodeArgs a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   char* extra = smem + W * NST * R::STAGE + warp * H::EXTRA;
   float2* ml = reinterpret_cast<float2*>(smem + W * (NST * R::STAGE + H::EXTRA));  // [W][HM]
-  grid_dep_launch();
   grid_dep_wait();
+  grid_dep_launch();  // not before: k_decode_join reads the lengths ahead of its own wait
   const TurnRow turns(a);
   const int cta = W * turns.per, at = turns.all / cta < (int)blockIdx.x ? turns.all
                                                                       : (int)blockIdx.x * cta;
@@ -748,8 +748,10 @@ __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W,
                                                             int out_blocks, int blocks) {
   __shared__ float2 fin[16];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // Every CTA of k_decode was past its wait before this kernel could start: what ran before
+  // k_decode is complete, and the lengths, which k_decode does not write, can be read (from
+  // L2: kv_len) while it works.  Its parts, sums and logits are read after the wait.
   grid_dep_launch();
-  grid_dep_wait();
   const TurnRow row(a);
   Walk w;
   if ((int)blockIdx.x < out_blocks) {
@@ -758,13 +760,14 @@ __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W,
     const int b = pair / a.c.Hkv;
     w.h = pair - b * a.c.Hkv;
     const int u = row.first(a, b, &w) + w.h * w.turns;
+    const Parts p(row, W, u, w.turns, pair);
+    grid_dep_wait();
     if (w.turns == 0) {  // it sees nothing
       for (int y = lane * 4; y < dp; y += 128)
         write_head<T>(a, b, w.h, g, y, make_float4(0.f, 0.f, 0.f, 0.f), 0.f);
       if (lane == 0) write_lse(a, b, w.h, g, 0.f, 0.f);
       return;
     }
-    const Parts p(row, W, u, w.turns, pair);
     if (p.whole) return;
     for (int y = lane * 4; y < dp; y += 128) {
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -809,6 +812,8 @@ __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W,
   w.h = pair - b * a.c.Hkv;
   const int u = row.first(a, b, &w) + w.h * w.turns;
   const int x0 = (x - pair * blocks) * JN_THREADS;
+  const Parts p(row, W, u, w.turns, pair);
+  grid_dep_wait();
   if (w.turns == 0) return;
   // this thread's logits and scores on their way while the sums are joined
 #pragma unroll
@@ -818,7 +823,6 @@ __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W,
     fetch_l1(a.logits + ((long long)pair * a.places + y) * a.hs);
     fetch_l1(a.scores + (long long)pair * a.score_stride + w.seen.place(y));
   }
-  const Parts p(row, W, u, w.turns, pair);
   for (int g = warp; g < a.heads; g += JN_WARPS) {
     const float2 v = join_ml(a, p, g, lane);
     if (lane == 0) fin[g] = final_ml(v.x, v.y);
