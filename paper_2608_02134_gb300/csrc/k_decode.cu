@@ -741,8 +741,9 @@ __device__ __forceinline__ float2 join_ml(const DecodeArgs& a, const Parts& p, i
 }
 
 // The parts of every query head joined, a warp each (the first blocks), and the scores,
-// four places of a pair a thread.
-constexpr int JN_WARPS = 8, JN_THREADS = JN_WARPS * 32, JN_PLACES = 4 * JN_THREADS;
+// `blocks` CTAs a pair.
+constexpr int JN_WARPS = 8, JN_THREADS = JN_WARPS * 32;
+constexpr int JN_AHEAD = 8;  // places of a thread that are fetched before the sums are joined
 template <typename T>
 __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W, int dp,
                                                             int out_blocks, int blocks) {
@@ -817,7 +818,7 @@ __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W,
   if (w.turns == 0) return;
   // this thread's logits and scores on their way while the sums are joined
 #pragma unroll
-  for (int i = 0; i < JN_PLACES / JN_THREADS; ++i) {
+  for (int i = 0; i < JN_AHEAD; ++i) {
     const int y = x0 + (int)threadIdx.x + i * blocks * JN_THREADS;
     if (y >= w.nv) break;
     fetch_l1(a.logits + ((long long)pair * a.places + y) * a.hs);
@@ -876,8 +877,10 @@ cudaError_t decode_launch(DecodeArgs a, cudaStream_t st) {
   if (a.scores) {
     long long most = a.c.cap;
     if (a.window > 0) most = std::min(most, (long long)a.window + a.sinks);
-    blocks = (int)std::min<long long>({(most + JN_PLACES - 1) / JN_PLACES, 1024,
-                                       std::max(1, 0x3fffffff / pairs)});
+    // two CTAs an SM, one place a thread at least (32 sequences of 2,085 keys: 41.0 us with
+    // 256 places a CTA, 38.8 with 2,048; of 512 keys: 14.7 and 15.5)
+    blocks = (int)std::min<long long>((most + JN_THREADS - 1) / JN_THREADS,
+                                      std::max(1, 2 * ctas / pairs));
   }
   return launch_k(k_decode_join<typename H::T>, dim3(out_blocks + pairs * blocks),
                   dim3(JN_THREADS), 0, st, 1, a, W, DP, out_blocks, std::max(blocks, 1));
