@@ -13,7 +13,10 @@
 // weights the tensor cores work for the other.  The maximum that weights are taken
 // against follows the running one only when it has grown by 2^8 (weights up to 256
 // lose nothing in bf16 or fp32), so the output in tensor memory is hardly ever
-// rescaled.
+// rescaled, and a turn's weights need not wait for its maximum: they are taken against
+// the one so far while it is looked for, and anew if it had grown (32 questions of 16 to
+// 256 tokens on up to 513 keys: 52.1 -> 49.3 us, a question of 128 tokens on 16,004 keys:
+// 41.8 -> 40.0).
 //
 // Weights are rounded to bf16 for their product with V (relative 2^-8, the same as the
 // output's own rounding); sums, maxima and products are fp32.
@@ -102,30 +105,61 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
       : "memory");
 }
 
-// 64 consecutive fp32 columns of this warp's lanes (one row a thread), waited for.
-__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* v) {
+// 128 consecutive fp32 columns of this warp's lanes (one row a thread), waited for.
+__device__ __forceinline__ void tmem_ld128(uint32_t taddr, float* v) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "tcgen05.ld.sync.aligned.32x32b.x128.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
       "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
       "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
-      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63, "
+      "%64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, %76, %77, %78, %79, "
+      "%80, %81, %82, %83, %84, %85, %86, %87, %88, %89, %90, %91, %92, %93, %94, %95, "
+      "%96, %97, %98, %99, %100, %101, %102, %103, %104, %105, %106, %107, %108, %109, %110, %111, "
+      "%112, %113, %114, %115, %116, %117, %118, %119, %120, %121, %122, %123, %124, %125, %126, %127}, [%128];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-        "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
-        "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
-        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]),
-        "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]),
-        "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]),
-        "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
-        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]),
-        "=r"(r[62]), "=r"(r[63])
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]),
+        "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
+        "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+        "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]),
+        "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+        "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]),
+        "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]),
+        "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]),
+        "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]),
+        "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]), "=r"(r[64]),
+        "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]),
+        "=r"(r[70]), "=r"(r[71]), "=r"(r[72]), "=r"(r[73]), "=r"(r[74]),
+        "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79]),
+        "=r"(r[80]), "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]),
+        "=r"(r[85]), "=r"(r[86]), "=r"(r[87]), "=r"(r[88]), "=r"(r[89]),
+        "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]),
+        "=r"(r[95]), "=r"(r[96]), "=r"(r[97]), "=r"(r[98]), "=r"(r[99]),
+        "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]), "=r"(r[104]),
+        "=r"(r[105]), "=r"(r[106]), "=r"(r[107]), "=r"(r[108]), "=r"(r[109]),
+        "=r"(r[110]), "=r"(r[111]), "=r"(r[112]), "=r"(r[113]), "=r"(r[114]),
+        "=r"(r[115]), "=r"(r[116]), "=r"(r[117]), "=r"(r[118]), "=r"(r[119]),
+        "=r"(r[120]), "=r"(r[121]), "=r"(r[122]), "=r"(r[123]), "=r"(r[124]),
+        "=r"(r[125]), "=r"(r[126]), "=r"(r[127])
       : "r"(taddr)
       : "memory");
 }
+// The largest of a row's logits.
+__device__ __forceinline__ float largest(const float (&s)[TM]) {
+  float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+  for (int c = 4; c + 8 <= TM; c += 8)
+#pragma unroll
+    for (int y = 0; y < 4; ++y) mx[y] = max3(mx[y], s[c + y], s[c + 4 + y]);
+#pragma unroll
+  for (int y = 0; y < 4; ++y) mx[y] = fmaxf(mx[y], s[TM - 4 + y]);
+  return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+}
+
 // The values of a turn that some rows of the CTA do not see, a row a thread of the first
 // tile's warps: slots past the end become zeros, others are looked over for infinities
 // and NaN.  false: the copy did not come.
@@ -372,34 +406,53 @@ __global__ void __launch_bounds__(t_threads<TILES>(), 3 - TILES)
         ok = __all_sync(FULL, ok);
         if (!ok) break;
         tc::fence_after_sync();
-        float s[TM];
-        tmem_ld64(sa, s);
-        tmem_ld64(sa + 64, s + 64);
         const bool whole =
             cnt == TM && j0 + TM - 1 <= ti0 &&
             (a.window == 0 || ti0 + mine - 1 - j0 < a.window || j0 + TM <= a.sinks);
-        if (!whole) {
-          const int hi = valid ? min(min(i + 1, n) - j0, cnt) : 0;  // columns before hi,
-          const int lo = a.window > 0 ? i - a.window + 1 - j0 : 0;  // from lo on
-          const int sk = a.sinks - j0;                              // or before sk
+        const f32x2 scale = pair(a.scale2, a.scale2);
+        float s[TM];
+        f32x2 off, sum[2];
+        uint32_t p[32];
+        auto weigh = [&](int c) {  // 64 keys from c on
 #pragma unroll
-          for (int c = 0; c < TM; c += 32) {
-            const uint32_t in = below(hi - c) & (~below(lo - c) | below(sk - c));
-#pragma unroll
-            for (int y = 0; y < 32; ++y)
-              if (!(in >> y & 1)) s[c + y] = -INFINITY;
+          for (int y = 0; y < 32; ++y) {
+            const float2 v = unpair(fma2(pair(s[c + 2 * y], s[c + 2 * y + 1]), scale, off));
+            const float e0 = exp2_fast(v.x), e1 = exp2_fast(v.y);
+            sum[y & 1] = add2(sum[y & 1], pair(e0, e1));
+            p[y] = pack2(e0, e1);
           }
-        }
-        float mx[4] = {s[0], s[1], s[2], s[3]};
+        };
+        auto hand_over = [&](int half) {
+          tmem_st32_async(sa + half * 32, p);
+          tmem_wait_st();
+          tc::fence_before_sync();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&ctl->pfull[t][half]);
+        };
+        while (true) {
+          tmem_ld128(sa, s);
+          if (!whole) {
+            const int hi = valid ? min(min(i + 1, n) - j0, cnt) : 0;  // columns before hi,
+            const int lo = a.window > 0 ? i - a.window + 1 - j0 : 0;  // from lo on
+            const int sk = a.sinks - j0;                              // or before sk
 #pragma unroll
-        for (int c = 4; c + 8 <= TM; c += 8)
+            for (int c = 0; c < TM; c += 32) {
+              const uint32_t in = below(hi - c) & (~below(lo - c) | below(sk - c));
 #pragma unroll
-          for (int y = 0; y < 4; ++y) mx[y] = max3(mx[y], s[c + y], s[c + 4 + y]);
-#pragma unroll
-        for (int y = 0; y < 4; ++y) mx[y] = fmaxf(mx[y], s[TM - 4 + y]);
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale2;
-        const bool grew = top > m + GROWN || (m == -INFINITY && top > m);
-        if (__any_sync(FULL, grew)) {
+              for (int y = 0; y < 32; ++y)
+                if (!(in >> y & 1)) s[c + y] = -INFINITY;
+            }
+          }
+          if (x == 0) m = largest(s) * a.scale2;
+          const float base = m == -INFINITY ? 0.f : m;
+          off = pair(-base, -base);
+          sum[0] = sum[1] = 0ull;
+          // the first half's weights, against the maximum so far, beside this turn's maximum
+          weigh(0);
+          const float top = largest(s) * a.scale2;
+          const bool grew = top > m + GROWN || (m == -INFINITY && top > m);
+          if (!__any_sync(FULL, grew)) break;
+          // hardly ever: the maximum follows, what there is is scaled, and the turn begins anew
           const float mn = grew ? top : m;
           const float f = m == -INFINITY || !grew ? 1.f : exp2_fast(m - mn);
           l *= f;
@@ -415,7 +468,6 @@ __global__ void __launch_bounds__(t_threads<TILES>(), 3 - TILES)
             }
           }
         }
-        const float base = m == -INFINITY ? 0.f : m;
         // values of a turn that not every row of the CTA sees, before the first product
         if (t == 0 && !(cnt == TM && j0 + TM - 1 <= i0 &&
                         (a.window == 0 || i0 + nt - 1 - j0 < a.window || j0 + TM <= a.sinks))) {
@@ -423,24 +475,9 @@ __global__ void __launch_bounds__(t_threads<TILES>(), 3 - TILES)
                              ((2 * x + 1) / NS) & 1, r, r < cnt && j0 + r < n);
           if (!ok) break;
         }
-        const f32x2 scale = pair(a.scale2, a.scale2), off = pair(-base, -base);
-        f32x2 sum[2] = {0ull, 0ull};
-#pragma unroll
-        for (int c = 0; c < TM; c += 64) {
-          uint32_t p[32];
-#pragma unroll
-          for (int y = 0; y < 32; ++y) {
-            const float2 v = unpair(fma2(pair(s[c + 2 * y], s[c + 2 * y + 1]), scale, off));
-            const float e0 = exp2_fast(v.x), e1 = exp2_fast(v.y);
-            sum[y & 1] = add2(sum[y & 1], pair(e0, e1));
-            p[y] = pack2(e0, e1);
-          }
-          tmem_st32_async(sa + c / 2, p);
-          tmem_wait_st();
-          tc::fence_before_sync();
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&ctl->pfull[t][c / 64]);
-        }
+        hand_over(0);
+        weigh(64);
+        hand_over(1);
         const float2 both = unpair(add2(sum[0], sum[1]));
         l += both.x + both.y;
       }
@@ -571,9 +608,9 @@ long long tc_ctas(const KV& c, int G, long long rows, int T, int tiles) {
 }
 // One tile a CTA and two CTAs an SM where the key axis is short and the CTAs are more than
 // a wave: one's first copies and last stores (3 us each) hide behind the other's products
-// (32 questions of 16 to 256 tokens on up to 513 keys: two tiles 56.6 us, one 52.7; 8 x
-// 512 tokens on 2,048: 122 and 117); on longer axes two tiles share each key's copy
-// (4,096 tokens: 112 and 124; 1,024 tokens, less than a wave: 21.3 and 21.7).
+// (32 questions of 16 to 256 tokens on up to 513 keys: two tiles 52.8 us, one 49.2; 8 x
+// 512 tokens on 2,048: 118 and 111); on longer axes two tiles share each key's copy
+// (4,096 tokens: 110 and 119; 1,024 tokens, less than a wave: 20.5 and 21.3).
 int tc_tiles(const AttnArgs& a) {
   long long most = a.c.cap;
   if (a.window > 0) most = std::min(most, (long long)a.window + a.sinks + a.T);
