@@ -168,10 +168,11 @@ __device__ __noinline__ void row_alone(const AttnArgs& a, int b, int h, long lon
 }
 
 // The sequence and the tile of it (`tokens` new tokens each) that is number c of all.
-__device__ __forceinline__ bool find_tile(const AttnArgs& a, int c, int tokens, int* b, int* tile,
-                                          NewRows* nr, int* n) {
+__device__ __forceinline__ bool find_tile(const AttnArgs& a, int c, int tokens, const Div& by_tokens,
+                                          int* b, int* tile, NewRows* nr, int* n) {
+  auto tiles = [&](int T) { return by_tokens.of(T + tokens - 1); };
   if (!a.q_offsets) {
-    const int each = ceil_div(a.T, tokens);
+    const int each = tiles(a.T);
     *b = c / each;
     *tile = c - *b * each;
     if (*b >= a.c.B) return false;
@@ -186,9 +187,11 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, int c, int tokens, 
   NewRows last = {0, 0};
 #pragma unroll 4
   for (int x = b0; x < b1; ++x) {
-    last = new_rows(a.q_offsets, x, a.rows, a.T, a.c.status);
-    len = kv_len(a.c, x);
-    mine += ceil_div(last.T, tokens);
+    // all on their way before the first is looked at
+    const int from = a.q_offsets[x], to = a.q_offsets[x + 1], raw = __ldcg(a.c.lens + x);
+    last = new_rows(from, to, a.rows, a.T, a.c.status);
+    len = kv_clamp(a.c, raw);
+    mine += tiles(last.T);
   }
   int sum = mine;
 #pragma unroll
@@ -211,7 +214,7 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, int c, int tokens, 
   }
   for (int x = lo * cs;; ++x) {
     *nr = new_rows(a.q_offsets, x, a.rows, a.T, a.c.status);
-    const int here = ceil_div(nr->T, tokens);
+    const int here = tiles(nr->T);
     if (u < here) {
       *b = x;
       *tile = u;

@@ -27,13 +27,15 @@ struct KV {
 
 // Tokens of sequence b, clamped to what the cache can hold (read from L2, see
 // k_decode_join).
-__device__ __forceinline__ int kv_len(const KV& c, int b) {
-  const int n = __ldcg(c.lens + b);
+__device__ __forceinline__ int kv_clamp(const KV& c, int n) {
   if (n < 0 || n > c.cap) {
     set_status(c.status, CACHE_BAD);
     return n < 0 ? 0 : c.cap;
   }
   return n;
+}
+__device__ __forceinline__ int kv_len(const KV& c, int b) {
+  return kv_clamp(c, __ldcg(c.lens + b));
 }
 
 // Element offset of token j's row of key head h (the same in both pools), or -1
@@ -52,22 +54,22 @@ __device__ __forceinline__ long long kv_row(const KV& c, int b, int h, int j) {
 struct NewRows {
   int off, T;
 };
-__device__ __forceinline__ NewRows new_rows(const int32_t* offsets, int b, int rows, int Tmax,
+__device__ __forceinline__ NewRows new_rows(int from, int to, int rows, int Tmax,
                                             uint32_t* status) {
   NewRows r;
-  if (!offsets) {
-    r.off = b * Tmax;
-    r.T = Tmax;
-    return r;
-  }
-  r.off = offsets[b];
-  r.T = offsets[b + 1] - r.off;
+  r.off = from;
+  r.T = to - from;
   if (r.T < 0 || r.T > Tmax || r.off < 0 || (long long)r.off + r.T > rows) {
     set_status(status, CACHE_BAD);
     r.off = 0;
     r.T = 0;
   }
   return r;
+}
+__device__ __forceinline__ NewRows new_rows(const int32_t* offsets, int b, int rows, int Tmax,
+                                            uint32_t* status) {
+  if (!offsets) return {b * Tmax, Tmax};
+  return new_rows(offsets[b], offsets[b + 1], rows, Tmax, status);
 }
 
 // The keys that the queries at places i0 .. i1 see between them: [0, a) and

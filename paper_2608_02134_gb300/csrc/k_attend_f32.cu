@@ -107,7 +107,7 @@ __device__ __forceinline__ void meet(int quarter) {
 }
 
 template <int DP>
-__global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_g) {
+__global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_g, Div by_tokens) {
   constexpr int KT = FK * DP * 2, C = DP / 8;
   // tensor memory: the queries' three parts, two turns of logits and weights, one of output
   constexpr int QC = DP / 2, STAGE = 3 * QC, SUM = STAGE + 2 * F_STAGE;
@@ -137,11 +137,11 @@ __global__ void __launch_bounds__(F_THREADS, 1) k_attend_f32(AttnArgs a, Div by_
   grid_dep_wait();
   // key heads first: neighbouring CTAs are equally long, the longest ones start first
   const int h = blockIdx.x % a.c.Hkv, part = blockIdx.x / a.c.Hkv, split = part % a.splits;
-  const int tpt = TM / a.G;  // tokens of a tile
+  const int tpt = by_g.of(TM);  // tokens of a tile
   int b, tile, n;
   NewRows nr;
-  if (!find_tile(a, part / a.splits, tpt, &b, &tile, &nr, &n)) return;
-  const int t0 = (ceil_div(nr.T, tpt) - 1 - tile) * tpt;
+  if (!find_tile(a, part / a.splits, tpt, by_tokens, &b, &tile, &nr, &n)) return;
+  const int t0 = (by_tokens.of(nr.T + tpt - 1) - 1 - tile) * tpt;
   const int nt = min(tpt, nr.T - t0);
   if (warp == F_ISSUE) {
     tc::tmem_alloc(&ctl->tmem, 512);
@@ -508,7 +508,8 @@ cudaError_t launch_attend_f32(const AttnArgs& a, cudaStream_t st) {
   auto go = [&](auto kernel, size_t smem) {
     const cudaError_t e = set_smem_limit((const void*)kernel, smem);
     if (e != cudaSuccess) return e;
-    return launch_k(kernel, dim3((unsigned)grid), dim3(F_THREADS), smem, st, 1, a, make_div(a.G));
+    return launch_k(kernel, dim3((unsigned)grid), dim3(F_THREADS), smem, st, 1, a, make_div(a.G),
+                    make_div(TM / a.G));
   };
   return a.c.d <= 64 ? go(k_attend_f32<64>, f_smem<64>()) : go(k_attend_f32<128>, f_smem<128>());
 }

@@ -59,7 +59,7 @@ template <int DP, int TILES> constexpr size_t t_smem() {
 // in pieces of 128 (the last one short).
 struct Turns {
   int ps, kt, ppt, tpp;
-  Div by_ps, by_kt, by_tpp, by_g;
+  Div by_ps, by_kt, by_tpp, by_g, by_tokens;
   __device__ __forceinline__ int of(int j) const {  // the turn that holds place j
     if (ps <= TM) return by_kt.of(j);
     const int p = by_ps.of(j);
@@ -75,7 +75,7 @@ struct Turns {
     return min(TM, ps - (u - by_tpp.of(u) * tpp) * TM);
   }
 };
-Turns make_turns(int ps, int G) {
+Turns make_turns(int ps, int G, int tiles) {
   Turns t;
   t.ps = ps;
   t.ppt = ps <= TM ? TM / ps : 1;
@@ -85,6 +85,7 @@ Turns make_turns(int ps, int G) {
   t.by_kt = make_div(t.kt);
   t.by_tpp = make_div(t.tpp);
   t.by_g = make_div(G);
+  t.by_tokens = make_div(TM / G * tiles);
   return t;
 }
 
@@ -228,14 +229,52 @@ __global__ void __launch_bounds__(t_threads<TILES>(), 3 - TILES)
   }
   grid_dep_launch();
   grid_dep_wait();
-  const int h = blockIdx.y, split = blockIdx.x % a.splits;
-  const int tpt = TM / a.G;  // tokens of a tile
+  const int h = blockIdx.y;
+  int c = blockIdx.x, split = 0;
+  if (a.splits > 1) {
+    c = blockIdx.x / a.splits;
+    split = blockIdx.x - c * a.splits;
+  }
+  const int tpt = tn.by_g.of(TM);  // tokens of a tile
   int b, tile, n;
   NewRows nr;
-  if (!find_tile(a, blockIdx.x / a.splits, tpt * TILES, &b, &tile, &nr, &n)) return;
+  if (!find_tile(a, c, tpt * TILES, tn.by_tokens, &b, &tile, &nr, &n)) return;
   // the last tokens see the most keys: they go first
-  const int t0 = (ceil_div(nr.T, tpt * TILES) - 1 - tile) * tpt * TILES;
+  const int t0 = (tn.by_tokens.of(nr.T + tpt * TILES - 1) - 1 - tile) * tpt * TILES;
   const int nt = min(tpt * TILES, nr.T - t0);  // tokens of this CTA
+  const int i0 = n - nr.T + t0;
+  const int two = TILES == 2 && nt > tpt ? 2 : 1;
+  int turns = 0, na = 0, ub0 = 0, x0 = 0;
+  {
+    const Seen seen = seen_keys(i0, i0 + nt - 1, a.window, a.sinks);
+    if (seen.b1 > 0) {
+      ub0 = tn.of(min(seen.b0, seen.b1 - 1));
+      na = seen.a > 0 ? min(tn.of(seen.a - 1) + 1, ub0) : 0;
+      const int all = na + tn.of(seen.b1 - 1) + 1 - ub0;
+      const int per = a.splits > 1 ? ceil_div(all, a.splits) : all;
+      x0 = min(all, split * per);
+      turns = min(all, x0 + per) - x0;
+    }
+  }
+  auto turn_at = [&](int x) { return x0 + x < na ? x0 + x : ub0 + x0 + x - na; };
+
+  const int box = tn.ps <= TM ? tn.ps : TM;  // rows of a copy
+  const int half = lane % NH, pg = lane / NH;
+  // this lane's page of turn x; num_pages (past the pool, zeros) where there is none
+  auto look_up = [&](int x, int* slot) {
+    *slot = 0;
+    if (pg >= tn.ppt || x >= turns) return a.c.num_pages;
+    const int u = turn_at(x), j = tn.first(u) + pg * tn.ps;
+    if (j >= n) return a.c.num_pages;
+    const int p = tn.by_ps.of(j);
+    *slot = j - p * tn.ps;
+    const int page = a.c.table[(long long)b * a.c.max_pages + p];
+    if ((unsigned)page < (unsigned)a.c.num_pages) return page;
+    set_status(a.c.status, CACHE_BAD);
+    return a.c.num_pages;
+  };
+  int slot = 0, page = 0;
+  if (warp == COPY) page = look_up(0, &slot);  // on its way while the CTA gets ready
   if (tn.kt < TM) {  // rows of a slot that no copy writes
     const int per = (TM - tn.kt) * 8;
     for (int x = tid; x < NS * NH * per; x += THREADS) {
@@ -252,22 +291,6 @@ __global__ void __launch_bounds__(t_threads<TILES>(), 3 - TILES)
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = ctl->tmem;
-  const int i0 = n - nr.T + t0;
-  const int two = TILES == 2 && nt > tpt ? 2 : 1;
-  int turns = 0, na = 0, ub0 = 0, x0 = 0;
-  {
-    const Seen seen = seen_keys(i0, i0 + nt - 1, a.window, a.sinks);
-    if (seen.b1 > 0) {
-      ub0 = tn.of(min(seen.b0, seen.b1 - 1));
-      na = seen.a > 0 ? min(tn.of(seen.a - 1) + 1, ub0) : 0;
-      const int all = na + tn.of(seen.b1 - 1) + 1 - ub0;
-      const int per = ceil_div(all, a.splits);
-      x0 = min(all, split * per);
-      turns = min(all, x0 + per) - x0;
-    }
-  }
-  auto turn_at = [&](int x) { return x0 + x < na ? x0 + x : ub0 + x0 + x - na; };
-
   int issued = 0;  // copies started (copying warp)
   if (turns > 0 && warp == COPY) {
     // ---- copies ---------------------------------------------------------------------
@@ -278,22 +301,6 @@ __global__ void __launch_bounds__(t_threads<TILES>(), 3 - TILES)
           tma_load_3d(Qs + t * SLOT + c * HALF, &qmap, c * 64, h * a.G, nr.off + t0 + t * tpt,
                       &ctl->qfull);
     }
-    const int box = tn.ps <= TM ? tn.ps : TM;  // rows of a copy
-    const int half = lane % NH, pg = lane / NH;
-    // this lane's page of turn x; num_pages (past the pool, zeros) where there is none
-    auto look_up = [&](int x, int* slot) {
-      *slot = 0;
-      if (pg >= tn.ppt || x >= turns) return a.c.num_pages;
-      const int u = turn_at(x), j = tn.first(u) + pg * tn.ps;
-      if (j >= n) return a.c.num_pages;
-      const int p = tn.by_ps.of(j);
-      *slot = j - p * tn.ps;
-      const int page = a.c.table[(long long)b * a.c.max_pages + p];
-      if ((unsigned)page < (unsigned)a.c.num_pages) return page;
-      set_status(a.c.status, CACHE_BAD);
-      return a.c.num_pages;
-    };
-    int slot, page = look_up(0, &slot);
     bool ok = true;
     for (int x = 0; x < turns && ok; ++x) {
       int nslot;
@@ -510,18 +517,22 @@ __global__ void __launch_bounds__(t_threads<TILES>(), 3 - TILES)
         const long long mine_at = valid ? row * a.o_row + (long long)hq * a.o_head : -1;
         // 32 rows a warp through its part of the queries' tile, whole rows stored
         char* st = Qs + t * SLOT + (warp & 3) * 32 * DP * 2;
-#pragma unroll 1
-        for (int c = 0; c < DP; c += 32) {
-          float o[32];
+        {
+          float o[DP];
           if (ok && turns > 0) {
-            tc::tmem_ld32(oa + c, o);
+            if constexpr (DP == 128) {
+              tmem_ld128(oa, o);
+            } else {
+              tc::tmem_ld32(oa, o);
+              tc::tmem_ld32(oa + 32, o + 32);
+            }
           } else {
 #pragma unroll
-            for (int y = 0; y < 32; ++y) o[y] = 0.f;
+            for (int y = 0; y < DP; ++y) o[y] = 0.f;
           }
 #pragma unroll
-          for (int y = 0; y < 32; y += 8) {
-            const int pc = (c + y) / 8;
+          for (int y = 0; y < DP; y += 8) {
+            const int pc = y / 8;
             *reinterpret_cast<int4*>(st + lane * DP * 2 + ((pc ^ (lane & 7)) * 16)) = make_int4(
                 pack2(o[y] * inv, o[y + 1] * inv), pack2(o[y + 2] * inv, o[y + 3] * inv),
                 pack2(o[y + 4] * inv, o[y + 5] * inv), pack2(o[y + 6] * inv, o[y + 7] * inv));
@@ -644,7 +655,7 @@ cudaError_t tc_launch(const AttnArgs& a, const CUtensorMap& qm, const CUtensorMa
   const long long tiles = tc_ctas(a.c, a.G, a.rows, a.T, TILES) / a.c.Hkv;
   return launch_k(k_attend_tc<DP, TILES>, dim3((unsigned)(tiles * a.splits), a.c.Hkv),
                   dim3(t_threads<TILES>()), smem, st, 1, qm, km, vm, a,
-                  make_turns(a.c.ps, a.G));
+                  make_turns(a.c.ps, a.G, TILES));
 }
 }  // namespace
 
