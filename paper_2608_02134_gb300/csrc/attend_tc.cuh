@@ -225,4 +225,21 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, int c, int tokens, 
   }
 }
 
+// The number of parts, `most` at most, in which a key axis of so many turns takes the least
+// time: a CTA's turns one after another (`turn` us each), and for more than one part the
+// joining kernel (2.5 us) and the parts' rows (`floats` each), written and read again at
+// about 5 TB/s.
+inline int cheapest_parts(long long most, int turns, float turn, long long floats) {
+  int best = 1;
+  float least = turns * turn;
+  for (int s = 2; s <= most; ++s) {
+    const float t = ceil_div(turns, s) * turn + 2.5f + (float)s * floats * 8.f / 5e6f;
+    if (t < least) {
+      least = t;
+      best = s;
+    }
+  }
+  return best;
+}
+
 }  // namespace gmc

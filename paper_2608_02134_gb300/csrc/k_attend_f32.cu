@@ -494,13 +494,13 @@ long long f32_tiles(const KV& c, int G, long long rows, int T) {
 
 bool attend_f32_takes(const KV& c, int dtype) { return dtype == GMC_F32 && c.d <= 128; }
 
-// Parts of the key axis: where the tiles leave SMs idle, as many as fill them, two turns
-// each at least.
+// Parts of the key axis where the tiles leave SMs idle: up to as many as fill them, two
+// turns each at least.
 int attend_f32_splits(const KV& c, int G, int T) {
-  const long long ctas = c.Hkv * f32_tiles(c, G, (long long)c.B * T, T);
+  const long long rows = (long long)c.B * T, ctas = c.Hkv * f32_tiles(c, G, rows, T);
   if (ctas > sm_count() / 2) return 1;
-  return (int)std::max<long long>(
-      1, std::min<long long>({sm_count() / ctas, 32, c.cap / (2 * FK)}));
+  return cheapest_parts(std::min<long long>({sm_count() / ctas, 32, c.cap / (2 * FK)}),
+                        ceil_div(c.cap, FK), 2.4f, rows * G * c.Hkv * c.d);
 }
 
 cudaError_t launch_attend_f32(const AttnArgs& a, cudaStream_t st) {
