@@ -1,6 +1,7 @@
 // The key-value cache's own kernels: new rows written to their pages, and the
 // best-scored rows of a sequence moved to fresh pages.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.cuh"
 
@@ -72,17 +73,16 @@ __global__ void __launch_bounds__(AP_THREADS)
 //
 // The threshold, the keep-th largest of the scores' order-preserving 32-bit keys, is
 // found in three passes of 11, 11 and 10 bits over a histogram in shared memory; keys
-// equal to it are taken from the lowest place on.  A thread holds up to 16 consecutive
+// equal to it are taken from the lowest place on.  A thread holds 2, 4, 8 or 16 consecutive
 // keys in registers, through all passes where the sequence has no more than 16,384 places,
 // so one scan over the threads' counts numbers the kept places.
 // ---------------------------------------------------------------------------
 constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32;
-constexpr int EV_EACH = 16;
 constexpr int EV_BINS = 2048, EV_COPIES = 4;  // copies by lane: fewer meet at one address
 constexpr int EV_LIST = 8192;                 // kept places of a CTA held in shared memory
 
 struct EvSmem {
-  int hist[EV_BINS * EV_COPIES];
+  int hist[2][EV_BINS * EV_COPIES];  // one is cleared while the other counts
   int list[EV_LIST];
   long long src[EV_THREADS], dst[EV_THREADS];
   int wsum[2][EV_WARPS];
@@ -94,7 +94,7 @@ struct EvSmem {
 __device__ __forceinline__ uint32_t score_key(float s) {
   if (!(s == s)) return 0x007fffffu;  // as -infinity
   const uint32_t u = __float_as_uint(s + 0.f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+  return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 
 // One more in a shared word, without a branch around it.
@@ -119,44 +119,51 @@ __device__ __forceinline__ int lanes_before(int v) {
   return sum - v;
 }
 
-__global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize, int vec, int E) {
+template <int E>
+__global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize, int vec) {
   extern __shared__ __align__(16) char ev_raw[];
   EvSmem* s = reinterpret_cast<EvSmem*>(ev_raw);
   const int r = blockIdx.x, S = gridDim.x, h = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t hist = (uint32_t)__cvta_generic_to_shared(s->hist);
+  auto clear = [&](int which) {
+    for (int x = tid; x < EV_BINS * EV_COPIES / 4; x += EV_THREADS)
+      reinterpret_cast<int4*>(s->hist[which])[x] = make_int4(0, 0, 0, 0);
+  };
+  clear(0);
   grid_dep_launch();
   grid_dep_wait();
   const long long pair = (long long)b * a.src.Hkv + h;
   const float* sc = a.scores + pair * a.score_stride;
   // this thread's places of a chunk: E from `at` on.  A row holds cap scores, so they are
   // on their way before the sequence's length is known
-  const int chunk = EV_THREADS * E;
-  float v[EV_EACH];
-  uint32_t key[EV_EACH];
+  constexpr int chunk = EV_THREADS * E;
+  float v[E];
+  uint32_t key[E];
   int at;
   auto fetch = [&](int c) {
     at = c * chunk + tid * E;
-    if (vec && at + E <= a.src.cap) {
+    if (E >= 4 && vec && at + E <= a.src.cap) {
 #pragma unroll
-      for (int x = 0; x < EV_EACH; x += 4)
-        if (x < E)
-          *reinterpret_cast<float4*>(v + x) = *reinterpret_cast<const float4*>(sc + at + x);
+      for (int x = 0; x < E; x += 4)
+        *reinterpret_cast<float4*>(v + x) = *reinterpret_cast<const float4*>(sc + at + x);
     } else {
 #pragma unroll
-      for (int x = 0; x < EV_EACH; ++x)
-        v[x] = x < E && at + x < a.src.cap ? sc[at + x] : 0.f;
+      for (int x = 0; x < E; ++x) v[x] = sc[min(at + x, a.src.cap - 1)];
     }
   };
   fetch(0);
   const int n = kv_len(a.src, b);
   const int k = min(a.keep, n), tail = n - a.recent;
   auto to_keys = [&]() {  // 0 is no key's value
+    if (at >= a.sinks && at + E <= tail) {
 #pragma unroll
-    for (int x = 0; x < EV_EACH; ++x) {
-      const int j = at + x;
-      key[x] = x >= E || j >= n ? 0u
-               : j < a.sinks || j >= tail ? 0xffffffffu : score_key(v[x]);
+      for (int x = 0; x < E; ++x) key[x] = score_key(v[x]);
+    } else {
+#pragma unroll
+      for (int x = 0; x < E; ++x) {
+        const int j = at + x;
+        key[x] = j >= n ? 0u : j < a.sinks || j >= tail ? 0xffffffffu : score_key(v[x]);
+      }
     }
   };
   int32_t* oi = a.out_idx + pair * a.keep;
@@ -178,29 +185,31 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
   if (k < n) {
     uint32_t prefix = 0;
     need = k;
-    for (int p = 0; p < 3; ++p) {
-      const int sh = p == 0 ? 21 : p == 1 ? 10 : 0, bits = p == 2 ? 10 : 11;
-      for (int x = tid; x < EV_BINS * EV_COPIES / 4; x += EV_THREADS)
-        reinterpret_cast<int4*>(s->hist)[x] = make_int4(0, 0, 0, 0);
-      __syncthreads();
+    __syncthreads();
+    auto pass = [&](auto number) {
+      constexpr int p = decltype(number)::value, sh = p == 0 ? 21 : p == 1 ? 10 : 0,
+                    bits = p == 2 ? 10 : 11;
+      const uint32_t bins = (uint32_t)__cvta_generic_to_shared(s->hist[p & 1]) + (lane & 3) * 4;
       for (int c = 0; c < chunks; ++c) {
         if (chunks > 1) {
           fetch(c);
           to_keys();
         }
 #pragma unroll
-        for (int x = 0; x < EV_EACH; ++x) {
-          if (x >= E) break;
-          count_if(hist + (((key[x] >> sh) & ((1u << bits) - 1)) * EV_COPIES + (lane & 3)) * 4,
-                   key[x] != 0 && (p == 0 || ((key[x] ^ prefix) >> (sh + bits)) == 0));
+        for (int x = 0; x < E; ++x) {
+          const uint32_t d = key[x] - prefix;
+          count_if(bins + (d >> sh) * (EV_COPIES * 4),
+                   p == 0 ? key[x] != 0 : d < 1u << (sh + bits));
         }
       }
+      if (p < 2) clear((p + 1) & 1);
       __syncthreads();
       // bins from the largest on, two a thread: the one whose keys reach the need-th
       int c[2];
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const int4 v = reinterpret_cast<const int4*>(s->hist)[EV_BINS - 1 - 2 * tid - y];
+        const int4 v =
+            reinterpret_cast<const int4*>(s->hist[p & 1])[EV_BINS - 1 - 2 * tid - y];
         c[y] = v.x + v.y + v.z + v.w;
       }
       const int here = __reduce_add_sync(FULL, c[0] + c[1]);
@@ -219,7 +228,10 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
       __syncthreads();
       prefix = s->prefix;
       need = s->need;
-    }
+    };
+    pass(std::integral_constant<int, 0>());
+    pass(std::integral_constant<int, 1>());
+    pass(std::integral_constant<int, 2>());
     thr = prefix;
   }
   // the kept places in order: larger keys and equal ones before this thread's
@@ -231,11 +243,11 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
     }
     int gt = 0, eq = 0;
 #pragma unroll
-    for (int x = 0; x < EV_EACH; ++x) {
-      if (x >= E) break;
+    for (int x = 0; x < E; ++x) {
       gt += key[x] > thr;
-      eq += key[x] == thr && thr != 0;
+      eq += key[x] == thr;
     }
+    if (thr == 0) eq = 0;
     const int both = (gt << 16) + eq;  // at most 16,384 each over the block
     const int here = __reduce_add_sync(FULL, both);
     int* ws = s->wsum[c & 1];
@@ -246,17 +258,15 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
     const int total = __reduce_add_sync(FULL, w);
     int g = g0 + (before >> 16), e = e0 + (before & 0xffff);
     if (g + min(e, need) < p1 && g + gt + min(e + eq, need) > p0) {
+      const unsigned held = min(p1 - p0, EV_LIST);
 #pragma unroll
-      for (int x = 0; x < EV_EACH; ++x) {
-        if (x >= E) break;
+      for (int x = 0; x < E; ++x) {
         const bool isg = key[x] > thr, ise = key[x] == thr && thr != 0;
-        const int pos = g + min(e, need);
-        if ((isg || (ise && e < need)) && pos >= p0 && pos < p1) {
-          if (pos - p0 < EV_LIST)
-            s->list[pos - p0] = at + x;
-          else
-            oi[pos] = at + x;
-        }
+        const int slot = g + min(e, need) - p0;
+        const bool take = isg || (ise && e < need);
+        if (take && (unsigned)slot < held) s->list[slot] = at + x;
+        if (p1 - p0 > EV_LIST && take && slot >= EV_LIST && slot < p1 - p0)
+          oi[p0 + slot] = at + x;
         g += isg;
         e += ise;
       }
@@ -333,14 +343,19 @@ cudaError_t launch_evict(const EvictArgs& a, int dtype, cudaStream_t st) {
   const long long pairs = (long long)a.src.B * a.src.Hkv;
   const int S = (int)std::max<long long>(
       1, std::min<long long>(sm_count() / pairs, ceil_div(a.keep, 32)));
-  const cudaError_t e = set_smem_limit((const void*)k_evict, sizeof(EvSmem));
-  if (e != cudaSuccess) return e;
   const int vec = (uintptr_t)a.scores % 16 == 0 && a.score_stride % 4 == 0;
-  // keys of a thread: as few as hold the longest sequence, whole vectors from four on
-  int E = std::min(EV_EACH, ceil_div(a.src.cap, EV_THREADS));
-  if (E >= 4) E = ceil_div(E, 4) * 4;
-  return launch_k(k_evict, dim3(S, a.src.Hkv, a.src.B), dim3(EV_THREADS), sizeof(EvSmem), st, 1, a,
-                  esize, (int)(vec && E >= 4), E);
+  auto go = [&](auto kernel) {
+    const cudaError_t e = set_smem_limit((const void*)kernel, sizeof(EvSmem));
+    if (e != cudaSuccess) return e;
+    return launch_k(kernel, dim3(S, a.src.Hkv, a.src.B), dim3(EV_THREADS), sizeof(EvSmem), st, 1,
+                    a, esize, vec);
+  };
+  // keys of a thread: as few as hold the longest sequence
+  const int each = ceil_div(a.src.cap, EV_THREADS);
+  return each <= 2   ? go(k_evict<2>)
+         : each <= 4 ? go(k_evict<4>)
+         : each <= 8 ? go(k_evict<8>)
+                     : go(k_evict<16>);
 }
 
 }  // namespace gmc
