@@ -14,7 +14,8 @@
 //
 // What a CTA holds of a pair that others share is left as a part in the workspace, and a
 // second kernel joins the parts of every query head in the order of the row and adds the
-// scores.  (Joined by the CTA that is last instead, one launch took 18.4 us for one
+// scores.  Where the sequences are short a CTA takes a pair, whatever its length, and
+// nothing is left to join.  (Joined by the CTA that is last instead, one launch took 18.4 us for one
 // sequence of 322 keys where the two take 8.4: a count, a fence and the joining one after
 // another on one SM.)
 #include <algorithm>
@@ -249,6 +250,7 @@ __device__ __forceinline__ float* logits_of(const DecodeArgs& a, const Walk& w) 
 // nothing that shows.
 template <int DP> struct HeadsBf16 {
   static constexpr int HM = 16, EXTRA = 0;  // shared memory of its own, a warp
+  static constexpr int CTAS = 0;  // an SM, for the registers: left to the compiler
   typedef __nv_bfloat16 T;
   uint32_t qf[DP / 16][4];
   float o[DP / 8][4], m[2], l[2];
@@ -391,6 +393,8 @@ template <int DP> struct HeadsBf16 {
 // for the products with q, and 4 columns of the output (or 2 x 4) for those with v.
 template <int DP, int HM_> struct HeadsF32 {
   static constexpr int HM = HM_, EXTRA = (HM * DP + DT * HM) * 4;
+  static constexpr int CTAS = 1;  // an SM: all registers (16 sequences of 4,000 keys, 7
+                                  // heads a key head: 77 us, 93 with 168 a thread)
   typedef float T;
   static constexpr int ROWB = DP * 4, P = DP / 4;
   static constexpr int NC = P >= 32 ? P / 32 : 1;  // output pieces of a lane
@@ -613,38 +617,62 @@ template <class H, int DP, int W, int NST> constexpr size_t decode_smem() {
                       H::HM * sizeof(float2));
 }
 
-template <class H, int DP, int W, int NST>
-__global__ void __launch_bounds__(W * 32) k_decode(DecodeArgs a) {
+// OWN: a CTA takes a whole pair, and no other.
+template <class H, int DP, int W, int NST, bool OWN>
+__global__ void __launch_bounds__(W * 32, H::CTAS) k_decode(DecodeArgs a) {
   typedef typename H::T T;
   typedef Ring<DP * sizeof(T), NST> R;
   constexpr int HM = H::HM, ES = sizeof(T);
   static_assert(NST * R::STAGE >= HM * DP * 4, "a warp's ring holds its output rows");
   extern __shared__ __align__(512) char smem[];
+  __shared__ float2 fin[OWN ? 16 : 1];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   char* extra = smem + W * NST * R::STAGE + warp * H::EXTRA;
   float2* ml = reinterpret_cast<float2*>(smem + W * (NST * R::STAGE + H::EXTRA));  // [W][HM]
   grid_dep_wait();
   grid_dep_launch();  // not before: k_decode_join reads the lengths ahead of its own wait
-  const TurnRow turns(a);
-  const int cta = W * turns.per, at = turns.all / cta < (int)blockIdx.x ? turns.all
-                                                                      : (int)blockIdx.x * cta;
-  const int count = min(cta, turns.all - at);  // the CTA's turns
-  if (count <= 0) return;
   Walk w;
-  turns.find(a, at, &w);
-  const bool one = w.t + count <= w.turns;  // all of one pair
-  const int pair0 = w.b * a.c.Hkv + w.h;
-  const bool whole = one && count == w.turns;
-  // this warp's turns: u, u + step, .. below end
-  int u = at + warp, end = at + count, step = W;
-  if (one) {
-    w.t += warp;
+  int at, count, u, end, step = W;  // this warp's turns: u, u + step, .. below end
+  bool one, whole;                  // all of the CTA's are of one pair; all the pair's
+  if constexpr (OWN) {
+    w.b = blockIdx.x / a.c.Hkv;
+    w.h = blockIdx.x - w.b * a.c.Hkv;
+    w.t = 0;
+    w.load(a);
+    at = 0;
+    count = w.turns;
+    one = whole = true;
+    if (count == 0) {  // it sees nothing
+      for (int x = tid; x < a.heads * (DP / 4); x += W * 32) {
+        const int g = x / (DP / 4), y = (x - g * (DP / 4)) * 4;
+        write_head<T>(a, w.b, w.h, g, y, make_float4(0.f, 0.f, 0.f, 0.f), 0.f);
+        if (y == 0) write_lse(a, w.b, w.h, g, 0.f, 0.f);
+      }
+      return;
+    }
+    w.t = u = warp;
+    end = count;
   } else {
-    u = at + warp * turns.per;
-    end = min(end, u + turns.per);
-    step = 1;
-    if (u < end) turns.find(a, u, &w);
+    const TurnRow turns(a);
+    const int cta = W * turns.per;
+    at = turns.all / cta < (int)blockIdx.x ? turns.all : (int)blockIdx.x * cta;
+    count = min(cta, turns.all - at);
+    if (count <= 0) return;
+    turns.find(a, at, &w);
+    one = w.t + count <= w.turns;
+    whole = one && count == w.turns;
+    u = at + warp;
+    end = at + count;
+    if (one) {
+      w.t += warp;
+    } else {
+      u = at + warp * turns.per;
+      end = min(end, u + turns.per);
+      step = 1;
+      if (u < end) turns.find(a, u, &w);
+    }
   }
+  const int pair0 = w.b * a.c.Hkv + w.h;
   const int b0 = w.b, h0 = w.h;
   if (u < end) {
     H heads;
@@ -723,7 +751,16 @@ __global__ void __launch_bounds__(W * 32) k_decode(DecodeArgs a) {
     } else {
       *reinterpret_cast<float4*>(a.part + (part * a.heads + g) * DP + y) = o;
     }
-    if (y == 0) a.ml[part * a.heads + g] = make_float2(M, L);
+    if (y == 0) {
+      if constexpr (OWN)
+        fin[g] = final_ml(base, L);
+      else
+        a.ml[part * a.heads + g] = make_float2(M, L);
+    }
+  }
+  if (OWN && a.scores) {
+    __syncthreads();
+    add_scores(a, w, fin, tid, W * 32);
   }
 }
 
@@ -861,18 +898,28 @@ DecodeWs decode_carve(const KV& c, int dtype, int H) {
 }
 
 template <class H, int DP, int W, int NST>
-cudaError_t decode_launch(DecodeArgs a, cudaStream_t st) {
+cudaError_t decode_launch(DecodeArgs a, cudaStream_t st, int* launches) {
   static_assert(W <= D_WARPS, "the workspace holds a part a warp");
   constexpr size_t smem = decode_smem<H, DP, W, NST>();
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");
-  cudaError_t e = set_smem_limit((const void*)k_decode<H, DP, W, NST>, smem);
-  if (e != cudaSuccess) return e;
   const int ctas = sm_count();
+  const int pairs = a.c.B * a.c.Hkv;
+  // A CTA a pair where that is a few turns a warp: no parts, no second launch.  32 sequences
+  // of 512 keys and 4 key heads: 10.1 us, in stretches 11.3; with scores 12.6 and 14.7.  A
+  // single sequence of 322 takes 9.0, in stretches 8.3, but its call 9.1 instead of 10.4:
+  // the second launch is what the host takes time for; of 768 keys 14.0 and 8.3.
+  const int most = ceil_div(a.c.cap, W * DT);
+  const bool own = pairs <= ctas && most <= (2 * pairs >= ctas ? 6 : 3);
   a.warps = ctas * W;
-  if ((e = launch_k(k_decode<H, DP, W, NST>, dim3(ctas), dim3(W * 32), smem, st, 1, a)) !=
+  auto kernel = own ? k_decode<H, DP, W, NST, true> : k_decode<H, DP, W, NST, false>;
+  cudaError_t e = set_smem_limit((const void*)kernel, smem);
+  if (e != cudaSuccess) return e;
+  if ((e = launch_k(kernel, dim3(own ? pairs : ctas), dim3(W * 32), smem, st, 1, a)) !=
       cudaSuccess)
     return e;
-  const int pairs = a.c.B * a.c.Hkv, out_blocks = ceil_div(pairs * a.heads, JN_WARPS);
+  ++*launches;
+  if (own) return cudaSuccess;
+  const int out_blocks = ceil_div(pairs * a.heads, JN_WARPS);
   int blocks = 0;  // of a pair's scores
   if (a.scores) {
     long long most = a.c.cap;
@@ -882,15 +929,16 @@ cudaError_t decode_launch(DecodeArgs a, cudaStream_t st) {
     blocks = (int)std::min<long long>((most + JN_THREADS - 1) / JN_THREADS,
                                       std::max(1, 2 * ctas / pairs));
   }
+  ++*launches;
   return launch_k(k_decode_join<typename H::T>, dim3(out_blocks + pairs * blocks),
                   dim3(JN_THREADS), 0, st, 1, a, W, DP, out_blocks, std::max(blocks, 1));
 }
 template <int DP, int W, int NST>
-cudaError_t decode_f32(int heads, const DecodeArgs& a, cudaStream_t st) {
-  return heads == 1   ? decode_launch<HeadsF32<DP, 1>, DP, W, NST>(a, st)
-         : heads == 2 ? decode_launch<HeadsF32<DP, 2>, DP, W, NST>(a, st)
-         : heads <= 4 ? decode_launch<HeadsF32<DP, 4>, DP, W, NST>(a, st)
-                      : decode_launch<HeadsF32<DP, 8>, DP, W, NST>(a, st);
+cudaError_t decode_f32(int heads, const DecodeArgs& a, cudaStream_t st, int* launches) {
+  return heads == 1   ? decode_launch<HeadsF32<DP, 1>, DP, W, NST>(a, st, launches)
+         : heads == 2 ? decode_launch<HeadsF32<DP, 2>, DP, W, NST>(a, st, launches)
+         : heads <= 4 ? decode_launch<HeadsF32<DP, 4>, DP, W, NST>(a, st, launches)
+                      : decode_launch<HeadsF32<DP, 8>, DP, W, NST>(a, st, launches);
 }
 
 }  // namespace
@@ -922,15 +970,14 @@ cudaError_t launch_decode(DecodeArgs a, int dtype, void* ws, cudaStream_t st, in
     if (a.h0 > 0) a.scores = a.scores ? a.out_scores : nullptr;  // on the launch before's
     cudaError_t e;
     if (dtype == GMC_BF16)
-      e = dp == 64    ? decode_launch<HeadsBf16<64>, 64, 8, 4>(a, st)
-          : dp == 128 ? decode_launch<HeadsBf16<128>, 128, 8, 3>(a, st)
-                      : decode_launch<HeadsBf16<256>, 256, 4, 3>(a, st);
+      e = dp == 64    ? decode_launch<HeadsBf16<64>, 64, 8, 4>(a, st, launches)
+          : dp == 128 ? decode_launch<HeadsBf16<128>, 128, 8, 3>(a, st, launches)
+                      : decode_launch<HeadsBf16<256>, 256, 4, 3>(a, st, launches);
     else
-      e = dp == 64    ? decode_f32<64, 8, 3>(hm, a, st)
-          : dp == 128 ? decode_f32<128, 4, 3>(hm, a, st)
-                      : decode_f32<256, 2, 3>(hm, a, st);
+      e = dp == 64    ? decode_f32<64, 8, 3>(hm, a, st, launches)
+          : dp == 128 ? decode_f32<128, 4, 3>(hm, a, st, launches)
+                      : decode_f32<256, 2, 3>(hm, a, st, launches);
     if (e != cudaSuccess) return e;
-    *launches += 2;
   }
   return cudaSuccess;
 }
