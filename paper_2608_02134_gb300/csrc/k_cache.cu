@@ -21,16 +21,17 @@ __global__ void __launch_bounds__(AP_THREADS)
   grid_dep_launch();
   grid_dep_wait();
   const int b = blockIdx.y, t0 = blockIdx.x * tile;
+  // the length and the offsets on their way together
+  const int len = __ldcg(c.lens + b);
   const NewRows nr = new_rows(offsets, b, rows, T, c.status);
   const int nt = min(tile, nr.T - t0);
   if (nt <= 0) return;
-  const int first = kv_len(c, b) - nr.T + t0;
+  const int first = kv_clamp(c, len) - nr.T + t0;
   if ((int)threadIdx.x < nt) {
     const int j = first + (int)threadIdx.x;
     if (j < 0) set_status(c.status, CACHE_BAD);
     at[threadIdx.x] = j < 0 ? -1 : kv_row(c, b, 0, j);
   }
-  __syncthreads();
   const int hc = c.d * esize / 16;  // 16-byte pieces of a head's row
   const int rc = hc * c.Hkv;
   const char *ks, *vs;
@@ -43,7 +44,8 @@ __global__ void __launch_bounds__(AP_THREADS)
   }
   const int total = nt * rc;
   constexpr int U = 4;
-  for (int x0 = threadIdx.x; x0 < total; x0 += AP_THREADS * U) {
+  bool looked = false;
+  for (int x0 = threadIdx.x;; x0 += AP_THREADS * U) {
     int4 kv[U], vv[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -53,6 +55,9 @@ __global__ void __launch_bounds__(AP_THREADS)
         vv[u] = __ldcs((const int4*)vs + x);
       }
     }
+    if (!looked) __syncthreads();  // the first rows load while their places are looked up
+    looked = true;
+    if (x0 >= total) break;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int x = x0 + u * AP_THREADS;
