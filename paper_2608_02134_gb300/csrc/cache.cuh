@@ -40,14 +40,23 @@ __device__ __forceinline__ int kv_len(const KV& c, int b) {
 
 // Element offset of token j's row of key head h (the same in both pools), or -1
 // where the page table names a page outside the pool.
-__device__ __forceinline__ long long kv_row(const KV& c, int b, int h, int j) {
-  const unsigned p = (unsigned)j / (unsigned)c.ps, s = (unsigned)j - p * (unsigned)c.ps;
-  const int page = c.table[(long long)b * c.max_pages + p];
+struct Slot {  // its page as the table has it, and the slot in it
+  int page, slot;
+};
+__device__ __forceinline__ Slot kv_slot(const KV& c, int b, int j) {
+  const unsigned p = (unsigned)j / (unsigned)c.ps;
+  return {c.table[(long long)b * c.max_pages + p], (int)((unsigned)j - p * (unsigned)c.ps)};
+}
+__device__ __forceinline__ long long kv_row(const KV& c, int h, const Slot& at) {
+  const int page = at.page;
   if ((unsigned)page >= (unsigned)c.num_pages) {
     set_status(c.status, CACHE_BAD);
     return -1;
   }
-  return page * c.page_stride + h * c.head_stride + s * c.slot_stride;
+  return page * c.page_stride + h * c.head_stride + at.slot * c.slot_stride;
+}
+__device__ __forceinline__ long long kv_row(const KV& c, int b, int h, int j) {
+  return kv_row(c, h, kv_slot(c, b, j));
 }
 
 // New rows of a sequence: rows [off, off + T) of the packed input.

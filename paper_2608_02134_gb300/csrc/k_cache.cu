@@ -288,10 +288,12 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
     const int nr = min(EV_THREADS, p1 - q0);
     if (tid < nr) {
       const int q = q0 + tid, j = q - p0 < EV_LIST ? s->list[q - p0] : oi[q];
+      const Slot from = kv_slot(a.src, b, j), to = kv_slot(a.dst, b, q);  // together
+      const float score = sc[j];
+      const long long so = kv_row(a.src, h, from);
+      const long long dto = kv_row(a.dst, h, to);
       oi[q] = j;
-      if (os) os[q] = sc[j];
-      const long long so = kv_row(a.src, b, h, j);
-      const long long dto = kv_row(a.dst, b, h, q);
+      if (os) os[q] = score;
       s->src[tid] = so < 0 || dto < 0 ? -1 : so * esize;
       s->dst[tid] = dto * esize;
     }
