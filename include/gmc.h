@@ -552,7 +552,9 @@ typedef struct gmc_kv_cache {
  * head h / (H / Hkv).  Products accumulate in fp32, softmax statistics are
  * fp32; with a bf16 cache gmc_attend may round the weights to bf16 for their
  * product with v (gmc_decode does not).  Keys and values that a query does not
- * see do not reach its output, whatever they hold.
+ * see do not reach its output, whatever they hold, and pages of which no query
+ * of the call sees a key are not looked up: a program that gives back the pages
+ * behind its window may leave anything in the table.
  */
 typedef struct gmc_attn {
   int H;       /* query heads, a multiple of Hkv, H / Hkv <= 128 */
