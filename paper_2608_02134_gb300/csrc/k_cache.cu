@@ -1,6 +1,7 @@
 // The key-value cache's own kernels: new rows written to their pages, and the
 // best-scored rows of a sequence moved to fresh pages.
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "cache.cuh"
@@ -329,13 +330,17 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
 }  // namespace
 
 int sm_count() {
+  static std::atomic<int> known[64];  // by device; a call asks several times
   int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-    cudaGetLastError();
-    return 152;
+  if (cudaGetDevice(&dev) == cudaSuccess) {
+    if (dev >= 0 && dev < 64 && (sms = known[dev].load(std::memory_order_relaxed)) > 0) return sms;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) {
+      if (dev >= 0 && dev < 64) known[dev].store(sms, std::memory_order_relaxed);
+      return sms;
+    }
   }
-  return sms;
+  cudaGetLastError();
+  return 152;
 }
 
 cudaError_t launch_cache_append(const KV& c, int dtype, const void* k_new, const void* v_new,

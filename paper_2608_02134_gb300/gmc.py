@@ -472,6 +472,8 @@ def launch_count() -> int:
 # The key-value cache after the boundary (include/gmc.h, gmc_kv_cache)
 # ---------------------------------------------------------------------------
 _DTYPES = {torch.float32: GMC_F32, torch.bfloat16: GMC_BF16}
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 class KVCache:
@@ -479,7 +481,8 @@ class KVCache:
     unit-stride rows, the same for both: a permuted view of [pages, page_size, Hkv, d]
     pools will do), page_table int32 [B, max_pages], lens int32 [B], on the device.
     max_len bounds the lengths (0: the table's room); status: an int32 device word that
-    calls set STATUS_CACHE in, or None.  Holds the tensors; reads nothing."""
+    calls set STATUS_CACHE in, or None.  Holds the tensors; reads nothing.  Operands,
+    workspaces and streams are of the cache's device, which has to be the current one."""
 
     def __init__(self, k, v, page_table, lens, max_len=0, status=None):
         if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1 \
@@ -490,14 +493,16 @@ class KVCache:
                 or lens.dtype != torch.int32 or lens.numel() != page_table.shape[0] \
                 or not page_table.is_contiguous() or not lens.is_contiguous():
             raise GMCError("cache: page_table int32 [B, max_pages] and lens int32 [B], dense")
-        if status is not None and status.element_size() != 4:
+        if status is not None and (status.element_size() != 4 or status.numel() < 1):
             raise GMCError("cache: status is one 32-bit device word")
-        if any(not t.is_cuda for t in (k, v, page_table, lens)):
-            raise GMCError("cache: every tensor lies on the device")
+        device = k.get_device()  # -1: the host
+        if device < 0 or any(t.get_device() != device for t in (v, page_table, lens)) \
+                or (status is not None and status.get_device() != device):
+            raise GMCError("cache: every tensor lies on one device")
         self.k, self.v, self.page_table, self.lens, self.status = k, v, page_table, lens, status
         self.B, self.max_pages = page_table.shape
         self.num_pages, self.Hkv, self.page_size, self.d = k.shape
-        self.max_len, self.dtype, self.device_index = max_len, k.dtype, k.get_device()
+        self.max_len, self.dtype, self.device_index = max_len, k.dtype, device
         self.struct = CacheStruct(
             self.B, self.Hkv, self.d, _DTYPES[k.dtype], self.page_size, self.num_pages,
             self.max_pages, max_len, k.stride(0), k.stride(1), k.stride(2), k.data_ptr(),
@@ -509,12 +514,12 @@ class KVCache:
         self._attn = {}                             # gmc_attn of dense queries and outputs
 
     def attn(self, q, out, window, sinks, scale):
-        """gmc_attn of these queries and outputs, and their head count."""
-        shape = q.shape
+        """gmc_attn of these queries and outputs, their head count and their rows."""
+        shape, device = q.shape, self.device_index
         if len(shape) != 3 or shape != out.shape or q.dtype != self.dtype \
-                or out.dtype != self.dtype or shape[2] != self.d or not q.is_cuda \
-                or not out.is_cuda:
-            raise GMCError("queries and outputs: [rows, H, d] of the cache's type")
+                or out.dtype != self.dtype or shape[2] != self.d \
+                or q.get_device() != device or out.get_device() != device:
+            raise GMCError("queries and outputs: [rows, H, d] of the cache's type, on its device")
         H = shape[1]
         if q.is_contiguous() and out.is_contiguous():
             key = (H, window, sinks, scale)
@@ -522,7 +527,7 @@ class KVCache:
             if a is None:
                 a = ctypes.byref(Attn(H, window, sinks, scale or 0.0, 0, 0, 0, 0))
                 self._attn[key] = a
-            return a, H
+            return a, H, shape[0]
         if q.stride(2) != 1 or out.stride(2) != 1 or \
                 (shape[0] > 1 and 0 in (q.stride(0), out.stride(0))) or \
                 (H > 1 and 0 in (q.stride(1), out.stride(1))):
@@ -530,13 +535,20 @@ class KVCache:
         # the stride of a dimension of one is anything: none is passed
         rs = [t.stride(0) if shape[0] > 1 else H * self.d for t in (q, out)]
         hs = [t.stride(1) if H > 1 else self.d for t in (q, out)]
-        return ctypes.byref(Attn(H, window, sinks, scale or 0.0, rs[0], hs[0], rs[1], hs[1])), H
+        a = Attn(H, window, sinks, scale or 0.0, rs[0], hs[0], rs[1], hs[1])
+        return ctypes.byref(a), H, shape[0]
 
     def stream(self, stream):
-        """Handle of `stream`, or of the current stream of the cache's device."""
-        if stream is not None:
-            return stream.cuda_stream
-        return torch._C._cuda_getCurrentRawStream(self.device_index)
+        """Handle of `stream`, or of the current stream.  A launch goes to the current device:
+        the library sizes its grids by it, and the default stream's handle is every device's."""
+        device = self.device_index
+        if _current_device() != device:
+            raise GMCError("the cache's device is not the current device")
+        if stream is None:
+            return _current_stream(device)
+        if stream.device_index != device:
+            raise GMCError("the stream is not of the cache's device")
+        return stream.cuda_stream
 
     def workspace(self, nbytes, stream):
         """A workspace for one call on `stream`, from that stream's memory."""
@@ -546,27 +558,31 @@ class KVCache:
             return alloc_workspace(nbytes, self.k.device)
 
 
-def _addr(t):
-    return None if t is None else t.data_ptr()
+def _int32_at(cache, t, n, what):
+    """The address of an operand (None: NULL) of n dense elements on the cache's device."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n \
+            or t.get_device() != cache.device_index:
+        raise GMCError(what + ", on the cache's device")
+    return t.data_ptr()
 
 
-def _check_int32(t, n, what):
-    if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n
-                          or not t.is_cuda):
-        raise GMCError(what)
-
-
-def _check_f32(t, n, what):
-    if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n
-                          or not t.is_cuda):
-        raise GMCError(what)
+def _f32_at(cache, t, n, what):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n \
+            or t.get_device() != cache.device_index:
+        raise GMCError(what + ", on the cache's device")
+    return t.data_ptr()
 
 
 def _check_scores(cache, t):
     shape = t.shape
     if t.dtype != torch.float32 or len(shape) != 3 or shape[0] != cache.B \
-            or shape[1] != cache.Hkv or not t.is_contiguous() or not t.is_cuda:
-        raise GMCError("scores: dense fp32 [B, Hkv, places] on the device")
+            or shape[1] != cache.Hkv or not t.is_contiguous() \
+            or t.get_device() != cache.device_index:
+        raise GMCError("scores: dense fp32 [B, Hkv, places] on the cache's device")
     return shape
 
 
@@ -577,14 +593,17 @@ def cache_append(cache: KVCache, k_new, v_new, T, offsets=None, stream=None):
     shape = k_new.shape
     rows = shape[0] if v_new is not None else shape[0] // 2
     if shape[1:] != cache._row_shape or k_new.dtype != cache.dtype \
-            or not k_new.is_contiguous() or not k_new.is_cuda:
-        raise GMCError("new rows: dense [rows, Hkv, d] of the cache's type")
+            or not k_new.is_contiguous() or k_new.get_device() != cache.device_index:
+        raise GMCError("new rows: dense [rows, Hkv, d] of the cache's type, on its device")
     if v_new is not None and (v_new.shape != shape or v_new.dtype != cache.dtype
-                              or not v_new.is_contiguous() or not v_new.is_cuda):
-        raise GMCError("new rows: as many values as keys")
-    _check_int32(offsets, cache.B + 1, "offsets: dense int32 [B + 1]")
-    rc = lib().gmc_cache_append(cache.ref, k_new.data_ptr(), _addr(v_new), _addr(offsets), rows, T,
-                                cache.stream(stream))
+                              or not v_new.is_contiguous()
+                              or v_new.get_device() != cache.device_index):
+        raise GMCError("new rows: as many values as keys, alike")
+    rc = lib().gmc_cache_append(cache.ref, k_new.data_ptr(),
+                                None if v_new is None else v_new.data_ptr(),
+                                _int32_at(cache, offsets, cache.B + 1,
+                                          "offsets: dense int32 [B + 1]"),
+                                rows, T, cache.stream(stream))
     if rc:
         _check(rc)
 
@@ -598,15 +617,15 @@ def attend(cache: KVCache, q, out, T, q_offsets=None, window=0, sinks=0, scale=N
     """gmc_attend: causal attention of the new tokens q [rows, H, d] into out (and lse fp32
     [rows, H]); T new tokens a sequence (the most of a ragged call, whose q_offsets is
     int32 [B+1]).  scale None: 1 / sqrt(d)."""
-    a, H = cache.attn(q, out, window, sinks, scale)
-    rows = q.shape[0]
-    _check_int32(q_offsets, cache.B + 1, "q_offsets: dense int32 [B + 1]")
-    _check_f32(lse, rows * H, "lse: dense fp32 [rows, H]")
+    a, H, rows = cache.attn(q, out, window, sinks, scale)
+    offsets = _int32_at(cache, q_offsets, cache.B + 1, "q_offsets: dense int32 [B + 1]")
+    lse_at = _f32_at(cache, lse, rows * H, "lse: dense fp32 [rows, H]")
     if workspace is None:
         workspace = cache.workspace(attend_workspace_size(cache, H, T), stream)
-    rc = lib().gmc_attend(cache.ref, a, q.data_ptr(), _addr(q_offsets), rows, T, out.data_ptr(),
-                          _addr(lse), workspace.data_ptr(), workspace.numel(),
-                          cache.stream(stream))
+    elif workspace.get_device() != cache.device_index or not workspace.is_contiguous():
+        raise GMCError("workspace: dense, on the cache's device")
+    rc = lib().gmc_attend(cache.ref, a, q.data_ptr(), offsets, rows, T, out.data_ptr(), lse_at,
+                          workspace.data_ptr(), workspace.numel(), cache.stream(stream))
     if rc:
         _check(rc)
 
@@ -621,26 +640,40 @@ def decode(cache: KVCache, q, out, k_new=None, v_new=None, window=0, sinks=0, sc
     k_new, v_new [B, Hkv, d]: appended at place lens - 1 on the way.  scores, out_scores
     fp32 [B, Hkv, places]: out_scores = scores + the weight every key received (the
     same tensor will do)."""
-    a, H = cache.attn(q, out, window, sinks, scale)
-    if q.shape[0] != cache.B:
+    a, H, rows = cache.attn(q, out, window, sinks, scale)
+    if rows != cache.B:
         raise GMCError("decode: one query row a sequence")
-    for t in (k_new, v_new):
-        if t is not None and (t.shape != cache._new_shape or t.dtype != cache.dtype
-                              or not t.is_contiguous() or not t.is_cuda):
-            raise GMCError("new rows: dense [B, Hkv, d] of the cache's type")
-    _check_f32(lse, cache.B * H, "lse: dense fp32 [B, H]")
-    places = 0
+    shape, dtype, device = cache._new_shape, cache.dtype, cache.device_index
+    k_at = v_at = None
+    if k_new is not None:
+        if k_new.shape != shape or k_new.dtype != dtype or not k_new.is_contiguous() \
+                or k_new.get_device() != device:
+            raise GMCError("new rows: dense [B, Hkv, d] of the cache's type, on its device")
+        k_at = k_new.data_ptr()
+    if v_new is not None:
+        if v_new.shape != shape or v_new.dtype != dtype or not v_new.is_contiguous() \
+                or v_new.get_device() != device:
+            raise GMCError("new rows: dense [B, Hkv, d] of the cache's type, on its device")
+        v_at = v_new.data_ptr()
+    lse_at = _f32_at(cache, lse, rows * H, "lse: dense fp32 [B, H]")
+    places, scores_at = 0, None
+    out_at = None if out_scores is None else out_scores.data_ptr()
     if scores is not None:
+        scores_at = scores.data_ptr()
         shape = _check_scores(cache, scores)
-        if out_scores is not scores and (out_scores is None
-                                         or _check_scores(cache, out_scores) != shape):
+        if out_scores is not scores and (
+                out_scores is None or out_scores.shape != shape
+                or out_scores.dtype != torch.float32 or not out_scores.is_contiguous()
+                or out_scores.get_device() != device):
             raise GMCError("decode: scores and out_scores alike")
         places = shape[2]
     if workspace is None:
         workspace = cache.workspace(decode_workspace_size(cache, H), stream)
-    rc = lib().gmc_decode(cache.ref, a, q.data_ptr(), _addr(k_new), _addr(v_new), out.data_ptr(),
-                          _addr(lse), _addr(scores), _addr(out_scores), places,
-                          workspace.data_ptr(), workspace.numel(), cache.stream(stream))
+    elif workspace.get_device() != cache.device_index or not workspace.is_contiguous():
+        raise GMCError("workspace: dense, on the cache's device")
+    rc = lib().gmc_decode(cache.ref, a, q.data_ptr(), k_at, v_at, out.data_ptr(), lse_at,
+                          scores_at, out_at, places, workspace.data_ptr(), workspace.numel(),
+                          cache.stream(stream))
     if rc:
         _check(rc)
 
@@ -654,14 +687,19 @@ def evict(src: KVCache, dst: KVCache, scores, keep, out_idx, out_scores=None, si
     """gmc_evict: every key head keeps its `keep` best-scored rows (the first `sinks` and
     the last `recent` always), moved to the pages of dst in ascending order; out_idx
     int32 [B, Hkv, keep], out_scores fp32 [B, Hkv, keep] or None.  Writes dst.lens."""
+    if dst.device_index != src.device_index:
+        raise GMCError("evict: caches of one device")
     _check_scores(src, scores)
-    _check_int32(out_idx, src.B * src.Hkv * keep, "out_idx: dense int32 [B, Hkv, keep]")
-    _check_f32(out_scores, src.B * src.Hkv * keep, "out_scores: dense fp32 [B, Hkv, keep]")
+    kept = src.B * src.Hkv * keep
+    idx_at = _int32_at(src, out_idx, kept, "out_idx: dense int32 [B, Hkv, keep]")
+    out_at = _f32_at(src, out_scores, kept, "out_scores: dense fp32 [B, Hkv, keep]")
     if workspace is None:
         workspace = src.workspace(evict_workspace_size(src, keep), stream)
+    elif workspace.get_device() != src.device_index or not workspace.is_contiguous():
+        raise GMCError("workspace: dense, on the cache's device")
     rc = lib().gmc_evict(src.ref, dst.ref, scores.data_ptr(), scores.shape[2], keep, sinks, recent,
-                         out_idx.data_ptr(), _addr(out_scores), workspace.data_ptr(),
-                         workspace.numel(), src.stream(stream))
+                         idx_at, out_at, workspace.data_ptr(), workspace.numel(),
+                         src.stream(stream))
     if rc:
         _check(rc)
 
