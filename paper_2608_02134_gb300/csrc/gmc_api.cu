@@ -14,17 +14,22 @@ using namespace gmc;
 
 namespace gmc {
 
+constexpr int SMEM_DEVICES = 64;  // whose limits are remembered
+
 cudaError_t set_smem_limit(const void* func, size_t bytes) {
   static std::mutex mu;
-  static std::unordered_map<const void*, size_t> done;
+  // the attribute is set for the current device only
+  static std::unordered_map<const void*, size_t> done[SMEM_DEVICES];
   // the 48 KB default covers a kernel's static arrays too (33 KB at most: k_transport<float>)
   if (bytes <= 14 * 1024) return cudaSuccess;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
   std::lock_guard<std::mutex> lk(mu);
-  auto it = done.find(func);
-  if (it != done.end() && it->second >= bytes) return cudaSuccess;
-  cudaError_t e =
-      cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-  if (e == cudaSuccess) done[func] = bytes;
+  size_t* known = dev < SMEM_DEVICES ? &done[dev][func] : nullptr;
+  if (known && *known >= bytes) return cudaSuccess;
+  e = cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess && known) *known = bytes;
   return e;
 }
 

@@ -245,7 +245,7 @@ int check_problem(const gmc_problem* prob, int N, int T, int d, int D, int max_n
 
 namespace gmc {
 // Raise a kernel's dynamic shared-memory limit when a launch needs more than
-// the 48 KB default (idempotent; remembers the largest value set per kernel).
+// the 48 KB default (idempotent; remembers the largest value set per kernel and device).
 cudaError_t set_smem_limit(const void* func, size_t bytes);
 void count_launches(int n);  // adds to gmc_launch_count()
 }  // namespace gmc
