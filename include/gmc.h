@@ -572,7 +572,8 @@ typedef struct gmc_attn {
  *                 T_b key rows, then its T_b value rows, from row 2 * offsets[b] on
  *   offsets       DEVICE int32 [B+1], T_b = offsets[b+1] - offsets[b], 0 <= T_b <= T;
  *                 or NULL: every sequence has T new rows
- *   rows          rows of all sequences (offsets past it are out of range)
+ *   rows          rows of all sequences (offsets past it are out of range); 0: nothing
+ *                 is done, k_new and v_new may be NULL
  * One launch.  Rows whose place would lie before the sequence are dropped
  * (GMC_STATUS_CACHE).
  */
@@ -584,8 +585,8 @@ int gmc_cache_append(const gmc_kv_cache* cache, const void* k_new, const void* v
  * appended) over its cached keys, whole or through a window with sinks.
  *   q        [rows][H][d] (strides in attn), sequence after sequence as q_offsets says
  *   out      as q;  lse  fp32 [rows][H] or NULL
- * q_offsets, rows, T: as offsets, rows, T of gmc_cache_append; rows of no
- * sequence are left alone.  q and out 16-byte aligned, their strides multiples
+ * q_offsets, rows, T: as offsets, rows, T of gmc_cache_append (rows == 0: q, out
+ * and workspace may be NULL); rows of no sequence are left alone.  q and out 16-byte aligned, their strides multiples
  * of 16 bytes.  bf16 caches with d <= 128 and pages of a multiple of 8 slots run
  * on the tcgen05 tensor cores, others on the CUDA cores.  One launch, or two
  * where the key axis is split.

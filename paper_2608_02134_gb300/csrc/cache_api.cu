@@ -111,9 +111,8 @@ int gmc_cache_append(const gmc_kv_cache* cache, const void* k_new, const void* v
                      const int32_t* offsets, int rows, int T, gmc_stream_t stream) {
   int rc = check_cache(cache);
   if (rc == GMC_OK) rc = check_rows(cache, offsets, rows, T);
-  if (rc != GMC_OK) return rc;
+  if (rc != GMC_OK || rows == 0) return rc;  // no rows: their pointers may be NULL
   if (!k_new || !aligned(k_new, 16) || !aligned(v_new, 16)) return GMC_ERR_ARG;
-  if (rows == 0) return GMC_OK;
   rc = cuda_rc(launch_cache_append(view(cache), cache->dtype, k_new, v_new, offsets, rows, T,
                                    (cudaStream_t)stream));
   if (rc == GMC_OK) count_launches(1);
@@ -131,14 +130,13 @@ int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
   int rc = check_cache(cache);
   if (rc == GMC_OK) rc = check_attn(cache, attn);
   if (rc == GMC_OK) rc = check_rows(cache, q_offsets, rows, T);
-  if (rc != GMC_OK) return rc;
+  if (rc != GMC_OK || rows == 0) return rc;  // no rows: their pointers may be NULL
   if (!q || !out || !workspace || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) ||
       !aligned(workspace, 256))
     return GMC_ERR_ARG;
   AttnArgs a{};
   a.c = view(cache);
   if (ws_bytes < attend_workspace(a.c, cache->dtype, attn->H, T)) return GMC_ERR_WORKSPACE;
-  if (rows == 0) return GMC_OK;
   a.q = (const char*)q;
   a.out = (char*)out;
   a.lse = lse;
