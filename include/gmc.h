@@ -571,7 +571,8 @@ typedef struct gmc_attn {
  *                 k_new in the layout of gmc_compress's out_kv: sequence b's
  *                 T_b key rows, then its T_b value rows, from row 2 * offsets[b] on
  *   offsets       DEVICE int32 [B+1], T_b = offsets[b+1] - offsets[b], 0 <= T_b <= T;
- *                 or NULL: every sequence has T new rows
+ *                 or NULL: every sequence has T new rows (T at most 2^30:
+ *                 GMC_ERR_UNSUPPORTED beyond)
  *   rows          rows of all sequences (offsets past it are out of range); 0: nothing
  *                 is done, k_new and v_new may be NULL
  * One launch.  Rows whose place would lie before the sequence are dropped

@@ -16,6 +16,8 @@ int cuda_rc(cudaError_t e) {
   return GMC_ERR_CUDA;
 }
 
+constexpr int MAX_PLACES = 0x40000000;  // of a sequence, new ones too: tiles are counted in 32 bits
+
 int esize_of(int dtype) { return dtype == GMC_BF16 ? 2 : 4; }
 
 // The cache's shape alone (what the workspace sizes need).
@@ -25,7 +27,7 @@ int check_shape(const gmc_kv_cache* c) {
     return GMC_ERR_ARG;
   if (c->dtype != GMC_F32 && c->dtype != GMC_BF16) return GMC_ERR_ARG;
   // places are 32-bit; grids hold a sequence or a key head a block
-  if ((long long)c->page_size * c->max_pages > 0x40000000LL || c->B > 65535 || c->Hkv > 65535)
+  if ((long long)c->page_size * c->max_pages > MAX_PLACES || c->B > 65535 || c->Hkv > 65535)
     return GMC_ERR_UNSUPPORTED;
   if (c->max_len > c->page_size * c->max_pages) return GMC_ERR_ARG;
   // turns of 16 keys over all sequences and key heads are counted in 32 bits
@@ -89,6 +91,7 @@ int check_attn(const gmc_kv_cache* c, const gmc_attn* a) {
 // rows rows of new tokens, T a sequence at most
 int check_rows(const gmc_kv_cache* c, const int32_t* offsets, int rows, int T) {
   if (rows < 0 || T < 1 || !aligned(offsets, 4)) return GMC_ERR_ARG;
+  if (T > MAX_PLACES) return GMC_ERR_UNSUPPORTED;
   if (!offsets && (long long)c->B * T != rows) return GMC_ERR_ARG;
   return GMC_OK;
 }
@@ -120,7 +123,9 @@ int gmc_cache_append(const gmc_kv_cache* cache, const void* k_new, const void* v
 }
 
 size_t gmc_attend_workspace_size(const gmc_kv_cache* cache, int H, int T) {
-  if (check_shape(cache) != GMC_OK || check_heads(cache, H) != GMC_OK || T < 1) return 0;
+  if (check_shape(cache) != GMC_OK || check_heads(cache, H) != GMC_OK || T < 1 ||
+      T > MAX_PLACES)
+    return 0;
   return attend_workspace(view(cache), cache->dtype, H, T);
 }
 

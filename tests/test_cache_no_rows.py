@@ -25,3 +25,13 @@ def test_the_other_checks_stay(gmc):  # noqa: F811
     assert _append(gmc, _cache(gmc, d=0), rows=0, off=FAKE) == gmc.GMC_ERR_ARG
     assert _attend(gmc, _cache(gmc), _attn(gmc, H=30), rows=0, off=FAKE) == gmc.GMC_ERR_ARG
     assert _attend(gmc, _cache(gmc), a, rows=0) == gmc.GMC_ERR_ARG  # B * T rows without offsets
+
+
+@pytest.mark.parametrize("T", [2 ** 30 + 1, 2 ** 31 - 1])
+def test_more_rows_a_sequence_than_places_are_counted_in(gmc, T):  # noqa: F811
+    # the tiles of so many rows do not fit 32 bits
+    c, a = _cache(gmc), _attn(gmc)
+    assert _append(gmc, c, T=T, off=FAKE) == gmc.GMC_ERR_UNSUPPORTED
+    assert _attend(gmc, c, a, T=T, off=FAKE) == gmc.GMC_ERR_UNSUPPORTED
+    assert gmc.lib().gmc_attend_workspace_size(c, 28, T) == 0
+    assert gmc.lib().gmc_attend_workspace_size(c, 28, 2 ** 30) > 0
