@@ -91,7 +91,7 @@ struct Seen {
 __device__ __forceinline__ Seen seen_keys(int i0, int i1, int window, int sinks) {
   Seen s;
   s.b1 = i1 + 1 > 0 ? i1 + 1 : 0;
-  s.b0 = window > 0 && i0 - window + 1 > 0 ? i0 - window + 1 : 0;
+  s.b0 = window > 0 && i0 >= window ? i0 - window + 1 : 0;  // i0 may lie far below 0
   if (s.b0 > s.b1) s.b0 = s.b1;
   s.a = window > 0 && sinks < s.b0 ? sinks : s.b0;
   if (s.a == s.b0) {  // the sinks reach the window: one range

@@ -96,6 +96,9 @@ int check_rows(const gmc_kv_cache* c, const int32_t* offsets, int rows, int T) {
   return GMC_OK;
 }
 
+// A window of all places is none; a smaller one can be taken from a place in 32 bits.
+int window_of(const KV& c, const gmc_attn* at) { return at->window < c.cap ? at->window : 0; }
+
 void heads_of(const gmc_kv_cache* c, const gmc_attn* at, long long* q_row, long long* q_head,
               long long* o_row, long long* o_head, float* scale2) {
   *q_row = at->q_row_stride ? at->q_row_stride : (long long)at->H * c->d;
@@ -149,7 +152,7 @@ int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
   heads_of(cache, attn, &a.q_row, &a.q_head, &a.o_row, &a.o_head, &a.scale2);
   a.H = attn->H;
   a.G = attn->H / cache->Hkv;
-  a.window = attn->window;
+  a.window = window_of(a.c, attn);
   a.sinks = attn->sinks;
   a.rows = rows;
   a.T = T;
@@ -193,7 +196,7 @@ int gmc_decode(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q, c
   heads_of(cache, attn, &a.q_row, &a.q_head, &a.o_row, &a.o_head, &a.scale2);
   a.H = attn->H;
   a.G = attn->H / cache->Hkv;
-  a.window = attn->window;
+  a.window = window_of(a.c, attn);
   a.sinks = attn->sinks;
   int launches = 0;
   rc = cuda_rc(launch_decode(a, cache->dtype, workspace, (cudaStream_t)stream, &launches));

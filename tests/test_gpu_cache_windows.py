@@ -1,4 +1,5 @@
-"""Windows: pages that no query sees are not looked up."""
+"""Windows: pages that no query sees are not looked up, and a window as wide as integers go is
+none."""
 
 import pytest
 import torch
@@ -97,3 +98,22 @@ def test_a_page_that_is_seen_in_part_is_still_looked_at():
         _attend(c, 70, 3)  # the first new token sees places 623 and on: page 38 holds the last one
         torch.cuda.synchronize()
         assert int(c.status.item()) == gmc.STATUS_CACHE
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 12, 2 ** 30])
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f32", 64), ("f32", 256)])
+def test_attend_with_a_window_as_wide_as_integers_go(dtype, d, window):
+    # the first queries of the first sequence lie before it
+    c = _harness().Case([10, 300], 4, 2, d, dtype, 16, [20, 20])
+    out, lse = _attend(c, window, 2)
+    torch.cuda.synchronize()
+    assert int(c.status.item()) == 0
+    _check_attend(c, out, lse, 0, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_window_of_all_places_is_none(dtype):
+    c = _harness().Case([300, 40], 4, 2, 128, dtype, 16, [60, 40])
+    want = _attend(c)
+    got = _attend(c, 300, 2)
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
