@@ -562,8 +562,9 @@ __global__ void __launch_bounds__(t_threads<TILES>(), 3 - TILES)
   if (warp == ISSUE) tc::tmem_dealloc(tmem, 256 * TILES);
   if (ctl->abort) {
     if (tid == 0) set_status(a.c.status, GMC_STATUS_TIMEOUT);
-    if (warp == COPY) {  // copies in flight land before shared memory is given back
+    if (warp == COPY && issued > 0) {  // copies in flight land before shared memory is given back
       const long long end = clock64() + T_WAIT;
+      while (!tc::mbar_try_wait(&ctl->qfull, 0) && clock64() < end) {}
       for (int q = issued > NS ? issued - NS : 0; q < issued; ++q)
         while (!tc::mbar_try_wait(&ctl->full[q % NS], (q / NS) & 1) && clock64() < end) {}
     }
