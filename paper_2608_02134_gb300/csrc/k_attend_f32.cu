@@ -6,9 +6,11 @@
 // differences are exact), and of the nine products of two such sums the six down to
 // 2^-16 of the largest are taken, the small ones first:
 //     S = q0 k2 + q2 k0 + q1 k1 + q0 k1 + q1 k0 + q0 k0
-// What is left out is 2^-23 of |q| |k| at most.  Products are exact and are added in fp32
-// in tensor memory over one turn of keys; across turns the output is added up in registers
-// (the tensor cores' own adding cuts, and over thousands of keys that would show).
+// What is left out, q1 k2 + q2 k1 + q2 k2, is 2^-21 of |q| |k| at most (q1 reaches 2^-7 and
+// q2 2^-15 of q's power of two) and 2^-24.6 on average, of the product's sign.  Products are
+// exact and are added in fp32 in tensor memory over one turn of keys; across turns the output
+// is added up in registers (the tensor cores' own adding cuts, and over thousands of keys that
+// would show).
 //
 // A CTA takes a tile of up to 128 rows, a row being one query head of one token (the G
 // query heads of a key head and 128 / G consecutive tokens), and walks the seen keys 64
@@ -31,9 +33,9 @@
 // integer ones at half rate).
 //
 // Keys that a row does not see get the weight 0.  Slots outside the seen ranges are not
-// read; where a key or value is not finite (its parts would be NaN, and 0 x NaN would
-// reach rows that do not see it) the CTA computes its rows again one by one, each from
-// the keys that it sees.
+// read; where any key or value read is not finite, also one that every row sees (its parts
+// would be NaN, and 0 x NaN would reach rows that do not see it), the CTA computes its rows
+// again one by one, each from the keys that it sees.
 //
 // Every wait is bounded (about two seconds); on timeout GMC_STATUS_TIMEOUT is set in
 // the cache's status word, products in flight are drained and tensor memory is freed.
