@@ -550,8 +550,9 @@ typedef struct gmc_kv_cache {
  *   out = sum_j exp(x_j) v_j / sum_j exp(x_j),   lse = log sum_j exp(x_j);
  * a query that sees nothing gets out = 0, lse = -inf.  Query head h reads key
  * head h / (H / Hkv).  Products accumulate in fp32, softmax statistics are
- * fp32; with a bf16 cache gmc_attend may round the weights to bf16 for their
- * product with v (gmc_decode does not).  Keys and values that a query does not
+ * fp32; on bf16 caches with d <= 128 and pages of a multiple of 8 slots gmc_attend
+ * rounds the weights to bf16 for their product with v (its other forms and
+ * gmc_decode do not).  Keys and values that a query does not
  * see do not reach its output, whatever they hold, and pages of which no query
  * of the call sees a key are not looked up: a program that gives back the pages
  * behind its window may leave anything in the table.
@@ -587,10 +588,14 @@ int gmc_cache_append(const gmc_kv_cache* cache, const void* k_new, const void* v
  *   q        [rows][H][d] (strides in attn), sequence after sequence as q_offsets says
  *   out      as q;  lse  fp32 [rows][H] or NULL
  * q_offsets, rows, T: as offsets, rows, T of gmc_cache_append (rows == 0: q, out
- * and workspace may be NULL); rows of no sequence are left alone.  q and out 16-byte aligned, their strides multiples
- * of 16 bytes.  bf16 caches with d <= 128 and pages of a multiple of 8 slots run
- * on the tcgen05 tensor cores, others on the CUDA cores.  One launch, or two
- * where the key axis is split.
+ * and workspace may be NULL); rows of no sequence are left alone.  q and out
+ * 16-byte aligned, their strides multiples of 16 bytes; out does not overlap q.
+ * fp32 caches with d <= 128, and bf16 caches with d <= 128 and pages of a multiple
+ * of 8 slots, run on the tcgen05 tensor cores, the others on the CUDA cores.  The
+ * bf16 kernel takes whole pages into turns of 128 keys: pages of 8, 16, 32, 64 or a
+ * multiple of 128 slots fill them, others leave a part of each turn idle (48 slots
+ * a quarter).  One launch, or two where the key axis is split.  No score is added
+ * to: only gmc_decode does that.
  */
 size_t gmc_attend_workspace_size(const gmc_kv_cache* cache, int H, int T);
 int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
@@ -609,7 +614,10 @@ int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
  *               j < lens[b] (later entries are left alone); unseen keys receive
  *               nothing, and a key appended by this call starts from 0.  May be
  *               `scores` itself; both or neither are NULL.
- * Two launches (for every 16 query heads of a key head with bf16, 8 with fp32).
+ * out does not overlap q.  A sequence of no tokens gets out = 0 and lse = -inf, and
+ * nothing is appended to it.  One launch where max_len is short, two otherwise (for
+ * every 16 query heads of a key head with bf16, 8 with fp32).  The workspace has
+ * room for the logits of scores, with or without them.
  * A page's rows must lie within 64 GB (GMC_ERR_UNSUPPORTED).
  */
 size_t gmc_decode_workspace_size(const gmc_kv_cache* cache, int H);
@@ -621,9 +629,10 @@ int gmc_decode(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q, c
  * gmc_evict -- every key head of a sequence keeps the `keep` tokens with the
  * largest scores (all of them where it holds no more): the first `sinks` and
  * the last `recent` always, the others by score, equal scores by the lowest
- * place, a NaN below every number.  The kept rows go, in ascending order, to
- * places 0 .. of the sequence in `dst`, whose pages must not be among the
- * sequence's in `src`; dst->lens[b] = min(keep, lens[b]) is written.
+ * place, a NaN as -infinity.  The kept rows go, in ascending order, to places
+ * 0 .. of the sequence in `dst`, whose pages must not be among those that any
+ * sequence holds in `src` (all sequences are moved at once);
+ * dst->lens[b] = min(keep, lens[b]) is written.
  *   scores      fp32 [B][Hkv][score_stride]
  *   out_idx     int32 [B][Hkv][keep]: the places kept, -1 after the last
  *   out_scores  fp32 [B][Hkv][keep]: their scores, 0 after the last; may be NULL

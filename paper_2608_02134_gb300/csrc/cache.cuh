@@ -38,15 +38,16 @@ __device__ __forceinline__ int kv_len(const KV& c, int b) {
   return kv_clamp(c, __ldcg(c.lens + b));
 }
 
-// Element offset of token j's row of key head h (the same in both pools), or -1
-// where the page table names a page outside the pool.
-struct Slot {  // its page as the table has it, and the slot in it
+// Where token j lies: its page as the table has it, and the slot in it.
+struct Slot {
   int page, slot;
 };
 __device__ __forceinline__ Slot kv_slot(const KV& c, int b, int j) {
   const unsigned p = (unsigned)j / (unsigned)c.ps;
   return {c.table[(long long)b * c.max_pages + p], (int)((unsigned)j - p * (unsigned)c.ps)};
 }
+// Element offset of that place's row of key head h (the same in both pools), or -1 where the
+// table names a page outside the pool.
 __device__ __forceinline__ long long kv_row(const KV& c, int h, const Slot& at) {
   const int page = at.page;
   if ((unsigned)page >= (unsigned)c.num_pages) {
@@ -147,7 +148,7 @@ struct AttnArgs {
   long long q_row, q_head, o_row, o_head;  // elements
   int H, G, window, sinks, rows, T;
   float scale2;  // scale * log2(e): softmax in powers of two
-  // a long key axis split over CTAs: partial sums [split][B][T][H][d], maxima and sums
+  // a key axis split over CTAs: partial sums [split][B][T][H][d], maxima and sums
   int splits;
   float* part;
   float2* ml;  // [split][B][T][H]
@@ -161,7 +162,6 @@ cudaError_t launch_cache_append(const KV&, int dtype, const void* k_new, const v
                                 const int32_t* offsets, int rows, int T, cudaStream_t);
 
 size_t attend_workspace(const KV&, int dtype, int H, int T);
-// The join of a split key axis (AttnArgs::part, ml).
 void* tensor_map_encoder();  // cuTensorMapEncodeTiled, or NULL
 bool attend_tc_takes(const KV&, int dtype, int G);
 int attend_tc_splits(const KV&, int G, int T);
@@ -169,7 +169,7 @@ cudaError_t launch_attend_tc(const AttnArgs&, cudaStream_t);
 bool attend_f32_takes(const KV&, int dtype);
 int attend_f32_splits(const KV&, int G, int T);
 cudaError_t launch_attend_f32(const AttnArgs&, cudaStream_t);
-cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t);
+cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t);  // of part and ml
 cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t, int* launches);
 
 struct DecodeArgs {

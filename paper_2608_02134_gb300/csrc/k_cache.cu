@@ -99,9 +99,9 @@ struct EvSmem {
   int need;
 };
 
-// Larger score, larger key; -0 equals 0, a NaN is below every number's key.
+// Larger score, larger key; -0 equals 0, a NaN is as -infinity.
 __device__ __forceinline__ uint32_t score_key(float s) {
-  if (!(s == s)) return 0x007fffffu;  // as -infinity
+  if (!(s == s)) return 0x007fffffu;  // -infinity's
   const uint32_t u = __float_as_uint(s + 0.f);
   return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }

@@ -685,8 +685,9 @@ def evict_workspace_size(cache: KVCache, keep) -> int:
 def evict(src: KVCache, dst: KVCache, scores, keep, out_idx, out_scores=None, sinks=0, recent=0,
           workspace=None, stream=None):
     """gmc_evict: every key head keeps its `keep` best-scored rows (the first `sinks` and
-    the last `recent` always), moved to the pages of dst in ascending order; out_idx
-    int32 [B, Hkv, keep], out_scores fp32 [B, Hkv, keep] or None.  Writes dst.lens."""
+    the last `recent` always), moved to the pages of dst, none of which src holds, in
+    ascending order; out_idx int32 [B, Hkv, keep], out_scores fp32 [B, Hkv, keep] or None.
+    Writes dst.lens."""
     if dst.device_index != src.device_index:
         raise GMCError("evict: caches of one device")
     _check_scores(src, scores)
