@@ -347,7 +347,8 @@ cudaError_t launch_cache_append(const KV& c, int dtype, const void* k_new, const
                                 const int32_t* offsets, int rows, int T, cudaStream_t st) {
   const int esize = dtype == GMC_BF16 ? 2 : 4;
   int tile = AP_ROWS;  // rows of a block: fewer where the blocks would not fill the GPU twice
-  while (tile > 4 && (long long)ceil_div(T, tile) * c.B < 304) tile /= 2;
+  const long long fill = 2LL * sm_count();
+  while (tile > 4 && (long long)ceil_div(T, tile) * c.B < fill) tile /= 2;
   return launch_k(k_cache_append, dim3(ceil_div(T, tile), c.B), dim3(AP_THREADS), 0, st, 1, c,
                   (const char*)k_new, (const char*)v_new, offsets, rows, T, esize, tile);
 }
