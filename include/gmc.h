@@ -63,13 +63,15 @@ typedef struct CUstream_st* gmc_stream_t; /* identical to cudaStream_t */
 /* element types of hidden / keys / queries / out_hidden / out_kv */
 #define GMC_F32 0
 #define GMC_BF16 1
+/* pages of a key-value cache alone: 4 bits a value and a scale for 16 (gmc_kv_cache) */
+#define GMC_FP4 2
 
 /* device status bits (gmc_read_status) */
 #define GMC_STATUS_NONFINITE 0x1u  /* check_mode: a client, gain, mass or output was not finite */
 #define GMC_STATUS_TIMEOUT 0x2u    /* a bounded device wait gave up; outputs are not valid */
 #define GMC_STATUS_TEXT_LEN 0x4u   /* text_offsets gave some T_b < 1 or T_b > T */
 #define GMC_STATUS_INTERNAL 0x8u   /* a device-side consistency check failed */
-#define GMC_STATUS_CACHE 0x10u     /* a cache's length, page number or new-row offset was out of range */
+#define GMC_STATUS_CACHE 0x10u     /* a cache's length, page number, new-row offset or position was out of range */
 
 /* Shape limits of this build (GMC_ERR_UNSUPPORTED beyond them). */
 #define GMC_MAX_N 8192            /* visual tokens per image */
@@ -526,15 +528,38 @@ int gmc_clients(const gmc_problem* prob, const gmc_params* params, const gmc_vie
  * Requirements: d a multiple of 8 (bf16) or 4 (fp32), d <= GMC_MAX_CACHE_D
  * (GMC_ERR_UNSUPPORTED beyond); k, v 16-byte aligned, strides multiples of 16
  * bytes and non-negative (GMC_ERR_ARG).
+ *
+ * GMC_FP4: pages hold 4 bits a value, all else (queries, new rows, outputs) is
+ * bf16.  d is 64, 128 or 256 (GMC_ERR_UNSUPPORTED otherwise).  A row is cut into
+ * blocks of 16 channels; a value is s * c, s its block's scale and c one of 0,
+ * 0.5, 1, 1.5, 2, 3, 4 and 6 with a sign (code: sign, two bits of exponent, one
+ * of mantissa).  A scale is a byte: a positive half's bits without its last
+ * seven, (1 + m / 8) 2^(e-15) of e = byte >> 3 > 0 and m = byte & 7, m 2^-17 of
+ * e = 0.  Rows are packed so: s is the block's largest magnitude / 6 rounded to
+ * such a scale (nearest, ties to even), at least 2^-17 where the block is not all
+ * zeros, at most 8192 (values above 49,152 saturate); c is the value / s rounded
+ * (nearest, ties to the even code).  A block with a value that is not finite
+ * becomes 16 NaN (byte 0xf9).
+ * Head `h`'s part of page `p` starts at byte  p * page_stride + h * head_stride:
+ * first the codes of its slots, d / 2 bytes each (channel 2x in the low half of
+ * byte x, channel 2x + 1 in the high), then the scales of its slots, d / 16 bytes
+ * each, together gmc_cache4_part_size bytes (rounded up to 16).  Strides are
+ * bytes; slot_stride is 0; the parts must not overlap (GMC_ERR_ARG).
+ * gmc_cache_append, gmc_cache_append_rope and gmc_decode pack what they append;
+ * all attention is over the values that the codes stand for, a decoded token's
+ * own included.  gmc_attend unpacks the seen rows to bf16 (which holds them
+ * exactly) in its workspace, which grows by B * cap * Hkv * d * 4 bytes, cap being
+ * max_len rounded up to 128.
  */
 typedef struct gmc_kv_cache {
   int B;                     /* sequences, >= 1 */
   int Hkv, d;                /* key/value heads, head size */
-  int dtype;                 /* GMC_F32 or GMC_BF16: pools, queries, new rows and outputs */
+  int dtype;                 /* GMC_F32 or GMC_BF16: pools, queries, new rows and outputs; or
+                                GMC_FP4: pools of 4 bits, the others bf16 */
   int page_size, num_pages;  /* slots of a page, pages of the pool */
   int max_pages;             /* columns of the page table */
   int max_len;               /* bound on every lens[b], 0: max_pages * page_size */
-  int64_t page_stride, head_stride, slot_stride; /* elements */
+  int64_t page_stride, head_stride, slot_stride; /* elements; GMC_FP4: bytes, slot_stride 0 */
   void* k;
   void* v;
   const int32_t* page_table; /* DEVICE int32 [B][max_pages] */
@@ -581,6 +606,55 @@ typedef struct gmc_attn {
  */
 int gmc_cache_append(const gmc_kv_cache* cache, const void* k_new, const void* v_new,
                      const int32_t* offsets, int rows, int T, gmc_stream_t stream);
+
+/*
+ * gmc_cache_append_rope -- gmc_cache_append with the rotation by positions applied
+ * on the way: keys are turned and written to their pages, values written, queries
+ * turned into `out`.  Pair i of a head, channels (i, i + rot / 2), or (2i, 2i + 1)
+ * with `interleaved`, becomes
+ *   (x c - y s, y c + x s),   c = table[p][i], s = table[p][rot / 2 + i],
+ * p being the row's position; channels from `rot` on stay.  Sums are fp32, rounded
+ * once (of GMC_FP4 keys they are exact, rounded to fp32, to bf16, and packed).
+ *   positions   DEVICE int32.  With sections: three rows (t, h, w) a sequence, as
+ *               gmc_compress's out_pos: sequence b's T_b of each from 3 * offsets[b]
+ *               on, and pair i goes by the first where i < sections[0], by the second
+ *               in the next sections[1] pairs, by the third in the last sections[2].
+ *               Without (all 0): one position a row, [rows]; NULL: the row's place in
+ *               its sequence.  A position outside 0 .. max_pos - 1 is clamped and
+ *               sets GMC_STATUS_CACHE.
+ *   k_new, v_new, offsets, rows, T   as in gmc_cache_append; rows new_row_stride apart
+ *   q           [rows][H][d], rows q_row_stride apart; NULL with H == 0
+ *   out         as q, out_row_stride apart; may be q itself with the same stride, and
+ *               overlaps nothing else.  Rows of no sequence are left alone.
+ * rot a multiple of 16, with GMC_FP4 of 32 (GMC_ERR_UNSUPPORTED otherwise).  One launch.
+ */
+typedef struct gmc_rope {
+  const float* table;  /* DEVICE fp32 [max_pos][rot]: cosines, then sines; 16-byte aligned */
+  int max_pos;
+  int rot;             /* channels that turn, <= d */
+  int interleaved;     /* 0 or 1 */
+  int sections[3];     /* all 0, or pairs by position row, rot / 2 together */
+  int H;               /* query heads, 0: none */
+  int64_t q_row_stride, out_row_stride, new_row_stride; /* elements; 0: dense */
+} gmc_rope;
+int gmc_cache_append_rope(const gmc_kv_cache* cache, const gmc_rope* rope,
+                          const int32_t* positions, const void* k_new, const void* v_new,
+                          const void* q, void* out, const int32_t* offsets, int rows, int T,
+                          gmc_stream_t stream);
+
+/*
+ * gmc_cache_read -- the last T_b rows of every sequence out of their pages, into
+ * k_out and v_out, [rows][Hkv][d] (of GMC_FP4 the values as bf16, which is exact).
+ * offsets, rows, T as in gmc_cache_append; a row whose place would lie before the
+ * sequence or whose page is outside the pool is left alone (GMC_STATUS_CACHE).
+ * One launch.
+ */
+int gmc_cache_read(const gmc_kv_cache* cache, void* k_out, void* v_out, const int32_t* offsets,
+                   int rows, int T, gmc_stream_t stream);
+
+/* Bytes of one key head's part of a page of a GMC_FP4 cache, rounded up to 16 (0 where d
+ * is not 64, 128 or 256). */
+size_t gmc_cache4_part_size(int page_size, int d);
 
 /*
  * gmc_attend -- causal attention of every sequence's T_b new tokens (already

@@ -21,7 +21,7 @@ struct KV {
   const int32_t* table;
   int32_t* lens;
   uint32_t* status;
-  long long page_stride, head_stride, slot_stride;  // elements
+  long long page_stride, head_stride, slot_stride;  // elements (GMC_FP4: bytes; of codes)
   int B, Hkv, d, ps, num_pages, max_pages, cap;
 };
 
@@ -158,6 +158,23 @@ __device__ __forceinline__ long long part_row(const AttnArgs& a, int split, int 
   return ((long long)split * a.c.B + b) * a.T + t;
 }
 
+// New rows on their way into the cache, queries and keys turned by their positions.
+struct RopeArgs {
+  KV c;
+  const float* table;  // NULL: nothing turns
+  const int32_t* pos;  // NULL: the places
+  const char *k_new, *v_new, *q;
+  char* out;
+  const int32_t* offsets;
+  long long q_row, o_row, n_row;  // elements
+  int max_pos, rot, near, rows3;  // rows3: three position rows, of pairs below sect0, below
+  int sect0, sect1;               // sect1 and above
+  int H, rows, T;
+};
+cudaError_t launch_append_rope(const RopeArgs&, int dtype, cudaStream_t);
+cudaError_t launch_cache_read(const KV&, int dtype, char* k_out, char* v_out,
+                              const int32_t* offsets, int rows, int T, cudaStream_t);
+
 cudaError_t launch_cache_append(const KV&, int dtype, const void* k_new, const void* v_new,
                                 const int32_t* offsets, int rows, int T, cudaStream_t);
 
@@ -171,6 +188,8 @@ int attend_f32_splits(const KV&, int G, int T);
 cudaError_t launch_attend_f32(const AttnArgs&, cudaStream_t);
 cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t);  // of part and ml
 cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t, int* launches);
+size_t attend_fp4_workspace(const KV&, int H, int T);
+cudaError_t launch_attend_fp4(AttnArgs a, void* ws, cudaStream_t, int* launches);
 
 struct DecodeArgs {
   KV c;
@@ -195,6 +214,7 @@ struct DecodeArgs {
 };
 int sm_count();  // of the current device
 size_t decode_workspace(const KV&, int dtype, int H);
+cudaError_t launch_decode_fp4(const DecodeArgs&, cudaStream_t, int* launches);
 cudaError_t launch_decode(DecodeArgs a, int dtype, void* ws, cudaStream_t, int* launches);
 
 struct EvictArgs {

@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include "cache.cuh"
+#include "fp4.cuh"
 
 using namespace gmc;
 
@@ -18,14 +19,15 @@ int cuda_rc(cudaError_t e) {
 
 constexpr int MAX_PLACES = 0x40000000;  // of a sequence, new ones too: tiles are counted in 32 bits
 
-int esize_of(int dtype) { return dtype == GMC_BF16 ? 2 : 4; }
+int esize_of(int dtype) { return dtype == GMC_FP4 ? 1 : dtype == GMC_BF16 ? 2 : 4; }  // in pages
+int row_type(int dtype) { return dtype == GMC_FP4 ? GMC_BF16 : dtype; }  // of rows outside
 
 // The cache's shape alone (what the workspace sizes need).
 int check_shape(const gmc_kv_cache* c) {
   if (!c || c->B < 1 || c->Hkv < 1 || c->d < 1 || c->page_size < 1 || c->num_pages < 1 ||
       c->max_pages < 1 || c->max_len < 0)
     return GMC_ERR_ARG;
-  if (c->dtype != GMC_F32 && c->dtype != GMC_BF16) return GMC_ERR_ARG;
+  if (c->dtype != GMC_F32 && c->dtype != GMC_BF16 && c->dtype != GMC_FP4) return GMC_ERR_ARG;
   // places are 32-bit; grids hold a sequence or a key head a block
   if ((long long)c->page_size * c->max_pages > MAX_PLACES || c->B > 65535 || c->Hkv > 65535)
     return GMC_ERR_UNSUPPORTED;
@@ -33,6 +35,8 @@ int check_shape(const gmc_kv_cache* c) {
   // turns of 16 keys over all sequences and key heads are counted in 32 bits
   if ((long long)c->B * c->Hkv * (c->page_size * (long long)c->max_pages / 16 + 1) > 0x40000000LL)
     return GMC_ERR_UNSUPPORTED;
+  if (c->dtype == GMC_FP4)
+    return c->d == 64 || c->d == 128 || c->d == 256 ? GMC_OK : GMC_ERR_UNSUPPORTED;
   if (c->d > GMC_MAX_CACHE_D || c->d % (16 / esize_of(c->dtype)) != 0) return GMC_ERR_UNSUPPORTED;
   return GMC_OK;
 }
@@ -49,6 +53,12 @@ int check_cache(const gmc_kv_cache* c) {
   if (!stride_ok(c->page_stride, c->dtype) || !stride_ok(c->head_stride, c->dtype) ||
       !stride_ok(c->slot_stride, c->dtype))
     return GMC_ERR_ARG;
+  if (c->dtype == GMC_FP4) {  // slots lie as the format says, parts of pages apart
+    const long long part = fp4_part(c->page_size, c->d);
+    if (c->slot_stride != 0 || (c->Hkv > 1 && c->head_stride < part) ||
+        (c->num_pages > 1 && c->page_stride < part))
+      return GMC_ERR_ARG;
+  }
   return GMC_OK;
 }
 
@@ -61,7 +71,7 @@ KV view(const gmc_kv_cache* c) {
   v.status = c->status;
   v.page_stride = c->page_stride;
   v.head_stride = c->head_stride;
-  v.slot_stride = c->slot_stride;
+  v.slot_stride = c->dtype == GMC_FP4 ? c->d / 2 : c->slot_stride;
   v.B = c->B;
   v.Hkv = c->Hkv;
   v.d = c->d;
@@ -82,8 +92,9 @@ int check_attn(const gmc_kv_cache* c, const gmc_attn* a) {
     return GMC_ERR_ARG;
   const int rc = check_heads(c, a->H);
   if (rc != GMC_OK) return rc;
-  if (!stride_ok(a->q_row_stride, c->dtype) || !stride_ok(a->q_head_stride, c->dtype) ||
-      !stride_ok(a->out_row_stride, c->dtype) || !stride_ok(a->out_head_stride, c->dtype))
+  const int t = row_type(c->dtype);
+  if (!stride_ok(a->q_row_stride, t) || !stride_ok(a->q_head_stride, t) ||
+      !stride_ok(a->out_row_stride, t) || !stride_ok(a->out_head_stride, t))
     return GMC_ERR_ARG;
   return GMC_OK;
 }
@@ -109,6 +120,11 @@ void heads_of(const gmc_kv_cache* c, const gmc_attn* at, long long* q_row, long 
   *scale2 = (float)(s * 1.4426950408889634074);
 }
 
+size_t attend_ws(const gmc_kv_cache* c, int H, int T) {
+  return c->dtype == GMC_FP4 ? attend_fp4_workspace(view(c), H, T)
+                             : attend_workspace(view(c), c->dtype, H, T);
+}
+
 }  // namespace
 
 extern "C" {
@@ -125,11 +141,86 @@ int gmc_cache_append(const gmc_kv_cache* cache, const void* k_new, const void* v
   return rc;
 }
 
+int gmc_cache_append_rope(const gmc_kv_cache* cache, const gmc_rope* rope,
+                          const int32_t* positions, const void* k_new, const void* v_new,
+                          const void* q, void* out, const int32_t* offsets, int rows, int T,
+                          gmc_stream_t stream) {
+  int rc = check_cache(cache);
+  if (rc == GMC_OK) rc = check_rows(cache, offsets, rows, T);
+  if (rc != GMC_OK) return rc;
+  const int t = row_type(cache->dtype);
+  const int d = cache->d, n = rope ? rope->rot / 2 : 0;
+  if (!rope || !rope->table || !aligned(rope->table, 16) || rope->max_pos < 1 || rope->H < 0 ||
+      rope->rot < 2 || rope->rot > d || (rope->interleaved != 0 && rope->interleaved != 1) ||
+      !aligned(positions, 4) || !stride_ok(rope->q_row_stride, t) ||
+      !stride_ok(rope->out_row_stride, t) || !stride_ok(rope->new_row_stride, t))
+    return GMC_ERR_ARG;
+  const int* sect = rope->sections;
+  if (sect[0] < 0 || sect[1] < 0 || sect[2] < 0) return GMC_ERR_ARG;
+  const long long pairs = (long long)sect[0] + sect[1] + sect[2];
+  const bool rows3 = pairs != 0;
+  if (rows3 && (pairs != n || !positions)) return GMC_ERR_ARG;
+  if (rope->H > 0 && check_heads(cache, rope->H) != GMC_OK) return check_heads(cache, rope->H);
+  // pieces of 16 bytes hold whole pairs, of 4 bits whole blocks
+  if (rope->rot % (cache->dtype == GMC_FP4 ? 32 : 16) != 0) return GMC_ERR_UNSUPPORTED;
+  const int64_t dense = (int64_t)cache->Hkv * d, dense_q = (int64_t)rope->H * d;
+  if ((rope->new_row_stride && (rope->new_row_stride < dense || (!v_new && rope->new_row_stride != dense))) ||
+      (rope->q_row_stride && rope->q_row_stride < dense_q) ||
+      (rope->out_row_stride && rope->out_row_stride < dense_q))
+    return GMC_ERR_ARG;
+  if (rows == 0) return GMC_OK;  // no rows: their pointers may be NULL
+  if (!k_new || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q, 16) ||
+      !aligned(out, 16) || (rope->H > 0) != (q != nullptr) || (rope->H > 0) != (out != nullptr))
+    return GMC_ERR_ARG;
+  RopeArgs a{};
+  a.c = view(cache);
+  a.table = rope->table;
+  a.pos = positions;
+  a.k_new = (const char*)k_new;
+  a.v_new = (const char*)v_new;
+  a.q = (const char*)q;
+  a.out = (char*)out;
+  a.offsets = offsets;
+  a.q_row = rope->q_row_stride ? rope->q_row_stride : dense_q;
+  a.o_row = rope->out_row_stride ? rope->out_row_stride : dense_q;
+  a.n_row = rope->new_row_stride ? rope->new_row_stride : dense;
+  if (q == out && a.q_row != a.o_row) return GMC_ERR_ARG;
+  a.max_pos = rope->max_pos;
+  a.rot = rope->rot;
+  a.near = rope->interleaved;
+  a.rows3 = rows3;
+  a.sect0 = sect[0];
+  a.sect1 = sect[0] + sect[1];
+  a.H = rope->H;
+  a.rows = rows;
+  a.T = T;
+  rc = cuda_rc(launch_append_rope(a, cache->dtype, (cudaStream_t)stream));
+  if (rc == GMC_OK) count_launches(1);
+  return rc;
+}
+
+int gmc_cache_read(const gmc_kv_cache* cache, void* k_out, void* v_out, const int32_t* offsets,
+                   int rows, int T, gmc_stream_t stream) {
+  int rc = check_cache(cache);
+  if (rc == GMC_OK) rc = check_rows(cache, offsets, rows, T);
+  if (rc != GMC_OK || rows == 0) return rc;  // no rows: their pointers may be NULL
+  if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16)) return GMC_ERR_ARG;
+  rc = cuda_rc(launch_cache_read(view(cache), cache->dtype, (char*)k_out, (char*)v_out, offsets,
+                                 rows, T, (cudaStream_t)stream));
+  if (rc == GMC_OK) count_launches(1);
+  return rc;
+}
+
+size_t gmc_cache4_part_size(int page_size, int d) {
+  if (page_size < 1 || page_size > MAX_PLACES || (d != 64 && d != 128 && d != 256)) return 0;
+  return (size_t)((fp4_part(page_size, d) + 15) / 16 * 16);
+}
+
 size_t gmc_attend_workspace_size(const gmc_kv_cache* cache, int H, int T) {
   if (check_shape(cache) != GMC_OK || check_heads(cache, H) != GMC_OK || T < 1 ||
       T > MAX_PLACES)
     return 0;
-  return attend_workspace(view(cache), cache->dtype, H, T);
+  return attend_ws(cache, H, T);
 }
 
 int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
@@ -144,7 +235,7 @@ int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
     return GMC_ERR_ARG;
   AttnArgs a{};
   a.c = view(cache);
-  if (ws_bytes < attend_workspace(a.c, cache->dtype, attn->H, T)) return GMC_ERR_WORKSPACE;
+  if (ws_bytes < attend_ws(cache, attn->H, T)) return GMC_ERR_WORKSPACE;
   a.q = (const char*)q;
   a.out = (char*)out;
   a.lse = lse;
@@ -157,7 +248,9 @@ int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
   a.rows = rows;
   a.T = T;
   int launches = 0;
-  rc = cuda_rc(launch_attend(a, cache->dtype, workspace, (cudaStream_t)stream, &launches));
+  rc = cuda_rc(cache->dtype == GMC_FP4
+                   ? launch_attend_fp4(a, workspace, (cudaStream_t)stream, &launches)
+                   : launch_attend(a, cache->dtype, workspace, (cudaStream_t)stream, &launches));
   count_launches(launches);
   return rc;
 }
@@ -182,7 +275,8 @@ int gmc_decode(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q, c
   a.c = view(cache);
   // offsets inside a page are kept as 32-bit numbers of 16 bytes
   const long long page = a.c.head_stride / 8 * (a.c.Hkv - 1) + a.c.slot_stride / 8 * (a.c.ps - 1);
-  if (page * esize_of(cache->dtype) / 2 > 0xffff0000LL) return GMC_ERR_UNSUPPORTED;
+  if (cache->dtype != GMC_FP4 && page * esize_of(cache->dtype) / 2 > 0xffff0000LL)
+    return GMC_ERR_UNSUPPORTED;
   if (scores && score_stride < a.c.cap) return GMC_ERR_ARG;
   if (ws_bytes < decode_workspace(a.c, cache->dtype, attn->H)) return GMC_ERR_WORKSPACE;
   a.q = (const char*)q;

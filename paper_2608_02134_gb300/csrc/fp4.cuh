@@ -1,0 +1,125 @@
+// Rows held in 4 bits.  A row is cut into blocks of 16 channels; a block has a scale s and a
+// value is c s with c one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign (e2m1).  s is the upper
+// byte but for the sign of a half: 5 bits of exponent, 3 of mantissa, so s as half is the byte
+// shifted left by 7, and c s, with at most 6 bits of mantissa, is exact in half and in bf16.
+// A byte above 0xf8 is a NaN: a block with a value that is not finite stands for 16 NaN.
+//
+// A head's part of a page holds the codes of its slots, d / 2 bytes each (the even channel in
+// the low half of a byte), and then their scales, d / 16 bytes each.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "cache.cuh"
+
+namespace gmc {
+
+constexpr uint32_t FP4_MAX_SCALE = 0xe0;  // 8192: 6 s stays below the largest half
+constexpr uint32_t FP4_NAN_SCALE = 0xf9;
+
+// Bytes of one head's part of a page (a multiple of 4).
+inline long long fp4_part(int ps, int d) { return (long long)ps * (d / 2 + d / 16); }
+
+// Byte offset of a row's scales from the start of its page and head.
+__device__ __forceinline__ long long fp4_scale_at(const KV& c, int slot) {
+  return (long long)c.ps * (c.d / 2) + (long long)slot * (c.d / 16);
+}
+
+// Two scales as halves, the first one's in the low half of a word.
+__device__ __forceinline__ uint32_t fp4_scales(uint32_t s0, uint32_t s1) {
+  return (s0 << 7) | (s1 << 23);
+}
+__device__ __forceinline__ uint32_t fp4_scale2(uint32_t s) { return s * 0x00800080u; }
+
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+
+// The four bytes of a word as four pairs of halves.
+__device__ __forceinline__ void fp4_halves(uint32_t w, uint32_t* h) {
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "mov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+      : "r"(w));
+}
+// Eight codes as eight bf16.
+__device__ __forceinline__ uint4 fp4_bf16(uint32_t w, uint32_t scale2) {
+  uint32_t h[4];
+  fp4_halves(w, h);
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    h[i] = hmul2(h[i], scale2);
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+    const __nv_bfloat162 b = __floats2bfloat162_rn(v.x, v.y);  // exact
+    r[i] = *reinterpret_cast<const uint32_t*>(&b);
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// Eight floats as codes: the nearest, ties to the even code, 6 at most.
+__device__ __forceinline__ uint32_t fp4_codes(const float* y) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r)
+      : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+  return r;
+}
+
+// A block of 16 bf16 values (as floats): its codes and its scale.
+//   s = max |x| / 6 rounded to 3 bits behind the point, ties to even, 2^-17 at least where any
+//   x is not 0, 8192 at most; code = x / s rounded.
+// Both are exact for bf16 values: a quotient of an 8-bit and a 4-bit mantissa that is no tie is
+// 2^-10 of itself or more away from one, and one division (for s) and one step of Newton's
+// method behind a product with 1 / s (for the codes: 1 / s alone is off by 2^-24, which misses
+// ties) leave ties ties.
+__device__ __forceinline__ uint2 fp4_block(const float* x, uint32_t* scale) {
+  uint32_t top = 0;  // of magnitudes, as integers: a NaN is larger than infinity
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  if (top >= 0x7f800000u) {
+    *scale = FP4_NAN_SCALE;
+    return make_uint2(0u, 0u);
+  }
+  const float t = __fdiv_rn(__uint_as_float(top), 6.f);
+  uint32_t s;
+  if (t >= 6.103515625e-05f) {  // 2^-14: a normal half
+    const uint32_t b = __float_as_uint(t);
+    s = ((b + 0x7ffffu + ((b >> 20) & 1u)) >> 20) - (112u << 3);
+    s = min(s, FP4_MAX_SCALE);
+  } else {
+    s = max((uint32_t)__float2int_rn(t * 131072.f), top != 0u ? 1u : 0u);
+  }
+  *scale = s;
+  const float sf = __half2float(__ushort_as_half((unsigned short)(s << 7)));
+  const float r = s ? __frcp_rn(sf) : 0.f;
+  float y[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float q = x[i] * r;
+    y[i] = fmaf(fmaf(-q, sf, x[i]), r, q);
+  }
+  return make_uint2(fp4_codes(y), fp4_codes(y + 8));
+}
+
+__device__ __forceinline__ void unpack_bf16(const uint4& v, float* x) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+
+}  // namespace gmc

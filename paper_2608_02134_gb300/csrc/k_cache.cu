@@ -5,6 +5,7 @@
 #include <type_traits>
 
 #include "cache.cuh"
+#include "fp4.cuh"
 
 namespace gmc {
 
@@ -94,6 +95,7 @@ struct EvSmem {
   int hist[2][EV_BINS * EV_COPIES];  // one is cleared while the other counts
   int list[EV_LIST];
   long long src[EV_THREADS], dst[EV_THREADS];
+  int src_z[EV_THREADS], dst_z[EV_THREADS];  // of 4 bits: from a row's codes to its scales
   int wsum[2][EV_WARPS];
   uint32_t prefix;
   int need;
@@ -128,7 +130,7 @@ __device__ __forceinline__ int lanes_before(int v) {
   return sum - v;
 }
 
-template <int E>
+template <int E, bool FP4>
 __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize, int vec) {
   extern __shared__ __align__(16) char ev_raw[];
   EvSmem* s = reinterpret_cast<EvSmem*>(ev_raw);
@@ -284,7 +286,8 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
     e0 += total & 0xffff;
   }
   __syncthreads();  // this CTA's places are written
-  const int rc = a.src.d * esize / 16;
+  // pieces of a row: of 4 bits the codes' and, as one more, the scales (d / 16 bytes)
+  const int codes = FP4 ? a.src.d / 32 : a.src.d * esize / 16, rc = FP4 ? codes + 1 : codes;
   for (int q0 = p0; q0 < p1; q0 += EV_THREADS) {
     const int nr = min(EV_THREADS, p1 - q0);
     if (tid < nr) {
@@ -297,6 +300,10 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
       if (os) os[q] = score;
       s->src[tid] = so < 0 || dto < 0 ? -1 : so * esize;
       s->dst[tid] = dto * esize;
+      if constexpr (FP4) {
+        s->src_z[tid] = (int)(fp4_scale_at(a.src, from.slot) - (long long)from.slot * (a.src.d / 2));
+        s->dst_z[tid] = (int)(fp4_scale_at(a.dst, to.slot) - (long long)to.slot * (a.dst.d / 2));
+      }
     }
     __syncthreads();
     const int total = nr * rc;
@@ -310,7 +317,15 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
         at[u] = -1;
         if (y < total) {
           const int row = y / rc, z = (y - row * rc) * 16;
-          if (s->src[row] >= 0) {
+          if (FP4 && z == codes * 16) {
+            if (s->src[row] >= 0) {
+              const long long from = s->src[row] + s->src_z[row], to = s->dst[row] + s->dst_z[row];
+              for (int x = 0; x < a.src.d / 16; x += 4) {
+                *(int*)(a.dst.k + to + x) = *(const int*)(a.src.k + from + x);
+                *(int*)(a.dst.v + to + x) = *(const int*)(a.src.v + from + x);
+              }
+            }
+          } else if (s->src[row] >= 0) {
             at[u] = s->dst[row] + z;
             kv[u] = *(const int4*)(a.src.k + s->src[row] + z);
             vv[u] = *(const int4*)(a.src.v + s->src[row] + z);
@@ -345,6 +360,17 @@ int sm_count() {
 
 cudaError_t launch_cache_append(const KV& c, int dtype, const void* k_new, const void* v_new,
                                 const int32_t* offsets, int rows, int T, cudaStream_t st) {
+  if (dtype == GMC_FP4) {  // packed on the way, nothing turns
+    RopeArgs a{};
+    a.c = c;
+    a.k_new = (const char*)k_new;
+    a.v_new = (const char*)v_new;
+    a.offsets = offsets;
+    a.n_row = (long long)c.Hkv * c.d;
+    a.rows = rows;
+    a.T = T;
+    return launch_append_rope(a, dtype, st);
+  }
   const int esize = dtype == GMC_BF16 ? 2 : 4;
   int tile = AP_ROWS;  // rows of a block: fewer where the blocks would not fill the GPU twice
   const long long fill = 2LL * sm_count();
@@ -354,7 +380,7 @@ cudaError_t launch_cache_append(const KV& c, int dtype, const void* k_new, const
 }
 
 cudaError_t launch_evict(const EvictArgs& a, int dtype, cudaStream_t st) {
-  const int esize = dtype == GMC_BF16 ? 2 : 4;
+  const int esize = dtype == GMC_FP4 ? 1 : dtype == GMC_BF16 ? 2 : 4;
   // CTAs of a pair: as many as fill the GPU, 32 kept rows each at least
   const long long pairs = (long long)a.src.B * a.src.Hkv;
   const int S = (int)std::max<long long>(
@@ -368,10 +394,15 @@ cudaError_t launch_evict(const EvictArgs& a, int dtype, cudaStream_t st) {
   };
   // keys of a thread: as few as hold the longest sequence
   const int each = ceil_div(a.src.cap, EV_THREADS);
-  return each <= 2   ? go(k_evict<2>)
-         : each <= 4 ? go(k_evict<4>)
-         : each <= 8 ? go(k_evict<8>)
-                     : go(k_evict<16>);
+  if (dtype == GMC_FP4)
+    return each <= 2   ? go(k_evict<2, true>)
+           : each <= 4 ? go(k_evict<4, true>)
+           : each <= 8 ? go(k_evict<8, true>)
+                       : go(k_evict<16, true>);
+  return each <= 2   ? go(k_evict<2, false>)
+         : each <= 4 ? go(k_evict<4, false>)
+         : each <= 8 ? go(k_evict<8, false>)
+                     : go(k_evict<16, false>);
 }
 
 }  // namespace gmc

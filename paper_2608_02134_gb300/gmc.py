@@ -18,7 +18,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libgmc.so")
 
 GMC_OK, GMC_ERR_ARG, GMC_ERR_UNSUPPORTED, GMC_ERR_WORKSPACE, GMC_ERR_CUDA = range(5)
-GMC_F32, GMC_BF16 = 0, 1
+GMC_F32, GMC_BF16, GMC_FP4 = 0, 1, 2
 STATUS_NONFINITE, STATUS_TIMEOUT, STATUS_TEXT_LEN, STATUS_INTERNAL = 0x1, 0x2, 0x4, 0x8
 STATUS_CACHE = 0x10
 
@@ -30,7 +30,8 @@ EXPORTS = (
     "gmc_transport_noalloc", "gmc_cosine_workspace_size", "gmc_cosine",
     "gmc_workspace_size_views", "gmc_compress_views", "gmc_clients", "gmc_selftest_bounded_wait",
     "gmc_compress_ex", "gmc_workspace_size_long", "gmc_compress_long", "gmc_clients_long",
-    "gmc_compress_host", "gmc_cache_append", "gmc_attend_workspace_size", "gmc_attend",
+    "gmc_compress_host", "gmc_cache_append", "gmc_cache_append_rope", "gmc_cache_read",
+    "gmc_cache4_part_size", "gmc_attend_workspace_size", "gmc_attend",
     "gmc_decode_workspace_size", "gmc_decode", "gmc_evict_workspace_size", "gmc_evict",
 )
 MAX_VIEWS = 4
@@ -96,6 +97,14 @@ class CacheStruct(ctypes.Structure):
                 ("slot_stride", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
                 ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
                 ("status", ctypes.c_void_p)]
+
+
+class RopeStruct(ctypes.Structure):
+    """gmc_rope."""
+    _fields_ = [("table", ctypes.c_void_p), ("max_pos", ctypes.c_int), ("rot", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("sections", ctypes.c_int * 3),
+                ("H", ctypes.c_int), ("q_row_stride", ctypes.c_int64),
+                ("out_row_stride", ctypes.c_int64), ("new_row_stride", ctypes.c_int64)]
 
 
 class Attn(ctypes.Structure):
@@ -203,6 +212,13 @@ def lib() -> ctypes.CDLL:
     C, A, i64 = ctypes.POINTER(CacheStruct), ctypes.POINTER(Attn), ctypes.c_int64
     L.gmc_cache_append.argtypes = [C, vp, vp, vp, i, i, vp]
     L.gmc_cache_append.restype = i
+    L.gmc_cache_append_rope.argtypes = [C, ctypes.POINTER(RopeStruct), vp, vp, vp, vp, vp, vp, i,
+                                        i, vp]
+    L.gmc_cache_append_rope.restype = i
+    L.gmc_cache_read.argtypes = [C, vp, vp, vp, i, i, vp]
+    L.gmc_cache_read.restype = i
+    L.gmc_cache4_part_size.argtypes = [i, i]
+    L.gmc_cache4_part_size.restype = sz
     L.gmc_attend_workspace_size.argtypes = [C, i, i]
     L.gmc_attend_workspace_size.restype = sz
     L.gmc_attend.argtypes = [C, A, vp, vp, i, i, vp, vp, vp, sz, vp]
@@ -489,6 +505,12 @@ class KVCache:
                 or k.dtype != v.dtype or k.dtype not in _DTYPES:
             raise GMCError("cache pools: two [pages, Hkv, page_size, d] tensors alike, fp32 or "
                            "bf16, with unit-stride rows")
+        self._check_rest(k, v, page_table, lens, status)
+        self.num_pages, self.Hkv, self.page_size, self.d = k.shape
+        self.dtype = k.dtype
+        self._finish(_DTYPES[k.dtype], k.stride(0), k.stride(1), k.stride(2), max_len)
+
+    def _check_rest(self, k, v, page_table, lens, status):
         if page_table.dim() != 2 or page_table.dtype != torch.int32 \
                 or lens.dtype != torch.int32 or lens.numel() != page_table.shape[0] \
                 or not page_table.is_contiguous() or not lens.is_contiguous():
@@ -501,13 +523,15 @@ class KVCache:
             raise GMCError("cache: every tensor lies on one device")
         self.k, self.v, self.page_table, self.lens, self.status = k, v, page_table, lens, status
         self.B, self.max_pages = page_table.shape
-        self.num_pages, self.Hkv, self.page_size, self.d = k.shape
-        self.max_len, self.dtype, self.device_index = max_len, k.dtype, device
+        self.device_index = device
+
+    def _finish(self, dtype, page_stride, head_stride, slot_stride, max_len):
+        self.max_len = max_len
         self.struct = CacheStruct(
-            self.B, self.Hkv, self.d, _DTYPES[k.dtype], self.page_size, self.num_pages,
-            self.max_pages, max_len, k.stride(0), k.stride(1), k.stride(2), k.data_ptr(),
-            v.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
-            None if status is None else status.data_ptr())
+            self.B, self.Hkv, self.d, dtype, self.page_size, self.num_pages,
+            self.max_pages, max_len, page_stride, head_stride, slot_stride, self.k.data_ptr(),
+            self.v.data_ptr(), self.page_table.data_ptr(), self.lens.data_ptr(),
+            None if self.status is None else self.status.data_ptr())
         self.ref = ctypes.byref(self.struct)
         self._row_shape = (self.Hkv, self.d)        # of new rows
         self._new_shape = (self.B, self.Hkv, self.d)
@@ -558,6 +582,60 @@ class KVCache:
             return alloc_workspace(nbytes, self.k.device)
 
 
+class KVCache4(KVCache):
+    """A paged key-value cache held in 4 bits: pools k, v uint8 [pages, Hkv, bytes], a head's
+    part of a page in `bytes` (cache4_part_size(page_size, d) or more; any 16-byte strides with
+    unit-stride parts, the same for both).  Queries, new rows and outputs are bf16."""
+
+    def __init__(self, k, v, page_table, lens, page_size, d, max_len=0, status=None):
+        if k.dim() != 3 or k.shape != v.shape or k.stride() != v.stride() or k.stride(2) != 1 \
+                or k.dtype != torch.uint8 or v.dtype != torch.uint8:
+            raise GMCError("cache pools: two uint8 [pages, Hkv, bytes] tensors alike, with "
+                           "unit-stride parts")
+        part = cache4_part_size(page_size, d)
+        if part == 0 or k.shape[2] < part:
+            raise GMCError("cache: head sizes of 64, 128 or 256, and parts of "
+                           "cache4_part_size(page_size, d) bytes")
+        self._check_rest(k, v, page_table, lens, status)
+        self.num_pages, self.Hkv = k.shape[:2]
+        self.page_size, self.d, self.dtype = page_size, d, torch.bfloat16
+        # the stride of a dimension of one is anything
+        self._finish(GMC_FP4, k.stride(0) if self.num_pages > 1 else 0,
+                     k.stride(1) if self.Hkv > 1 else 0, 0, max_len)
+
+
+def cache4_part_size(page_size, d) -> int:
+    """Bytes of one key head's part of a page of a 4-bit cache (0: no such head size)."""
+    return int(lib().gmc_cache4_part_size(page_size, d))
+
+
+class Rope:
+    """The rotation of cache_append_rope: table fp32 [positions, rot] on the device (cosines of
+    the rot / 2 pairs, then sines), pairs of neighbours or halves, and how many pairs go by
+    each of three position rows (None: one position a row).  Holds the table."""
+
+    def __init__(self, table, interleaved=False, sections=None):
+        if table.dim() != 2 or table.dtype != torch.float32 or not table.is_contiguous() \
+                or table.get_device() < 0 or table.shape[0] < 1 or table.shape[1] % 2:
+            raise GMCError("rope: table dense fp32 [positions, rot] on the device")
+        sections = (0, 0, 0) if sections is None else tuple(int(x) for x in sections)
+        if len(sections) != 3 or min(sections) < 0 or \
+                (any(sections) and sum(sections) != table.shape[1] // 2):
+            raise GMCError("rope: three sections of rot / 2 pairs together")
+        self.table, self.rot, self.device_index = table, table.shape[1], table.get_device()
+        self.rows = 3 if any(sections) else 1
+        self._fields = (table.data_ptr(), table.shape[0], table.shape[1], int(interleaved),
+                        (ctypes.c_int * 3)(*sections))
+        self._refs = {}
+
+    def ref(self, H, q_row, out_row, new_row):
+        key = (H, q_row, out_row, new_row)
+        r = self._refs.get(key)
+        if r is None:
+            r = self._refs[key] = ctypes.byref(RopeStruct(*self._fields, *key))
+        return r
+
+
 def _int32_at(cache, t, n, what):
     """The address of an operand (None: NULL) of n dense elements on the cache's device."""
     if t is None:
@@ -604,6 +682,79 @@ def cache_append(cache: KVCache, k_new, v_new, T, offsets=None, stream=None):
                                 _int32_at(cache, offsets, cache.B + 1,
                                           "offsets: dense int32 [B + 1]"),
                                 rows, T, cache.stream(stream))
+    if rc:
+        _check(rc)
+
+
+def _rows_apart(t, shape, what):
+    """The row stride of a tensor [rows, heads, d] whose rows are dense."""
+    if t.shape[1:] != shape or t.stride(2) != 1 or (shape[0] > 1 and t.stride(1) != shape[1]):
+        raise GMCError(what)
+    dense = shape[0] * shape[1]
+    if t.shape[0] > 1:
+        if t.stride(0) < dense:
+            raise GMCError(what + ", none of them shared")
+        return t.stride(0)
+    return dense
+
+
+def cache_append_rope(cache: KVCache, rope: Rope, k_new, v_new, T, positions=None, q=None,
+                      out=None, offsets=None, stream=None):
+    """gmc_cache_append_rope: keys [rows, Hkv, d] turned by their positions into the cache,
+    values into the cache, queries q [rows, H, d] turned into out (which may be q).  Rows may
+    lie apart, as views of a projection's output do.  positions int32: [3 * rows] with the
+    rope's sections ((t, h, w) rows, a sequence after another, as gmc_compress's out_pos),
+    [rows] without, or None: the rows' places.  v_new None: k_new as gmc_compress's out_kv."""
+    device, dtype = cache.device_index, cache.dtype
+    if rope.device_index != device:
+        raise GMCError("rope: its table is on the cache's device")
+    if k_new.dim() != 3 or k_new.dtype != dtype or k_new.get_device() != device:
+        raise GMCError("new rows: [rows, Hkv, d] of the cache's type, on its device")
+    new_row = _rows_apart(k_new, cache._row_shape, "new rows: dense [Hkv, d] of the cache's type")
+    rows = k_new.shape[0]
+    if v_new is None:
+        if not k_new.is_contiguous():
+            raise GMCError("new rows: keys and values in one dense tensor")
+        rows //= 2
+        new_row = cache.Hkv * cache.d
+    elif v_new.shape != k_new.shape or v_new.dtype != dtype or v_new.get_device() != device \
+            or _rows_apart(v_new, cache._row_shape, "new rows: values as keys") != new_row:
+        raise GMCError("new rows: as many values as keys, alike")
+    H = q_row = out_row = 0
+    q_at = out_at = None
+    if q is not None:
+        if out is None or q.dim() != 3 or q.shape != out.shape or q.shape[0] != rows \
+                or q.dtype != dtype or out.dtype != dtype or q.get_device() != device \
+                or out.get_device() != device:
+            raise GMCError("queries and outputs: [rows, H, d] of the cache's type, on its device")
+        H = q.shape[1]
+        q_row = _rows_apart(q, (H, cache.d), "queries: dense [H, d] rows")
+        out_row = _rows_apart(out, (H, cache.d), "outputs: dense [H, d] rows")
+        q_at, out_at = q.data_ptr(), out.data_ptr()
+    elif out is not None:
+        raise GMCError("outputs without queries")
+    rc = lib().gmc_cache_append_rope(
+        cache.ref, rope.ref(H, q_row, out_row, new_row),
+        _int32_at(cache, positions, rope.rows * rows, "positions: dense int32, "
+                  "one (with sections three) a row"),
+        k_new.data_ptr(), None if v_new is None else v_new.data_ptr(), q_at, out_at,
+        _int32_at(cache, offsets, cache.B + 1, "offsets: dense int32 [B + 1]"), rows, T,
+        cache.stream(stream))
+    if rc:
+        _check(rc)
+
+
+def cache_read(cache: KVCache, k_out, v_out, T, offsets=None, stream=None):
+    """gmc_cache_read: the last T rows of every sequence (the most of a ragged call, whose
+    offsets is int32 [B+1]) into k_out, v_out [rows, Hkv, d], of a 4-bit cache as bf16."""
+    for t in (k_out, v_out):
+        if t.shape != k_out.shape or t.shape[1:] != cache._row_shape or t.dtype != cache.dtype \
+                or not t.is_contiguous() or t.get_device() != cache.device_index:
+            raise GMCError("rows: dense [rows, Hkv, d] of the cache's type, on its device")
+    rc = lib().gmc_cache_read(cache.ref, k_out.data_ptr(), v_out.data_ptr(),
+                              _int32_at(cache, offsets, cache.B + 1,
+                                        "offsets: dense int32 [B + 1]"),
+                              k_out.shape[0], T, cache.stream(stream))
     if rc:
         _check(rc)
 
