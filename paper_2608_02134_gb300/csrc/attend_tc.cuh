@@ -11,23 +11,6 @@ constexpr int TM = 128;                 // rows of a tile
 constexpr long long T_WAIT = 4000000000LL;
 constexpr float GROWN = 8.f;            // powers of two the maximum may fall behind
 
-// Division by a number that the host knows: n / d = (n * mul) >> (32 + shift), exact for
-// 0 <= n < 2^31 (mul = ceil(2^(32 + shift) / d) with 2^shift >= d / 2).
-struct Div {
-  unsigned mul, shift, d;
-  __device__ __forceinline__ int of(int n) const {
-    return d == 1 ? n : (int)(__umulhi((unsigned)n, mul) >> shift);
-  }
-};
-inline Div make_div(int d) {
-  Div v;
-  v.d = (unsigned)d;
-  v.shift = 0;
-  while ((2ull << v.shift) < (unsigned long long)d) ++v.shift;
-  v.mul = (unsigned)(((1ull << (32 + v.shift)) + d - 1) / d);
-  return v;
-}
-
 // Bits 0 .. n - 1 of a word.
 __device__ __forceinline__ uint32_t below(int n) {
   return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1;

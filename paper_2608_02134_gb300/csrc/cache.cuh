@@ -15,6 +15,23 @@ __device__ __forceinline__ void grid_dep_launch() {
 constexpr uint32_t CACHE_BAD = GMC_STATUS_CACHE;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
+// Division by a number that the host knows: n / d = (n * mul) >> (32 + shift), exact for
+// 0 <= n < 2^31 (mul = ceil(2^(32 + shift) / d) with 2^shift >= d / 2).
+struct Div {
+  unsigned mul, shift, d;
+  __device__ __forceinline__ int of(int n) const {
+    return d == 1 ? n : (int)(__umulhi((unsigned)n, mul) >> shift);
+  }
+};
+inline Div make_div(int d) {
+  Div v;
+  v.d = (unsigned)d;
+  v.shift = 0;
+  while ((2ull << v.shift) < (unsigned long long)d) ++v.shift;
+  v.mul = (unsigned)(((1ull << (32 + v.shift)) + d - 1) / d);
+  return v;
+}
+
 // gmc_kv_cache by value; cap = the longest a sequence may be.
 struct KV {
   char *k, *v;
@@ -211,6 +228,7 @@ struct DecodeArgs {
   int places, hs;
   int warps;  // of the launch
   unsigned page16, head16, slot16;  // strides in pieces of 16 bytes
+  Div by_ps;
 };
 int sm_count();  // of the current device
 size_t decode_workspace(const KV&, int dtype, int H);

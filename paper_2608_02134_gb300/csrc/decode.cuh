@@ -16,16 +16,39 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 // ---- the row of turns ----------------------------------------------------------------
+// The keys that the new token of a sequence of n tokens walks.  In turns of 32 (pages of 4
+// bits) a turn starts at a multiple of 32 in the sequence, so that it can be copied whole:
+// the sinks' and the window's first turns may hold keys that are not seen.
+template <int DT> __device__ __forceinline__ Seen walked(const DecodeArgs& a, int n) {
+  Seen s = seen_keys(n - 1, n - 1, a.window, a.sinks);
+  if (DT == 32) {
+    s.a = (s.a + 31) & ~31;
+    s.b0 &= ~31;
+    if (s.a >= s.b0) s.a = s.b0 = 0;
+  }
+  return s;
+}
+
 // A pair and a turn of it.
 template <int DT> struct Walk {
   int b, h, t, turns, nv, n;
   Seen seen;
+  int lo, hi;  // turns of 32: those from lo to hi - 1 hold cached keys of one range that are all
+               // seen, key 32 t + off first
+  int off;
   __device__ __forceinline__ void load(const DecodeArgs& a) { load(a, kv_len(a.c, b)); }
   __device__ __forceinline__ void load(const DecodeArgs& a, int tokens) {
     n = tokens;
-    seen = seen_keys(n - 1, n - 1, a.window, a.sinks);
+    seen = walked<DT>(a, n);
     nv = seen.count();
     turns = ceil_div(nv, DT);
+    if (DT == 32) {
+      off = seen.b0 - seen.a;
+      const int from = a.window > 0 ? max(n - a.window, 0) : 0;  // sinks' turns are not among them
+      const int to = a.k_new ? n - 1 : n;
+      lo = (max(from, seen.b0) - off + 31) >> 5;
+      hi = (to - off) >> 5;
+    }
   }
   __device__ __forceinline__ void next_pair(const DecodeArgs& a) {
     t = 0;
@@ -55,7 +78,7 @@ template <int DT> struct TurnRow {
 #pragma unroll 4
     for (int b = b0; b < b1; ++b) {
       n = kv_len(a.c, b);
-      mine += ceil_div(seen_keys(n - 1, n - 1, a.window, a.sinks).count(), DT);
+      mine += ceil_div(walked<DT>(a, n).count(), DT);
     }
     mine *= a.c.Hkv;
     int sum = mine;
@@ -85,6 +108,10 @@ template <int DT> struct TurnRow {
     w->h = u / w->turns;
     w->t = u - w->h * w->turns;
   }
+  // Turns of a CTA of W warps: of 4 bits, whose warps share them out, as many as the others'.
+  __device__ __forceinline__ int of_cta(const DecodeArgs& a, int W) const {
+    return DT == 32 ? max(ceil_div(all, a.warps / W), 1) : W * per;
+  }
   // The first turn of sequence b, and its walk.
   __device__ __forceinline__ int first(const DecodeArgs& a, int b, Walk<DT>* w) const {
     int u = __shfl_sync(FULL, before, b / cs);
@@ -108,23 +135,40 @@ __device__ __forceinline__ float* logits_of(const DecodeArgs& a, const Walk<DT>&
   return a.logits + (((long long)w.b * a.c.Hkv + w.h) * a.places + w.t * DT) * a.hs;
 }
 // ---- joining -------------------------------------------------------------------------------
+// Whether a CTA, whose turns are lo .. hi - 1 of the row, joins its warps' parts and leaves one
+// of a pair: where it has nothing else, and of 4 bits also where it has three pairs at most.
+template <int DT>
+__device__ __forceinline__ bool together(const DecodeArgs& a, const TurnRow<DT>& r, int lo,
+                                         int hi) {
+  Walk<DT> x, y;
+  r.find(a, lo, &x);
+  r.find(a, hi - 1, &y);
+  return (y.b - x.b) * a.c.Hkv + y.h - x.h < (DT == 32 ? 3 : 1);
+}
+
 // The parts of a pair whose turns are u0 .. u0 + turns - 1 of the row: one of every CTA
-// that has nothing else, one of every warp's run in the others.  Runs and pairs both only
+// that joins its warps', one of every warp's run in the others.  Runs and pairs both only
 // grow along the row, so the sum of their numbers numbers the parts' places.
 struct Parts {
   int run0, n0, run1, mid, run2, count, W;
   long long pair;
   bool whole;  // one CTA had it all: its output is written
   template <int DT>
-  __device__ __forceinline__ Parts(const TurnRow<DT>& r, int W_, int u0, int turns, long long pair_) {
+  __device__ __forceinline__ Parts(const DecodeArgs& a, const TurnRow<DT>& r, int W_, int u0,
+                                   int turns, long long pair_) {
     W = W_;
     pair = pair_;
-    const int cta = W * r.per, u1 = u0 + turns;
+    const int cta = r.of_cta(a, W), u1 = u0 + turns;
     const int c0 = u0 / cta, c1 = (u1 - 1) / cta;
+    if (turns == 0) {  // no part
+      n0 = mid = count = 0;
+      whole = false;
+      return;
+    }
     int n, first;
     auto of = [&](int c) {
       const int lo = c * cta, hi = r.all - lo < cta ? r.all : lo + cta;
-      const bool one = lo >= u0 && hi <= u1;
+      const bool one = DT == 32 ? together(a, r, lo, hi) : lo >= u0 && hi <= u1;
       first = one ? 0 : (max(u0, lo) - lo) / r.per;
       n = one ? 1 : (min(u1, hi) - 1 - lo) / r.per - first + 1;
       return one;
@@ -201,117 +245,75 @@ __device__ __forceinline__ void add_scores(const DecodeArgs& a, const Walk<DT>& 
     for (int j = w.seen.a + x0; j < w.seen.b0; j += step) out[j] = in[j];
 }
 
-template <class H, int DP, int W, int NST> constexpr size_t decode_smem() {
-  return (size_t)W * (NST * H::template Ring<NST>::STAGE + H::EXTRA + H::HM * sizeof(float2));
-}
-
-// OWN: a CTA takes a whole pair, and no other.
-template <class H, int DP, int W, int NST, bool OWN>
-__global__ void __launch_bounds__(W * 32, H::CTAS) k_decode(DecodeArgs a) {
-  typedef typename H::T T;
-  typedef typename H::template Ring<NST> R;
-  constexpr int HM = H::HM, DT = H::DT;
-  static_assert(NST * R::STAGE >= HM * DP * 4, "a warp's ring holds its output rows");
-  extern __shared__ __align__(512) char smem[];
-  __shared__ float2 fin[OWN ? 16 : 1];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  char* extra = smem + W * NST * R::STAGE + warp * H::EXTRA;
-  float2* ml = reinterpret_cast<float2*>(smem + W * (NST * R::STAGE + H::EXTRA));  // [W][HM]
-  grid_dep_wait();
-  grid_dep_launch();  // not before: k_decode_join reads the lengths ahead of its own wait
+// The turns of a CTA, and of a warp of its W: u, u + step, .. below end, the first one w.
+template <int DT, int W> struct Stretch {
+  int at, count, u, end, step;
+  bool one, whole;  // all of the CTA's are of one pair; all the pair's
+  bool few;         // of 4 bits: it joins its warps' parts (`together`)
   Walk<DT> w;
-  int at, count, u, end, step = W;  // this warp's turns: u, u + step, .. below end
-  bool one, whole;                  // all of the CTA's are of one pair; all the pair's
-  if constexpr (OWN) {
+  // A whole pair, and no other.
+  __device__ __forceinline__ void own(const DecodeArgs& a) {
     w.b = blockIdx.x / a.c.Hkv;
     w.h = blockIdx.x - w.b * a.c.Hkv;
     w.t = 0;
     w.load(a);
     at = 0;
     count = w.turns;
-    one = whole = true;
-    if (count == 0) {  // it sees nothing
-      for (int x = tid; x < a.heads * (DP / 4); x += W * 32) {
-        const int g = x / (DP / 4), y = (x - g * (DP / 4)) * 4;
-        write_head<T>(a, w.b, w.h, g, y, make_float4(0.f, 0.f, 0.f, 0.f), 0.f);
-        if (y == 0) write_lse(a, w.b, w.h, g, 0.f, 0.f);
-      }
-      return;
-    }
-    w.t = u = warp;
-    end = count;
-  } else {
-    const TurnRow<DT> turns(a);
-    const int cta = W * turns.per;
+    one = whole = few = true;
+  }
+  // As many as every other CTA; false if there are none left.
+  __device__ __forceinline__ bool share(const DecodeArgs& a, const TurnRow<DT>& turns) {
+    const int cta = turns.of_cta(a, W);
     at = turns.all / cta < (int)blockIdx.x ? turns.all : (int)blockIdx.x * cta;
     count = min(cta, turns.all - at);
-    if (count <= 0) return;
+    if (count <= 0) return false;
     turns.find(a, at, &w);
     one = w.t + count <= w.turns;
     whole = one && count == w.turns;
+    few = DT == 32 && together(a, turns, at, at + count);
+    return true;
+  }
+  __device__ __forceinline__ void warp_of_one(int warp) {
+    w.t += warp;
     u = at + warp;
     end = at + count;
-    if (one) {
-      w.t += warp;
-    } else {
-      u = at + warp * turns.per;
-      end = min(end, u + turns.per);
-      step = 1;
-      if (u < end) turns.find(a, u, &w);
-    }
+    step = W;
   }
-  const int pair0 = w.b * a.c.Hkv + w.h;
-  const int b0 = w.b, h0 = w.h;
-  if (u < end) {
-    H heads;
-    R ring{smem + warp * NST * R::STAGE, 0, 0};
-    const int run = (int)blockIdx.x * W + warp;
-    heads.begin(a, w, extra, lane);
-    Walk<DT> f = w;  // the turn whose pages are looked up
-    typename H::Row row;
-    row.look_up(a, f, lane);
-    int fu = u, ahead = 0;
-#pragma unroll 1
-    while (true) {
-      if (fu < end) {  // into the stage that the turn before has left
-        ring.fill(a, row, f.b, f.h, lane);
-        if ((fu += step) < end) {
-          f.next(a, step);
-          row.look_up(a, f, lane);
-        }
-      }
-      cp_async_commit();
-      if (++ahead < NST) continue;
-      cp_async_wait<NST - 1>();
-      __syncwarp();
-      const char* stage = ring.take();
-      heads.turn(a, w, stage, extra, lane);
-      __syncwarp();  // every lane has read the stage
-      const bool last = w.t == w.turns - 1;
-      if (last && a.k_new) H::append(a, w, stage, lane);
-      u += step;
-      if (u < end && !last) {
-        w.t += step;
-        continue;
-      }
-      // the run or the pair ends
-      const long long part = (long long)run + w.b * a.c.Hkv + w.h;
-      if (one)
-        heads.leave(a, ml + warp * HM, reinterpret_cast<float*>(ring.at), lane);
-      else
-        heads.leave(a, a.ml + part * a.heads, a.part + part * a.heads * DP, lane);
-      if (u >= end) break;
-      w.next_pair(a);
-      __syncwarp();
-      heads.begin(a, w, extra, lane);
-    }
+  // Of a CTA with a whole pair a warp's run of it.
+  __device__ __forceinline__ void warp_of_own(int warp) {
+    step = 1;
+    u = warp * ceil_div(count, W);
+    end = min(count, u + ceil_div(count, W));
+    w.t = u;
   }
-  if (!one) return;
-  // one pair: the warps' outputs become the CTA's
-  __syncthreads();
-  const int nw = min(W, count);
-  const long long part = (long long)blockIdx.x * W + pair0;
-  for (int x = tid; x < a.heads * (DP / 4); x += W * 32) {
+  __device__ __forceinline__ void warp_of_several(const DecodeArgs& a, const TurnRow<DT>& turns,
+                                                  int warp) {
+    u = at + warp * turns.per;
+    end = min(at + count, u + turns.per);
+    step = 1;
+    if (u < end) turns.find(a, u, &w);
+  }
+};
+
+// A pair without a seen key.
+template <typename T, int DP>
+__device__ __forceinline__ void write_nothing(const DecodeArgs& a, int b, int h) {
+  for (int x = threadIdx.x; x < a.heads * (DP / 4); x += blockDim.x) {
+    const int g = x / (DP / 4), y = (x - g * (DP / 4)) * 4;
+    write_head<T>(a, b, h, g, y, make_float4(0.f, 0.f, 0.f, 0.f), 0.f);
+    if (y == 0) write_lse(a, b, h, g, 0.f, 0.f);
+  }
+}
+
+// The outputs of a CTA's first nw warps, all of one pair (b, h), become the CTA's: ml[warp][HM]
+// maxima and sums, rows [HM][DP] at `rows`, `room` bytes a warp.  fin: of each head, where the pair
+// is whole.
+template <typename T, int HM, int DP, int W>
+__device__ __forceinline__ void join_warps(const DecodeArgs& a, int b, int h, int nw, bool whole,
+                                           const float2* ml, const char* rows, int room,
+                                           float2* fin) {
+  const long long part = (long long)blockIdx.x * W + b * a.c.Hkv + h;
+  for (int x = threadIdx.x; x < a.heads * (DP / 4); x += W * 32) {
     const int g = x / (DP / 4), y = (x - g * (DP / 4)) * 4;
     float M = -INFINITY, L = 0.f;
     float2 v[W];
@@ -326,8 +328,7 @@ __global__ void __launch_bounds__(W * 32, H::CTAS) k_decode(DecodeArgs a) {
     for (int q = 0; q < W; ++q) {
       if (q >= nw) break;
       const float f = exp2_fast(v[q].x - base);
-      const float4 z =
-          *reinterpret_cast<const float4*>(smem + q * NST * R::STAGE + (g * DP + y) * 4);
+      const float4 z = *reinterpret_cast<const float4*>(rows + q * room + (g * DP + y) * 4);
       L = fmaf(v[q].y, f, L);
       o.x = fmaf(z.x, f, o.x);
       o.y = fmaf(z.y, f, o.y);
@@ -335,21 +336,17 @@ __global__ void __launch_bounds__(W * 32, H::CTAS) k_decode(DecodeArgs a) {
       o.w = fmaf(z.w, f, o.w);
     }
     if (whole) {
-      write_head<T>(a, b0, h0, g, y, o, final_ml(base, L).y);
-      if (y == 0) write_lse(a, b0, h0, g, base, L);
+      write_head<T>(a, b, h, g, y, o, final_ml(base, L).y);
+      if (y == 0) write_lse(a, b, h, g, base, L);
     } else {
       *reinterpret_cast<float4*>(a.part + (part * a.heads + g) * DP + y) = o;
     }
     if (y == 0) {
-      if constexpr (OWN)
+      if (fin)
         fin[g] = final_ml(base, L);
       else
         a.ml[part * a.heads + g] = make_float2(M, L);
     }
-  }
-  if (OWN && a.scores) {
-    __syncthreads();
-    add_scores(a, w, fin, tid, W * 32);
   }
 }
 
@@ -368,8 +365,8 @@ __device__ __forceinline__ float2 join_ml(const DecodeArgs& a, const Parts& p, i
 
 // The parts of every query head joined, a warp each (the first blocks), and the scores,
 // `blocks` CTAs a pair.
-constexpr int JN_WARPS = 8, JN_THREADS = JN_WARPS * 32;
 constexpr int JN_AHEAD = 8;  // places of a thread that are fetched before the sums are joined
+constexpr int JN_WARPS = 8, JN_THREADS = JN_WARPS * 32;
 template <typename T, int DT>
 __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W, int dp,
                                                             int out_blocks, int blocks) {
@@ -387,7 +384,7 @@ __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W,
     const int b = pair / a.c.Hkv;
     w.h = pair - b * a.c.Hkv;
     const int u = row.first(a, b, &w) + w.h * w.turns;
-    const Parts p(row, W, u, w.turns, pair);
+    const Parts p(a, row, W, u, w.turns, pair);
     grid_dep_wait();
     if (w.turns == 0) {  // it sees nothing
       for (int y = lane * 4; y < dp; y += 128)
@@ -439,7 +436,7 @@ __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W,
   w.h = pair - b * a.c.Hkv;
   const int u = row.first(a, b, &w) + w.h * w.turns;
   const int x0 = (x - pair * blocks) * JN_THREADS;
-  const Parts p(row, W, u, w.turns, pair);
+  const Parts p(a, row, W, u, w.turns, pair);
   grid_dep_wait();
   if (w.turns == 0) return;
   // this thread's logits and scores on their way while the sums are joined
@@ -487,21 +484,22 @@ inline DecodeWs decode_carve(const KV& c, int dtype, int H) {
   w.all = w.logits + pairs * logit_heads(dtype, G) * 4 * (size_t)(ceil_div(c.cap, turn) * turn);
   return w;
 }
-template <class H, int DP, int W, int NST>
-cudaError_t decode_launch(DecodeArgs a, cudaStream_t st, int* launches) {
-  constexpr int DT = H::DT;
-  constexpr size_t smem = decode_smem<H, DP, W, NST>();
-  static_assert(smem <= 227 * 1024, "shared memory of a CTA");
+// kernels: a CTA a pair, and equal stretches.
+// Turns a warp of a CTA with a pair of its own has at most: where the pairs are half of the CTAs
+// or more, and where they are fewer.
+struct OwnTurns {
+  int many, few;
+};
+template <typename T, int DT, int DP, int W>
+cudaError_t decode_launch(DecodeArgs a, void (*own_kernel)(DecodeArgs), void (*kernel)(DecodeArgs),
+                          OwnTurns most, size_t smem, cudaStream_t st, int* launches) {
   const int ctas = sm_count();
   const int pairs = a.c.B * a.c.Hkv;
-  // A CTA a pair where that is a few turns a warp: no parts, no second launch.  32 sequences
-  // of 512 keys and 4 key heads: 10.1 us, in stretches 11.3; with scores 12.6 and 14.7.  A
-  // single sequence of 322 takes 9.0, in stretches 8.3, but its call 9.1 instead of 10.4:
-  // the second launch is what the host takes time for; of 768 keys 14.0 and 8.3.
-  const int most = ceil_div(a.c.cap, W * DT);
-  const bool own = pairs <= ctas && most <= (2 * pairs >= ctas ? 6 : 3);
+  // A CTA a pair where that is a few turns a warp: no parts, no second launch.
+  const int turns = ceil_div(a.c.cap, W * DT);
+  const bool own = pairs <= ctas && turns <= (2 * pairs >= ctas ? most.many : most.few);
   a.warps = ctas * W;
-  auto kernel = own ? k_decode<H, DP, W, NST, true> : k_decode<H, DP, W, NST, false>;
+  if (own) kernel = own_kernel;
   cudaError_t e = set_smem_limit((const void*)kernel, smem);
   if (e != cudaSuccess) return e;
   if ((e = launch_k(kernel, dim3(own ? pairs : ctas), dim3(W * 32), smem, st, 1, a)) !=
@@ -520,7 +518,7 @@ cudaError_t decode_launch(DecodeArgs a, cudaStream_t st, int* launches) {
                                       std::max(1, 2 * ctas / pairs));
   }
   ++*launches;
-  return launch_k(k_decode_join<typename H::T, DT>, dim3(out_blocks + pairs * blocks),
+  return launch_k(k_decode_join<T, DT>, dim3(out_blocks + pairs * blocks),
                   dim3(JN_THREADS), 0, st, 1, a, W, DP, out_blocks, std::max(blocks, 1));
 }
 }  // namespace

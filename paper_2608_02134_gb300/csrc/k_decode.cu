@@ -152,9 +152,6 @@ __device__ __forceinline__ void append_new(const DecodeArgs& a, const Walk<DT>& 
 // nothing that shows.
 template <int DP> struct HeadsBf16 {
   static constexpr int HM = 16, EXTRA = 0;  // shared memory of its own, a warp
-  static constexpr int DT = gmc::DT;
-  typedef gmc::Row Row;
-  template <int NST> using Ring = RowRing<DP * 2, NST, 2>;
   static constexpr int CTAS = 0;  // an SM, for the registers: left to the compiler
   typedef __nv_bfloat16 T;
   uint32_t qf[DP / 16][4];
@@ -276,10 +273,6 @@ template <int DP> struct HeadsBf16 {
       for (int y = 0; y < 4; ++y) mma16816(o[2 * c + y], pl, x[2 * y], x[2 * y + 1]);
     }
   }
-  static __device__ __forceinline__ void append(const DecodeArgs& a, const Walk<DT>& w,
-                                                const char*, int lane) {
-    append_new<2>(a, w, lane);
-  }
   // Maxima and sums, and the unnormalised output rows [heads][DP].
   __device__ __forceinline__ void leave(const DecodeArgs& a, float2* ml, float* out, int lane) {
 #pragma unroll
@@ -301,10 +294,7 @@ template <int DP> struct HeadsBf16 {
 // fp32 on the CUDA cores, up to HM query heads a launch: a lane holds half a key's row
 // for the products with q, and 4 columns of the output (or 2 x 4) for those with v.
 template <int DP, int HM_> struct HeadsF32 {
-  static constexpr int DT = gmc::DT;
   static constexpr int HM = HM_, EXTRA = (HM * DP + DT * HM) * 4;
-  typedef gmc::Row Row;
-  template <int NST> using Ring = RowRing<DP * 4, NST, 4>;
   static constexpr int CTAS = 1;  // an SM: all registers (16 sequences of 4,000 keys, 7
                                   // heads a key head: 77 us, 93 with 168 a thread)
   typedef float T;
@@ -407,10 +397,6 @@ template <int DP, int HM_> struct HeadsF32 {
       }
     }
   }
-  static __device__ __forceinline__ void append(const DecodeArgs& a, const Walk<DT>& w,
-                                                const char*, int lane) {
-    append_new<4>(a, w, lane);
-  }
   __device__ __forceinline__ void leave(const DecodeArgs& a, float2* ml, float* out, int lane) {
 #pragma unroll
     for (int g = 0; g < HM; ++g) {
@@ -436,12 +422,113 @@ template <int DP, int HM_> struct HeadsF32 {
   }
 };
 
+// OWN: a CTA takes a whole pair, and no other.
+template <class H, int DP, int W, int NST, bool OWN>
+__global__ void __launch_bounds__(W * 32, H::CTAS) k_decode(DecodeArgs a) {
+  typedef typename H::T T;
+  typedef RowRing<DP * sizeof(T), NST, sizeof(T)> R;
+  constexpr int HM = H::HM;
+  static_assert(NST * R::STAGE >= HM * DP * 4, "a warp's ring holds its output rows");
+  extern __shared__ __align__(512) char smem[];
+  __shared__ float2 fin[OWN ? 16 : 1];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  char* extra = smem + W * NST * R::STAGE + warp * H::EXTRA;
+  float2* ml = reinterpret_cast<float2*>(smem + W * (NST * R::STAGE + H::EXTRA));  // [W][HM]
+  grid_dep_wait();
+  grid_dep_launch();  // not before: k_decode_join reads the lengths ahead of its own wait
+  Stretch<DT, W> s;
+  if constexpr (OWN) {
+    s.own(a);
+    if (s.count == 0) {
+      write_nothing<T, DP>(a, s.w.b, s.w.h);
+      return;
+    }
+    s.warp_of_one(warp);
+  } else {
+    const TurnRow<DT> turns(a);
+    if (!s.share(a, turns)) return;
+    if (s.one)
+      s.warp_of_one(warp);
+    else
+      s.warp_of_several(a, turns, warp);
+  }
+  Walk<DT> w = s.w;
+  const int b0 = w.b, h0 = w.h;
+  int u = s.u;
+  if (u < s.end) {
+    H heads;
+    R ring{smem + warp * NST * R::STAGE, 0, 0};
+    const int run = (int)blockIdx.x * W + warp;
+    heads.begin(a, w, extra, lane);
+    Walk<DT> f = w;  // the turn whose pages are looked up
+    Row row;
+    row.look_up(a, f, lane);
+    int fu = u, ahead = 0;
+#pragma unroll 1
+    while (true) {
+      if (fu < s.end) {  // into the stage that the turn before has left
+        ring.fill(a, row, f.b, f.h, lane);
+        if ((fu += s.step) < s.end) {
+          f.next(a, s.step);
+          row.look_up(a, f, lane);
+        }
+      }
+      cp_async_commit();
+      if (++ahead < NST) continue;
+      cp_async_wait<NST - 1>();
+      __syncwarp();
+      heads.turn(a, w, ring.take(), extra, lane);
+      __syncwarp();  // every lane has read the stage
+      const bool last = w.t == w.turns - 1;
+      if (last && a.k_new) append_new<sizeof(T)>(a, w, lane);
+      u += s.step;
+      if (u < s.end && !last) {
+        w.t += s.step;
+        continue;
+      }
+      // the run or the pair ends
+      const long long part = (long long)run + w.b * a.c.Hkv + w.h;
+      if (s.one)
+        heads.leave(a, ml + warp * HM, reinterpret_cast<float*>(ring.at), lane);
+      else
+        heads.leave(a, a.ml + part * a.heads, a.part + part * a.heads * DP, lane);
+      if (u >= s.end) break;
+      w.next_pair(a);
+      __syncwarp();
+      heads.begin(a, w, extra, lane);
+    }
+  }
+  if (!s.one) return;
+  __syncthreads();
+  join_warps<T, HM, DP, W>(a, b0, h0, min(W, s.count), s.whole, ml, smem, NST * R::STAGE,
+                           OWN ? fin : nullptr);
+  if (OWN && a.scores) {
+    __syncthreads();
+    add_scores(a, w, fin, tid, W * 32);
+  }
+}
+
+template <class H, int DP, int W, int NST>
+cudaError_t decode_go(const DecodeArgs& a, cudaStream_t st, int* launches) {
+  static_assert(W <= 8, "the workspace holds a part a warp");
+  constexpr size_t smem = (size_t)W * (NST * RowRing<DP * sizeof(typename H::T), NST,
+                                                     sizeof(typename H::T)>::STAGE +
+                                       H::EXTRA + H::HM * sizeof(float2));
+  static_assert(smem <= 227 * 1024, "shared memory of a CTA");
+  // own pairs: 32 sequences of 512 keys and 4 key heads 10.1 us, in stretches 11.3; with scores
+  // 12.6 and 14.7.  A single sequence of 322 takes 9.0, in stretches 8.3, but its call 9.1
+  // instead of 10.4: the second launch is what the host takes time for; of 768 keys 14.0 and 8.3.
+  return decode_launch<typename H::T, DT, DP, W>(a, k_decode<H, DP, W, NST, true>,
+                                                 k_decode<H, DP, W, NST, false>, OwnTurns{6, 3},
+                                                 smem, st, launches);
+}
+
 template <int DP, int W, int NST>
 cudaError_t decode_f32(int heads, const DecodeArgs& a, cudaStream_t st, int* launches) {
-  return heads == 1   ? decode_launch<HeadsF32<DP, 1>, DP, W, NST>(a, st, launches)
-         : heads == 2 ? decode_launch<HeadsF32<DP, 2>, DP, W, NST>(a, st, launches)
-         : heads <= 4 ? decode_launch<HeadsF32<DP, 4>, DP, W, NST>(a, st, launches)
-                      : decode_launch<HeadsF32<DP, 8>, DP, W, NST>(a, st, launches);
+  return heads == 1   ? decode_go<HeadsF32<DP, 1>, DP, W, NST>(a, st, launches)
+         : heads == 2 ? decode_go<HeadsF32<DP, 2>, DP, W, NST>(a, st, launches)
+         : heads <= 4 ? decode_go<HeadsF32<DP, 4>, DP, W, NST>(a, st, launches)
+                      : decode_go<HeadsF32<DP, 8>, DP, W, NST>(a, st, launches);
 }
 
 }  // namespace
@@ -468,6 +555,7 @@ cudaError_t launch_decode(DecodeArgs a, int dtype, void* ws, cudaStream_t st, in
                      0xffff0000LL
                  ? (unsigned)page16
                  : 0u;
+  a.by_ps = make_div(a.c.ps);
   for (a.h0 = 0; a.h0 < a.G; a.h0 += hm) {
     a.heads = std::min(hm, a.G - a.h0);
     a.fresh = a.h0 == 0 && a.k_new != nullptr;
@@ -476,9 +564,9 @@ cudaError_t launch_decode(DecodeArgs a, int dtype, void* ws, cudaStream_t st, in
     if (dtype == GMC_FP4)
       e = launch_decode_fp4(a, st, launches);
     else if (dtype == GMC_BF16)
-      e = dp == 64    ? decode_launch<HeadsBf16<64>, 64, 8, 4>(a, st, launches)
-          : dp == 128 ? decode_launch<HeadsBf16<128>, 128, 8, 3>(a, st, launches)
-                      : decode_launch<HeadsBf16<256>, 256, 4, 3>(a, st, launches);
+      e = dp == 64    ? decode_go<HeadsBf16<64>, 64, 8, 4>(a, st, launches)
+          : dp == 128 ? decode_go<HeadsBf16<128>, 128, 8, 3>(a, st, launches)
+                      : decode_go<HeadsBf16<256>, 256, 4, 3>(a, st, launches);
     else
       e = dp == 64    ? decode_f32<64, 8, 3>(hm, a, st, launches)
           : dp == 128 ? decode_f32<128, 4, 3>(hm, a, st, launches)

@@ -17,12 +17,13 @@
 //   are rounded to half (relative 2^-12, an eighth of the output's own rounding; below 2^-14 of
 //   the largest 2^-25 of it), their sum is the unrounded ones'.
 //
-// A turn is 32 keys.  Key x of it lies in row slot(x) of the stage's keys and row x of its
-// values, and 16-byte pieces are swizzled, so that neither read meets a bank twice.
+// A turn is 32 keys from a multiple of 32 on.  Where they are all seen a warp copies their codes
+// and scales in straight runs, else row by row.
 #include <cuda_fp16.h>
 
 #include "decode.cuh"
 #include "fp4.cuh"
+#include "tc.cuh"
 
 namespace gmc {
 
@@ -45,6 +46,21 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+// Words of shared memory.
+template <int BYTES> __device__ __forceinline__ void lds(uint32_t at, uint32_t* w) {
+  if constexpr (BYTES == 16)
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                 : "r"(at));
+  else if constexpr (BYTES == 8)
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+  else if constexpr (BYTES == 4)
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at));
+  else if constexpr (BYTES == 2)
+    asm volatile("ld.shared.u16 %0, [%1];" : "=r"(w[0]) : "r"(at));
+  else
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(w[0]) : "r"(at));
+}
 template <int BYTES>
 __device__ __forceinline__ void cp_async_small(void* smem, const void* src, bool pred) {
   const unsigned sa = (unsigned)__cvta_generic_to_shared(smem);
@@ -53,115 +69,158 @@ __device__ __forceinline__ void cp_async_small(void* smem, const void* src, bool
                : "memory");
 }
 
-// A lane's row of a turn: place `lane` of it.
-struct Fp4Row {
-  enum { NONE, PAGE, FIXED } kind;
-  int slot, page;
-  __device__ __forceinline__ void look_up(const DecodeArgs& a, const Walk<32>& w, int lane) {
-    const int x = w.t * 32 + lane;
-    kind = NONE;
-    page = slot = 0;
-    if (x >= w.nv) return;
-    const int j = w.seen.place(x);
-    if (a.k_new && j == w.n - 1) {
-      kind = FIXED;
-      return;
-    }
-    kind = PAGE;
-    const Slot at = kv_slot(a.c, w.b, j);
-    page = at.page;
-    slot = at.slot;
-  }
-};
-
-// Rows of a stage: the key of row r of an mma's 16 is t + 4 e + 8 h with r = 2 t + e + 8 h.
-__device__ __forceinline__ int key_of_row(int r) { return (r & 24) | ((r & 7) >> 1) | ((r & 1) << 2); }
-__device__ __forceinline__ int row_of_key(int x) { return (x & 24) | ((x & 3) << 1) | ((x & 4) >> 2); }
+// The key of row r (0 .. 7) of an mma.  Four lanes read a key's codes, and lanes 2t (and 2t + 1)
+// of the rows the values' that they are multiplied with: in this order neither meets a bank
+// twice with 64 channels, values twice with 128.
+template <int DP> __device__ __forceinline__ int key_of_row(int r) {
+  return DP == 64 ? (r & 4) | (((r & 1) << 1 | (r >> 1 & 1)) ^ (r >> 1 & 2)) : r ^ (r >> 1 & 1);
+}
 
 // A stage: 32 keys' codes, 32 values', 32 keys' scales, 32 values'.
 template <int DP> struct Fp4Stage {
   static constexpr int CB = DP / 2, SB = DP / 16, P = CB / 16;  // bytes of a row, pieces of codes
   static constexpr int VC = 32 * CB, KS = 64 * CB, VS = KS + 32 * SB, BYTES = VS + 32 * SB;
-  // where a 16-byte piece of a row lies in it
-  static __device__ __forceinline__ int key_piece(int row, int p) {
-    return DP == 256 ? p ^ (row & 1) : p;
-  }
-  static __device__ __forceinline__ int value_piece(int row, int p) {
-    return DP == 256 ? p ^ ((row & 3) * 2) : DP == 128 ? p ^ (row & 2) : p;
-  }
 };
 
-template <int DP, int NST> struct Fp4Ring {
-  typedef Fp4Stage<DP> S;
-  static constexpr int STAGE = S::BYTES;
-  char* at;
-  int put, got;
-  // The next stage takes the turn that `row` was looked up for; rows past the end become
-  // zeros.  The appended row is packed here, from the caller's.
-  __device__ __forceinline__ void fill(const DecodeArgs& a, const Fp4Row& row, int b, int h,
-                                       int lane) {
-    char* base = at + put * STAGE;
-    put = put + 1 == NST ? 0 : put + 1;
-    const bool there = row.kind == Fp4Row::PAGE && (unsigned)row.page < (unsigned)a.c.num_pages;
-    if (row.kind == Fp4Row::PAGE && !there) set_status(a.c.status, CACHE_BAD);
-    const long long part = row.page * a.c.page_stride + h * a.c.head_stride;
-    // -1: no row, zeros; -2: written below
-    const long long codes = there ? part + row.slot * S::CB : row.kind == Fp4Row::FIXED ? -2 : -1;
-    constexpr int P = S::P, RPI = 32 / P;
-    const int sub = lane / P, pc = lane % P;
-#pragma unroll
-    for (int r0 = 0; r0 < 32; r0 += RPI) {
-      const int x = r0 + sub, y = row_of_key(x);
-      const long long o = __shfl_sync(FULL, codes, x);
-      if (o == -2) continue;
-      const long long from = (o >= 0 ? o : 0) + pc * 16;
-      cp_async16(base + y * S::CB + S::key_piece(y, pc) * 16, a.c.k + from, o >= 0);
-      cp_async16(base + S::VC + x * S::CB + S::value_piece(x, pc) * 16, a.c.v + from, o >= 0);
-    }
-    if (row.kind != Fp4Row::FIXED) {
-      const long long from = there ? part + fp4_scale_at(a.c, row.slot) : 0;
-      cp_async_small<S::SB>(base + S::KS + row_of_key(lane) * S::SB, a.c.k + from, there);
-      cp_async_small<S::SB>(base + S::VS + lane * S::SB, a.c.v + from, there);
-    }
-    const unsigned fixed = __ballot_sync(FULL, row.kind == Fp4Row::FIXED);
-    if (fixed) {
-      const int x = __ffs(fixed) - 1, y = row_of_key(x), blk = lane % S::SB;
-      if (lane < 2 * S::SB) {
-        const bool key = lane < S::SB;
-        const uint4* src = reinterpret_cast<const uint4*>(
-            (key ? a.k_new : a.v_new) + (((long long)b * a.c.Hkv + h) * DP + blk * 16) * 2);
-        float v[16];
-        unpack_bf16(src[0], v);
-        unpack_bf16(src[1], v + 8);
-        uint32_t s;
-        const uint2 codes16 = fp4_block(v, &s);
-        char* c = key ? base + y * S::CB + S::key_piece(y, blk >> 1) * 16
-                      : base + S::VC + x * S::CB + S::value_piece(x, blk >> 1) * 16;
-        *reinterpret_cast<uint2*>(c + (blk & 1) * 8) = codes16;
-        base[key ? S::KS + y * S::SB + blk : S::VS + x * S::SB + blk] = (char)s;
-      }
-    }
-  }
-  __device__ __forceinline__ const char* take() {
-    const char* p = at + got * STAGE;
-    got = got + 1 == NST ? 0 : got + 1;
-    return p;
-  }
+// A turn's copies.  Turns whose keys are all seen and cached, in runs of 32 or 16 of one page
+// each, are copied straight through, their page numbers read a turn ahead; any other goes row by
+// row.  Where pages hold whole turns the next turn of the same page is just further on.
+struct Fp4Turn {
+  bool whole, found;        // found: codes and scales are this turn's
+  int page[2], slot, more;  // more: turns of the same page from here on
+  long long codes, scales;  // offsets of the lane's first pieces
 };
+__device__ __forceinline__ int page_of(const DecodeArgs& a, const Walk<32>& w, int j, int* slot) {
+  const int p = a.by_ps.of(j);
+  *slot = j - p * a.c.ps;
+  return a.c.table[(long long)w.b * a.c.max_pages + p];
+}
+__device__ __forceinline__ void look_up(const DecodeArgs& a, const Walk<32>& w, Fp4Turn* x) {
+  x->more = 0;
+  x->found = false;
+  x->whole = (a.c.ps & 15) == 0 && w.t >= w.lo && w.t < w.hi;
+  if (!x->whole) return;
+  const int j = w.t * 32 + w.off;
+  x->page[0] = x->page[1] = page_of(a, w, j, &x->slot);
+  int other;
+  if (a.c.ps & 31)
+    x->page[1] = page_of(a, w, j + 16, &other);
+  else
+    x->more = min((a.c.ps - x->slot) >> 5, w.hi - w.t);
+}
+
+// A key a lane; rows that are not seen become zeros, the appended one is packed here, from the
+// caller's.
+template <int DP>
+__device__ __forceinline__ void fill_rows(const DecodeArgs& a, const Walk<32>& w, int lane,
+                                          char* base) {
+  typedef Fp4Stage<DP> S;
+  const int x = w.t * 32 + lane, j = w.seen.place(x);
+  const bool in = x < w.nv && sees(w.n - 1, j, a.window, a.sinks);
+  const bool fixed = in && a.k_new && j == w.n - 1;
+  int slot = 0, page = -1;
+  if (in && !fixed) page = page_of(a, w, j, &slot);
+  const bool there = in && !fixed && (unsigned)page < (unsigned)a.c.num_pages;
+  if (in && !fixed && !there) set_status(a.c.status, CACHE_BAD);
+  if (!fixed) {
+    const long long part = there ? page * a.c.page_stride + w.h * a.c.head_stride : 0;
+    const long long codes = there ? part + slot * S::CB : 0;
+#pragma unroll
+    for (int pc = 0; pc < S::P; ++pc) {
+      cp_async16(base + lane * S::CB + pc * 16, a.c.k + codes + pc * 16, there);
+      cp_async16(base + S::VC + lane * S::CB + pc * 16, a.c.v + codes + pc * 16, there);
+    }
+    const long long from = there ? part + fp4_scale_at(a.c, slot) : 0;
+    cp_async_small<S::SB>(base + S::KS + lane * S::SB, a.c.k + from, there);
+    cp_async_small<S::SB>(base + S::VS + lane * S::SB, a.c.v + from, there);
+  }
+  const unsigned who = __ballot_sync(FULL, fixed);
+  if (who && lane < 2 * S::SB) {
+    const int y = __ffs(who) - 1, blk = lane % S::SB;
+    const bool key = lane < S::SB;
+    const uint4* src = reinterpret_cast<const uint4*>(
+        (key ? a.k_new : a.v_new) + (((long long)w.b * a.c.Hkv + w.h) * DP + blk * 16) * 2);
+    float v[16];
+    unpack_bf16(src[0], v);
+    unpack_bf16(src[1], v + 8);
+    uint32_t s;
+    const uint2 block = fp4_block(v, &s);
+    *reinterpret_cast<uint2*>(base + (key ? 0 : S::VC) + y * S::CB + blk * 8) = block;
+    base[(key ? S::KS : S::VS) + y * S::SB + blk] = (char)s;
+  }
+}
+// The stage at `base` takes the turn w, looked up before.  Behind it x is the next turn's, if
+// x.more is not 0.
+template <int DP>
+__device__ __forceinline__ void fill(const DecodeArgs& a, const Walk<32>& w, Fp4Turn& x, int lane,
+                                     char* base) {
+  typedef Fp4Stage<DP> S;
+  constexpr int STEPS = 16 * S::CB / 512;  // codes: two runs of 16 keys, 512 bytes a step
+  constexpr int RP = 2 * S::SB;            // scales: of the keys, then of the values, 16 bytes each
+  if (!x.whole || (unsigned)x.page[0] >= (unsigned)a.c.num_pages ||
+      (unsigned)x.page[1] >= (unsigned)a.c.num_pages) {
+    x.more = 0;
+    fill_rows<DP>(a, w, lane, base);
+    return;
+  }
+  const int l16 = lane * 16;
+  if (a.c.ps & 31) {  // two runs of 16
+    const long long head = w.h * a.c.head_stride;
+    const long long p0 = head + x.page[0] * a.c.page_stride,
+                    p1 = head + x.page[1] * a.c.page_stride;
+    const int slot1 = x.slot + 16 < a.c.ps ? x.slot + 16 : 0;
+    const long long o0 = p0 + x.slot * S::CB + l16, o1 = p1 + slot1 * S::CB + l16;
+#pragma unroll
+    for (int y = 0; y < STEPS; ++y) {
+      cp_async16(base + l16 + y * 512, a.c.k + o0 + y * 512);
+      cp_async16(base + S::VC + l16 + y * 512, a.c.v + o0 + y * 512);
+      cp_async16(base + l16 + (STEPS + y) * 512, a.c.k + o1 + y * 512);
+      cp_async16(base + S::VC + l16 + (STEPS + y) * 512, a.c.v + o1 + y * 512);
+    }
+#pragma unroll
+    for (int y = 0; y < 2 * RP; y += 32) {
+      const int z = y + lane, run = z / S::SB, pc = z % S::SB;  // runs: keys' two, values' two
+      const long long o = (run & 1 ? p1 + slot1 * S::SB : p0 + x.slot * S::SB) +
+                          (long long)a.c.ps * S::CB + pc * 16;
+      if (2 * RP >= 32 || z < 2 * RP)
+        cp_async16(base + S::KS + z * 16, (run & 2 ? a.c.v : a.c.k) + o);
+    }
+    return;
+  }
+  if (!x.found) {
+    const long long part = w.h * a.c.head_stride + x.page[0] * a.c.page_stride;
+    x.codes = part + x.slot * S::CB + l16;
+    x.scales = part + (long long)a.c.ps * S::CB + x.slot * S::SB + (lane & (RP - 1)) * 16;
+    x.found = true;
+  }
+  const char *k = a.c.k + x.codes, *v = a.c.v + x.codes;
+#pragma unroll
+  for (int y = 0; y < 2 * STEPS; ++y) {
+    cp_async16(base + l16 + y * 512, k + y * 512);
+    cp_async16(base + S::VC + l16 + y * 512, v + y * 512);
+  }
+  if constexpr (RP == 32) {
+    cp_async16(base + S::KS + l16, a.c.k + x.scales);
+    cp_async16(base + S::VS + l16, a.c.v + x.scales);
+  } else if (2 * RP >= 32 || lane < 2 * RP) {
+    cp_async16(base + S::KS + l16, (lane & RP ? a.c.v : a.c.k) + x.scales);
+  }
+  x.codes += 32 * S::CB;
+  x.scales += 32 * S::SB;
+  --x.more;
+}
 
 template <int DP> struct HeadsFp4 {
-  static constexpr int DT = 32, HM = 8, EXTRA = 0, CTAS = 1;
+  static constexpr int HM = 8;
   typedef __nv_bfloat16 T;
-  typedef Fp4Row Row;
-  template <int NST> using Ring = Fp4Ring<DP, NST>;
   typedef Fp4Stage<DP> S;
   static constexpr int CT = DP / 4;  // channels of a thread in a key
   static constexpr int CV = DP / 8;  // and in a value
   // Lane (g, t) = (lane / 4, lane % 4).  qf: head g, channels t CT ..; o: heads 2t and 2t + 1,
   // channels g CV .. in pairs.
   uint32_t qf[DP / 16][2];
-  float o[DP / 16][4], m[2], l[2], factor[2];
-  __device__ __forceinline__ void begin(const DecodeArgs& a, const Walk<32>& w, char*, int lane) {
+  float o[DP / 16][4], m[2], l[2], factor[2], room[2];
+  __device__ __forceinline__ void begin(const DecodeArgs& a, const Walk<32>& w, int lane) {
     const int g = lane >> 2, t = lane & 3;
     uint2 raw[DP / 16];
     const T* q = reinterpret_cast<const T*>(a.q) + w.b * a.q_row +
@@ -194,81 +253,55 @@ template <int DP> struct HeadsFp4 {
                                : 0u;
     }
     // logits are multiplied by the scale and 2^-k of their heads
-    const float down = a.scale2 * __uint_as_float((uint32_t)(127 - k) << 23);
+    const float down = fmaxf(a.scale2 * __uint_as_float((uint32_t)(127 - k) << 23), 1e-37f);
     factor[0] = __shfl_sync(FULL, down, t * 8);
     factor[1] = __shfl_sync(FULL, down, t * 8 + 4);
 #pragma unroll
     for (int x = 0; x < DP / 16; ++x)
 #pragma unroll
       for (int y = 0; y < 4; ++y) o[x][y] = 0.f;
-    m[0] = m[1] = -INFINITY;
+    m[0] = m[1] = room[0] = room[1] = -INFINITY;
     l[0] = l[1] = 0.f;
   }
   // The key's codes and scales of a thread: CT / 8 words, CT / 16 scales.
-  static __device__ __forceinline__ void load_key(const char* stage, int row, int t, uint32_t* w,
+  static __device__ __forceinline__ void load_key(uint32_t stage, int row, int t, uint32_t* w,
                                                   uint32_t* s) {
-    const char* c = stage + row * S::CB;
-    if constexpr (DP == 64) {
-      const uint2 v = *reinterpret_cast<const uint2*>(c + t * 8);
-      w[0] = v.x;
-      w[1] = v.y;
+    const uint32_t c = stage + row * S::CB + t * (CT / 2);
+    if constexpr (DP == 256) {
+      lds<16>(c, w);
+      lds<16>(c + 16, w + 4);
     } else {
-#pragma unroll
-      for (int i = 0; i < DP / 128; ++i) {
-        const int p = DP / 128 * t + i;
-        const uint4 v = *reinterpret_cast<const uint4*>(c + S::key_piece(row, p) * 16);
-        w[4 * i] = v.x;
-        w[4 * i + 1] = v.y;
-        w[4 * i + 2] = v.z;
-        w[4 * i + 3] = v.w;
-      }
+      lds<CT / 2>(c, w);
     }
-    const char* z = stage + S::KS + row * S::SB + t * (DP / 64);
-    if constexpr (DP == 64) {
-      s[0] = fp4_scale2((uint32_t)(uint8_t)*z);
-    } else if constexpr (DP == 128) {
-      const uint32_t v = *reinterpret_cast<const uint16_t*>(z);
-      s[0] = fp4_scale2(v & 0xffu);
-      s[1] = fp4_scale2(v >> 8);
-    } else {
-      const uint32_t v = *reinterpret_cast<const uint32_t*>(z);
+    uint32_t z;
+    lds<DP / 64>(stage + S::KS + row * S::SB + t * (DP / 64), &z);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = fp4_scale2((v >> (8 * i)) & 0xffu);
-    }
+    for (int i = 0; i < DP / 64; ++i)
+      s[i] = fp4_scale2(DP == 64 ? z : (z >> (8 * i)) & 0xffu);
   }
   // The value's: CV / 8 words, and its blocks' scales, a byte each.
-  static __device__ __forceinline__ void load_value(const char* stage, int row, int g, uint32_t* w,
+  static __device__ __forceinline__ void load_value(uint32_t stage, int row, int g, uint32_t* w,
                                                     uint32_t* s) {
-    const char* c = stage + S::VC + row * S::CB;
-    const char* z = stage + S::VS + row * S::SB;
-    if constexpr (DP == 64) {
-      w[0] = *reinterpret_cast<const uint32_t*>(c + g * 4);
-      *s = (uint8_t)z[g >> 1];
-    } else if constexpr (DP == 128) {
-      const uint2 v =
-          *reinterpret_cast<const uint2*>(c + S::value_piece(row, g >> 1) * 16 + (g & 1) * 8);
-      w[0] = v.x;
-      w[1] = v.y;
-      *s = (uint8_t)z[g];
-    } else {
-      const uint4 v = *reinterpret_cast<const uint4*>(c + S::value_piece(row, g) * 16);
-      w[0] = v.x;
-      w[1] = v.y;
-      w[2] = v.z;
-      w[3] = v.w;
-      *s = *reinterpret_cast<const uint16_t*>(z + 2 * g);
-    }
+    lds<CV / 2>(stage + S::VC + row * S::CB + g * (CV / 2), w);
+    const uint32_t z = stage + S::VS + row * S::SB;
+    if constexpr (DP == 256)
+      lds<2>(z + 2 * g, s);
+    else
+      lds<1>(z + (DP == 64 ? g >> 1 : g), s);
   }
-  __device__ __forceinline__ void turn(const DecodeArgs& a, const Walk<32>& w, const char* stage,
-                                       char*, int lane) {
+  __device__ __forceinline__ void turn(const DecodeArgs& a, const Walk<32>& w, const char* from,
+                                       int lane) {
+    const uint32_t stage = tc::smem_u32(from);
     const int g = lane >> 2, t = lane & 3;
-    float s[2][4];  // keys of rows g and g + 8 of two groups of 16
+    const int kg = key_of_row<DP>(g), k0 = key_of_row<DP>(2 * t), k1 = key_of_row<DP>(2 * t + 1);
+    float s[2][4];  // keys kg and kg + 8 of two groups of 16
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};  // shorter chains
+      float* d = s[n];
+      d[0] = d[1] = d[2] = d[3] = 0.f;
       uint32_t w0[CT / 8], w1[CT / 8], s0[CT / 16], s1[CT / 16];
-      load_key(stage, n * 16 + g, t, w0, s0);
-      load_key(stage, n * 16 + g + 8, t, w1, s1);
+      load_key(stage, n * 16 + kg, t, w0, s0);
+      load_key(stage, n * 16 + kg + 8, t, w1, s1);
 #pragma unroll
       for (int i = 0; i < CT / 8; ++i) {
         uint32_t h0[4], h1[4];
@@ -278,46 +311,44 @@ template <int DP> struct HeadsFp4 {
         for (int j = 0; j < 2; ++j) {
           const uint32_t x[4] = {hmul2(h0[2 * j], s0[i / 2]), hmul2(h1[2 * j], s1[i / 2]),
                                  hmul2(h0[2 * j + 1], s0[i / 2]), hmul2(h1[2 * j + 1], s1[i / 2])};
-          mma_f16(d[j], x, qf[2 * i + j][0], qf[2 * i + j][1]);
+          mma_f16(d, x, qf[2 * i + j][0], qf[2 * i + j][1]);
         }
       }
-#pragma unroll
-      for (int y = 0; y < 4; ++y) s[n][y] = (d[0][y] + d[1][y]) * factor[y & 1];
     }
-    const int x0 = w.t * 32 + key_of_row(g);
-    if (w.t == w.turns - 1) {  // places past the end leave
+    if (w.t < w.lo || w.t >= w.hi) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-          if (x0 + n * 16 + (y >> 1) * 8 >= w.nv) s[n][y] = -INFINITY;
+        for (int y = 0; y < 4; ++y) {
+          const int x = w.t * 32 + n * 16 + (y >> 1) * 8 + kg;
+          if (x >= w.nv || !sees(w.n - 1, w.seen.place(x), a.window, a.sinks))
+            s[n][y] = -INFINITY;
+        }
     }
     if (a.scores) {
-      float* lg = logits_of(a, w) + key_of_row(g) * a.hs + t * 2;
+      float* lg = logits_of(a, w) + kg * a.hs + t * 2;
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           float* z = lg + (n * 16 + y * 8) * a.hs;
+          const float x0 = s[n][2 * y] * factor[0], x1 = s[n][2 * y + 1] * factor[1];
           if (t * 2 + 1 < a.hs)
-            *reinterpret_cast<float2*>(z) = make_float2(s[n][2 * y], s[n][2 * y + 1]);
+            *reinterpret_cast<float2*>(z) = make_float2(x0, x1);
           else if (t * 2 < a.hs)
-            *z = s[n][2 * y];
+            *z = x0;
         }
     }
     // the maximum that weights are taken against follows the running one when that has grown
-    // by 2^8: lanes only meet then
+    // by 2^8 (`room`: that much more as a sum of products): lanes only meet then
     float top[2];
-    bool grew = false;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < 2; ++r)
       top[r] = fmaxf(fmaxf(s[0][r], s[0][2 + r]), fmaxf(s[1][r], s[1][2 + r]));
-      grew |= top[r] > m[r] + 8.f || (m[r] == -INFINITY && top[r] > m[r]);
-    }
-    if (__any_sync(FULL, grew)) {
+    if (__any_sync(FULL, top[0] > room[0] || top[1] > room[1])) {
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        float mn = fmaxf(top[r], m[r]);
+        float mn = fmaxf(top[r] * factor[r], m[r]);
         mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 4));
         mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 8));
         mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 16));
@@ -329,22 +360,28 @@ template <int DP> struct HeadsFp4 {
           o[y][2 + r] *= f;
         }
         m[r] = mn;
+        room[r] = (mn + 8.f) / factor[r];
       }
     }
-    const float base[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+    const f32x2 scale = pair(factor[0], factor[1]),
+                off = pair(m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]);
+    f32x2 sum = pair(l[0], l[1]);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        s[n][y] = exp2_fast(s[n][y] - base[y & 1]);
-        l[y & 1] += s[n][y];
+      for (int y = 0; y < 4; y += 2) {
+        const float2 x = unpair(fma2(pair(s[n][y], s[n][y + 1]), scale, off));
+        s[n][y] = exp2_fast(x.x);
+        s[n][y + 1] = exp2_fast(x.y);
+        sum = add2(sum, pair(s[n][y], s[n][y + 1]));
       }
       const uint32_t p0 = transpose8(pack_half(s[n][0], s[n][1]));
       const uint32_t p1 = transpose8(pack_half(s[n][2], s[n][3]));
-      // values of keys t, t + 4 (the k of p0) and t + 8, t + 12 (of p1)
+      // values of keys k0, k1 (the k of p0) and k0 + 8, k1 + 8 (of p1)
       uint32_t v[4][CV / 8], z[4];
 #pragma unroll
-      for (int y = 0; y < 4; ++y) load_value(stage, n * 16 + y * 4 + t, g, v[y], &z[y]);
+      for (int y = 0; y < 4; ++y)
+        load_value(stage, n * 16 + (y >> 1) * 8 + (y & 1 ? k1 : k0), g, v[y], &z[y]);
 #pragma unroll
       for (int i = 0; i < CV / 8; ++i) {
         const int sh = DP == 256 ? (i >> 1) * 8 : 0;
@@ -364,6 +401,9 @@ template <int DP> struct HeadsFp4 {
         }
       }
     }
+    const float2 all = unpair(sum);
+    l[0] = all.x;
+    l[1] = all.y;
   }
   // Maxima and sums, and the unnormalised output rows [heads][DP].
   __device__ __forceinline__ void leave(const DecodeArgs& a, float2* ml, float* out, int lane) {
@@ -391,33 +431,154 @@ template <int DP> struct HeadsFp4 {
       set_status(a.c.status, CACHE_BAD);
       return;
     }
-    const int x = w.nv - 1 - w.t * 32, y = row_of_key(x);
+    const int x = w.nv - 1 - w.t * 32;
     const long long part = at.page * a.c.page_stride + w.h * a.c.head_stride;
     const long long codes = part + (long long)at.slot * S::CB,
                     scales = part + fp4_scale_at(a.c, at.slot);
     if (lane < S::P)
       *reinterpret_cast<uint4*>(a.c.k + codes + lane * 16) =
-          *reinterpret_cast<const uint4*>(stage + y * S::CB + S::key_piece(y, lane) * 16);
+          *reinterpret_cast<const uint4*>(stage + x * S::CB + lane * 16);
     else if (lane < 2 * S::P)
       *reinterpret_cast<uint4*>(a.c.v + codes + (lane - S::P) * 16) =
-          *reinterpret_cast<const uint4*>(stage + S::VC + x * S::CB +
-                                          S::value_piece(x, lane - S::P) * 16);
+          *reinterpret_cast<const uint4*>(stage + S::VC + x * S::CB + (lane - S::P) * 16);
     constexpr int SW = S::SB / 4;
     if (lane < SW)
       *reinterpret_cast<uint32_t*>(a.c.k + scales + lane * 4) =
-          *reinterpret_cast<const uint32_t*>(stage + S::KS + y * S::SB + lane * 4);
+          *reinterpret_cast<const uint32_t*>(stage + S::KS + x * S::SB + lane * 4);
     else if (lane < 2 * SW)
       *reinterpret_cast<uint32_t*>(a.c.v + scales + (lane - SW) * 4) =
           *reinterpret_cast<const uint32_t*>(stage + S::VS + x * S::SB + (lane - SW) * 4);
   }
 };
 
+// W warps, each with a ring of NST stages and a run of turns.  Where a CTA has three pairs at most
+// it joins its warps' parts: they are balanced whatever the borders, and few are left.  (A pair's
+// turns shared out among all warps, pair after pair, took 28.7 us for 8 x 16,005 keys: a border
+// costs a barrier, and the parts' rounding up.)  OWN: a CTA takes a whole pair, and no other.
+template <int DP, int W, int NST, bool OWN>
+__global__ void __launch_bounds__(W * 32, 1) k_decode_fp4(DecodeArgs a) {
+  typedef HeadsFp4<DP> H;
+  typedef typename H::T T;
+  typedef Fp4Stage<DP> S;
+  constexpr int HM = H::HM, ROWS = HM * DP * 4, SLOTS = W + 2;  // bytes of a part, parts
+  extern __shared__ __align__(512) char smem[];
+  __shared__ float2 fin[OWN ? 8 : 1];
+  char* rows = smem + W * NST * S::BYTES;                       // [SLOTS][HM][DP]
+  float2* ml = reinterpret_cast<float2*>(rows + SLOTS * ROWS);  // [SLOTS][HM]
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  grid_dep_wait();
+  grid_dep_launch();  // not before: k_decode_join reads the lengths ahead of its own wait
+  Stretch<32, W> s;
+  int per;
+  Walk<32> first;  // the CTA's first turn
+  if constexpr (OWN) {
+    s.own(a);
+    if (s.count == 0) {
+      write_nothing<T, DP>(a, s.w.b, s.w.h);
+      return;
+    }
+    first = s.w;
+    per = ceil_div(s.count, W);
+    s.warp_of_own(warp);
+  } else {
+    const TurnRow<32> turns(a);
+    if (!s.share(a, turns)) return;
+    first = s.w;
+    per = turns.per;
+    s.warp_of_several(a, turns, warp);
+  }
+  const int pair0 = first.b * a.c.Hkv + first.h;
+  int left = s.end - s.u;  // of the run
+  if (left > 0) {
+    char* const ring = smem + warp * NST * S::BYTES;
+    int put = 0, got = 0, ahead = left;  // stages, turns to be copied
+    Walk<32> f = s.w;
+    Fp4Turn x;
+    look_up(a, f, &x);
+    auto copy = [&]() {
+      if (ahead > 0) {
+        fill<DP>(a, f, x, lane, ring + put * S::BYTES);
+        put = put + 1 == NST ? 0 : put + 1;
+        if (--ahead > 0) {
+          if (++f.t >= f.turns) {
+            f.next_pair(a);
+            x.more = 0;
+          }
+          if (x.more == 0) look_up(a, f, &x);
+        }
+      }
+      cp_async_commit();
+    };
+#pragma unroll 1
+    for (int y = 0; y < NST - 1; ++y) copy();
+    H heads;
+    Walk<32> w = s.w;
+    while (true) {  // pair after pair
+      heads.begin(a, w, lane);
+      const int limit = min(w.turns, w.t + left);
+      left -= limit - w.t;
+#pragma unroll 1
+      for (; w.t < limit; ++w.t) {
+        copy();  // into the stage that the turn before has left
+        cp_async_wait<NST - 1>();
+        __syncwarp();
+        const char* here = ring + got * S::BYTES;
+        got = got + 1 == NST ? 0 : got + 1;
+        heads.turn(a, w, here, lane);
+        if (w.t == w.turns - 1 && a.k_new) H::append(a, w, here, lane);
+        __syncwarp();  // every lane has read the stage
+      }
+      const int pair = w.b * a.c.Hkv + w.h;
+      if (s.few) {
+        const int slot = warp + pair - pair0;
+        heads.leave(a, ml + slot * HM, reinterpret_cast<float*>(rows + slot * ROWS), lane);
+      } else {
+        const long long part = (long long)blockIdx.x * W + warp + pair;
+        heads.leave(a, a.ml + part * a.heads, a.part + part * a.heads * DP, lane);
+      }
+      if (left <= 0) break;
+      w.next_pair(a);
+    }
+  }
+  if (!s.few) return;
+  __syncthreads();
+  // the pairs' parts: of warps t0 / per to (t1 - 1) / per
+  Walk<32>& w = first;
+  for (int t0 = 0;;) {
+    const int t1 = min(s.count, t0 + w.turns - w.t), p0 = t0 / per, p1 = (t1 - 1) / per;
+    const int slot = p0 + w.b * a.c.Hkv + w.h - pair0;
+    join_warps<T, HM, DP, W>(a, w.b, w.h, p1 - p0 + 1, t1 - t0 == w.turns, ml + slot * HM,
+                             rows + slot * ROWS, ROWS, OWN ? fin : nullptr);
+    if (t1 >= s.count) break;
+    t0 = t1;
+    w.next_pair(a);
+  }
+  if (OWN && a.scores) {
+    __syncthreads();
+    add_scores(a, w, fin, tid, W * 32);
+  }
+}
+
+template <int DP, int W, int NST>
+cudaError_t decode_fp4_go(const DecodeArgs& a, cudaStream_t st, int* launches) {
+  static_assert(W <= 16, "the workspace holds a part a warp");
+  constexpr size_t smem =
+      (size_t)W * NST * Fp4Stage<DP>::BYTES + (size_t)(W + 2) * (8 * DP * 4 + 8 * sizeof(float2));
+  static_assert(smem <= 226 * 1024, "shared memory of a CTA");
+  // own pairs, with 128 channels and 4 key heads: 32 sequences of 512 keys and scores 8.2 us, in
+  // stretches 14.0; of up to 3,000 25.7 and 27.6; 20 of 4,000 21.7 and 21.2.  One of 322 keys 5.6
+  // and 9.7, of 1,500 9.9 and 11.8; two of 3,000 15.5 and 14.7.
+  return decode_launch<__nv_bfloat16, 32, DP, W>(a, k_decode_fp4<DP, W, NST, true>,
+                                                 k_decode_fp4<DP, W, NST, false>,
+                                                 OwnTurns{8 * 12 / W, 4 * 12 / W}, smem, st, launches);
+}
+
 }  // namespace
 
 cudaError_t launch_decode_fp4(const DecodeArgs& a, cudaStream_t st, int* launches) {
-  return a.c.d == 64    ? decode_launch<HeadsFp4<64>, 64, 16, 4>(a, st, launches)
-         : a.c.d == 128 ? decode_launch<HeadsFp4<128>, 128, 16, 3>(a, st, launches)
-                        : decode_launch<HeadsFp4<256>, 256, 8, 3>(a, st, launches);
+  return a.c.d == 64    ? decode_fp4_go<64, 12, 4>(a, st, launches)
+         : a.c.d == 128 ? decode_fp4_go<128, 12, 2>(a, st, launches)
+                        : decode_fp4_go<256, 6, 2>(a, st, launches);
 }
 
 }  // namespace gmc
