@@ -2,6 +2,8 @@
 // documented in include/gmc.h): argument checks, workspaces and launches.
 #include <math.h>
 
+#include <algorithm>
+
 #include "cache.cuh"
 #include "fp4.cuh"
 
@@ -120,9 +122,28 @@ void heads_of(const gmc_kv_cache* c, const gmc_attn* at, long long* q_row, long 
   *scale2 = (float)(s * 1.4426950408889634074);
 }
 
+// One token a sequence over 4 bits goes the way of gmc_decode, which reads the codes themselves.
 size_t attend_ws(const gmc_kv_cache* c, int H, int T) {
-  return c->dtype == GMC_FP4 ? attend_fp4_workspace(view(c), H, T)
-                             : attend_workspace(view(c), c->dtype, H, T);
+  if (c->dtype != GMC_FP4) return attend_workspace(view(c), c->dtype, H, T);
+  const size_t n = attend_fp4_workspace(view(c), H, T);
+  return T == 1 ? std::max(n, decode_workspace(view(c), c->dtype, H)) : n;
+}
+cudaError_t attend_one(const AttnArgs& a, void* ws, cudaStream_t st, int* launches) {
+  DecodeArgs d{};
+  d.c = a.c;
+  d.q = a.q;
+  d.out = a.out;
+  d.lse = a.lse;
+  d.q_row = a.q_row;
+  d.q_head = a.q_head;
+  d.o_row = a.o_row;
+  d.o_head = a.o_head;
+  d.H = a.H;
+  d.G = a.G;
+  d.window = a.window;
+  d.sinks = a.sinks;
+  d.scale2 = a.scale2;
+  return launch_decode(d, GMC_FP4, ws, st, launches);
 }
 
 }  // namespace
@@ -248,7 +269,9 @@ int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
   a.rows = rows;
   a.T = T;
   int launches = 0;
-  rc = cuda_rc(cache->dtype == GMC_FP4
+  rc = cuda_rc(cache->dtype == GMC_FP4 && T == 1 && !q_offsets
+                   ? attend_one(a, workspace, (cudaStream_t)stream, &launches)
+               : cache->dtype == GMC_FP4
                    ? launch_attend_fp4(a, workspace, (cudaStream_t)stream, &launches)
                    : launch_attend(a, cache->dtype, workspace, (cudaStream_t)stream, &launches));
   count_launches(launches);

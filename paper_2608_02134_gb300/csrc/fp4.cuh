@@ -77,40 +77,70 @@ __device__ __forceinline__ uint32_t fp4_codes(const float* y) {
   return r;
 }
 
-// A block of 16 bf16 values (as floats): its codes and its scale.
+// 32 bytes at once: whole sectors.
+__device__ __forceinline__ void store32(void* p, const uint4& lo, const uint4& hi) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(lo.x),
+               "r"(lo.y), "r"(lo.z), "r"(lo.w), "r"(hi.x), "r"(hi.y), "r"(hi.z), "r"(hi.w)
+               : "memory");
+}
+
+// A block's codes and scale from its bf16 values.
 //   s = max |x| / 6 rounded to 3 bits behind the point, ties to even, 2^-17 at least where any
 //   x is not 0, 8192 at most; code = x / s rounded.
 // Both are exact for bf16 values: a quotient of an 8-bit and a 4-bit mantissa that is no tie is
-// 2^-10 of itself or more away from one, and one division (for s) and one step of Newton's
-// method behind a product with 1 / s (for the codes: 1 / s alone is off by 2^-24, which misses
-// ties) leave ties ties.
-__device__ __forceinline__ uint2 fp4_block(const float* x, uint32_t* scale) {
-  uint32_t top = 0;  // of magnitudes, as integers: a NaN is larger than infinity
+// 2^-10 of itself or more away from one, and products with 1 / 6 and 1 / s as sums of two floats
+// leave ties ties (1 / s alone is off by 2^-24, which misses them).
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// The largest of eight magnitudes, as an integer: a NaN is larger than infinity.
+__device__ __forceinline__ uint32_t fp4_top(const uint4& v) {
+  constexpr uint32_t M = 0x7fff7fffu;
+  const uint32_t t = max_u16x2(max_u16x2(v.x & M, v.y & M), max_u16x2(v.z & M, v.w & M));
+  return max(t & 0xffffu, t >> 16);
+}
+struct Fp4Scale {
+  uint32_t byte;
+  float hi, lo;  // 1 / s
+  // top: the block's largest magnitude, the bits of a bf16
+  __device__ __forceinline__ explicit Fp4Scale(uint32_t top) {
+    hi = lo = 0.f;
+    byte = FP4_NAN_SCALE;
+    if (top >= 0x7f80u) return;
+    const float x = __uint_as_float(top << 16);
+    constexpr float S = 0.166666671633720397949f, R = -4.967053879312289e-09f;  // S + R = 1 / 6
+    const float t = fmaf(x, S, x * R);
+    if (t >= 6.103515625e-05f) {  // 2^-14: a normal half
+      const uint32_t b = __float_as_uint(t);
+      byte = min(((b + 0x7ffffu + ((b >> 20) & 1u)) >> 20) - (112u << 3), FP4_MAX_SCALE);
+    } else {
+      byte = max((uint32_t)__float2int_rn(t * 131072.f), top != 0u ? 1u : 0u);
+      if (byte == 0u) return;
+    }
+    const float s = __half2float(__ushort_as_half((unsigned short)(byte << 7)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(hi) : "f"(s));
+    lo = fmaf(-s, hi, 1.f) * hi;
+  }
+  __device__ __forceinline__ uint32_t codes(const uint4& v) const {
+    if (byte == FP4_NAN_SCALE) return 0u;
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    float y[8];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-  if (top >= 0x7f800000u) {
-    *scale = FP4_NAN_SCALE;
-    return make_uint2(0u, 0u);
+    for (int i = 0; i < 4; ++i) {
+      const f32x2 x = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+      const float2 z = unpair(fma2(x, pair(hi, hi), mul2(x, pair(lo, lo))));
+      y[2 * i] = z.x;
+      y[2 * i + 1] = z.y;
+    }
+    return fp4_codes(y);
   }
-  const float t = __fdiv_rn(__uint_as_float(top), 6.f);
-  uint32_t s;
-  if (t >= 6.103515625e-05f) {  // 2^-14: a normal half
-    const uint32_t b = __float_as_uint(t);
-    s = ((b + 0x7ffffu + ((b >> 20) & 1u)) >> 20) - (112u << 3);
-    s = min(s, FP4_MAX_SCALE);
-  } else {
-    s = max((uint32_t)__float2int_rn(t * 131072.f), top != 0u ? 1u : 0u);
-  }
-  *scale = s;
-  const float sf = __half2float(__ushort_as_half((unsigned short)(s << 7)));
-  const float r = s ? __frcp_rn(sf) : 0.f;
-  float y[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float q = x[i] * r;
-    y[i] = fmaf(fmaf(-q, sf, x[i]), r, q);
-  }
-  return make_uint2(fp4_codes(y), fp4_codes(y + 8));
+};
+__device__ __forceinline__ uint2 fp4_block(const uint4& v0, const uint4& v1, uint32_t* scale) {
+  const Fp4Scale s(max(fp4_top(v0), fp4_top(v1)));
+  *scale = s.byte;
+  return make_uint2(s.codes(v0), s.codes(v1));
 }
 
 __device__ __forceinline__ void unpack_bf16(const uint4& v, float* x) {

@@ -14,17 +14,20 @@ namespace {
 constexpr int UP_PAGE = 128;  // slots of a page of the workspace: whole turns of k_attend_tc
 constexpr int UP_THREADS = 256, UP_ROWS = 32;
 
-// UP_ROWS rows of one page; rows that no query sees become zeros, and pages without a seen
-// row are left alone.
+// UP_ROWS rows of one page and head; rows that no query sees become zeros, and pages without a
+// seen row are left alone.  A lane takes a block of 16 channels, the loads of four blocks before
+// the first is stored.
+template <int D>
 __global__ void __launch_bounds__(UP_THREADS) k_unpack(AttnArgs a, KV to) {
+  constexpr int HC = D / 16, ITEMS = 2 * UP_ROWS * HC;  // keys' blocks, then the values'
   __shared__ long long at[UP_ROWS];
   __shared__ int slots[UP_ROWS];
   grid_dep_launch();
   grid_dep_wait();
-  const int b = blockIdx.y, j0 = blockIdx.x * UP_ROWS, page = j0 / UP_PAGE;
+  const int b = blockIdx.z, h = blockIdx.y, j0 = blockIdx.x * UP_ROWS, page = j0 / UP_PAGE;
   const int n = kv_len(a.c, b);
   const NewRows nr = new_rows(a.q_offsets, b, a.rows, a.T, a.c.status);
-  if (j0 % UP_PAGE == 0 && threadIdx.x == 0)
+  if (h == 0 && j0 % UP_PAGE == 0 && threadIdx.x == 0)
     const_cast<int32_t*>(to.table)[(long long)b * to.max_pages + page] = b * to.max_pages + page;
   if (nr.T == 0) return;
   const Seen seen = seen_keys(n - nr.T, n - 1, a.window, a.sinks);
@@ -39,32 +42,38 @@ __global__ void __launch_bounds__(UP_THREADS) k_unpack(AttnArgs a, KV to) {
     if (j < n && sees_any(j, j + 1)) {
       const Slot s = kv_slot(a.c, b, j);
       slot = s.slot;
-      o = kv_row(a.c, 0, Slot{s.page, 0});
+      o = kv_row(a.c, h, Slot{s.page, 0});
     }
     at[threadIdx.x] = o;
     slots[threadIdx.x] = slot;
   }
   __syncthreads();
-  const int hc = a.c.d / 16, rc = UP_ROWS * hc;
   const long long base = (long long)(b * to.max_pages + page) * to.page_stride +
-                         (long long)(j0 % UP_PAGE) * to.slot_stride;
-  for (int x = threadIdx.x; x < rc * a.c.Hkv; x += UP_THREADS) {
-    const int h = x / rc, y = x - h * rc, r = y / hc, z = y - r * hc;
-    const long long dst = base + h * to.head_stride + r * to.slot_stride + z * 16;
+                         h * to.head_stride + (long long)(j0 % UP_PAGE) * D;
+  constexpr int U = ITEMS / UP_THREADS < 4 ? ITEMS / UP_THREADS : 4;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+  for (int x0 = 0; x0 < ITEMS; x0 += U * UP_THREADS) {
+    uint2 c[U];
+    uint32_t s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int x = x0 + u * UP_THREADS + threadIdx.x, v = x / (UP_ROWS * HC),
+                y = x % (UP_ROWS * HC), r = y / HC, z = y % HC;
+      c[u] = make_uint2(0u, 0u);
+      s[u] = 0;
       if (at[r] >= 0) {
-        const char* part = (i ? a.c.v : a.c.k) + at[r] + h * a.c.head_stride;
-        const uint2 v =
-            *reinterpret_cast<const uint2*>(part + (long long)slots[r] * (a.c.d / 2) + z * 8);
-        const uint32_t s2 = fp4_scale2((uint8_t)part[fp4_scale_at(a.c, slots[r]) + z]);
-        lo = fp4_bf16(v.x, s2);
-        hi = fp4_bf16(v.y, s2);
+        const char* part = (v ? a.c.v : a.c.k) + at[r];
+        c[u] = *reinterpret_cast<const uint2*>(part + (long long)slots[r] * (D / 2) + z * 8);
+        s[u] = (uint8_t)part[fp4_scale_at(a.c, slots[r]) + z];
       }
-      uint4* p = reinterpret_cast<uint4*>((i ? to.v : to.k) + dst * 2);
-      p[0] = lo;
-      p[1] = hi;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int x = x0 + u * UP_THREADS + threadIdx.x, v = x / (UP_ROWS * HC),
+                y = x % (UP_ROWS * HC);
+      const uint32_t s2 = fp4_scale2(s[u]);
+      store32((v ? to.v : to.k) + (base + y * 16) * 2, fp4_bf16(c[u].x, s2),
+              fp4_bf16(c[u].y, s2));
     }
   }
 }
@@ -100,8 +109,10 @@ cudaError_t launch_attend_fp4(AttnArgs a, void* ws, cudaStream_t st, int* launch
   u.c.table = reinterpret_cast<int32_t*>(ws);
   u.c.k = (char*)ws + u.table;
   u.c.v = u.c.k + u.pool;
-  const cudaError_t e = launch_k(k_unpack, dim3(u.c.max_pages * (UP_PAGE / UP_ROWS), a.c.B),
-                                 dim3(UP_THREADS), 0, st, 1, a, u.c);
+  auto unpack = a.c.d == 64 ? k_unpack<64> : a.c.d == 128 ? k_unpack<128> : k_unpack<256>;
+  const cudaError_t e =
+      launch_k(unpack, dim3(u.c.max_pages * (UP_PAGE / UP_ROWS), a.c.Hkv, a.c.B),
+               dim3(UP_THREADS), 0, st, 1, a, u.c);
   if (e != cudaSuccess) return e;
   ++*launches;
   a.c = u.c;

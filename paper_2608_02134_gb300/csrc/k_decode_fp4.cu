@@ -140,11 +140,8 @@ __device__ __forceinline__ void fill_rows(const DecodeArgs& a, const Walk<32>& w
     const bool key = lane < S::SB;
     const uint4* src = reinterpret_cast<const uint4*>(
         (key ? a.k_new : a.v_new) + (((long long)w.b * a.c.Hkv + w.h) * DP + blk * 16) * 2);
-    float v[16];
-    unpack_bf16(src[0], v);
-    unpack_bf16(src[1], v + 8);
     uint32_t s;
-    const uint2 block = fp4_block(v, &s);
+    const uint2 block = fp4_block(src[0], src[1], &s);
     *reinterpret_cast<uint2*>(base + (key ? 0 : S::VC) + y * S::CB + blk * 8) = block;
     base[(key ? S::KS : S::VS) + y * S::SB + blk] = (char)s;
   }

@@ -624,16 +624,9 @@ class Rope:
             raise GMCError("rope: three sections of rot / 2 pairs together")
         self.table, self.rot, self.device_index = table, table.shape[1], table.get_device()
         self.rows = 3 if any(sections) else 1
-        self._fields = (table.data_ptr(), table.shape[0], table.shape[1], int(interleaved),
-                        (ctypes.c_int * 3)(*sections))
-        self._refs = {}
-
-    def ref(self, H, q_row, out_row, new_row):
-        key = (H, q_row, out_row, new_row)
-        r = self._refs.get(key)
-        if r is None:
-            r = self._refs[key] = ctypes.byref(RopeStruct(*self._fields, *key))
-        return r
+        self.fields = (table.data_ptr(), table.shape[0], table.shape[1], int(interleaved),
+                       (ctypes.c_int * 3)(*sections))
+        self.layouts = {}
 
 
 def _int32_at(cache, t, n, what):
@@ -698,6 +691,30 @@ def _rows_apart(t, shape, what):
     return dense
 
 
+def _rope_layout(cache, rope, k_new, v_new, q, out):
+    """Rows and gmc_rope of these operands' shapes and strides."""
+    if k_new.dim() != 3:
+        raise GMCError("new rows: [rows, Hkv, d] of the cache's type, on its device")
+    new_row = _rows_apart(k_new, cache._row_shape, "new rows: dense [Hkv, d] of the cache's type")
+    rows = k_new.shape[0]
+    if v_new is None:
+        if not k_new.is_contiguous():
+            raise GMCError("new rows: keys and values in one dense tensor")
+        rows //= 2
+        new_row = cache.Hkv * cache.d
+    elif v_new.shape != k_new.shape \
+            or _rows_apart(v_new, cache._row_shape, "new rows: values as keys") != new_row:
+        raise GMCError("new rows: as many values as keys, alike")
+    H = q_row = out_row = 0
+    if q is not None:
+        if q.dim() != 3 or q.shape != out.shape or q.shape[0] != rows:
+            raise GMCError("queries and outputs: [rows, H, d] of the cache's type, on its device")
+        H = q.shape[1]
+        q_row = _rows_apart(q, (H, cache.d), "queries: dense [H, d] rows")
+        out_row = _rows_apart(out, (H, cache.d), "outputs: dense [H, d] rows")
+    return rows, ctypes.byref(RopeStruct(*rope.fields, H, q_row, out_row, new_row))
+
+
 def cache_append_rope(cache: KVCache, rope: Rope, k_new, v_new, T, positions=None, q=None,
                       out=None, offsets=None, stream=None):
     """gmc_cache_append_rope: keys [rows, Hkv, d] turned by their positions into the cache,
@@ -708,36 +725,29 @@ def cache_append_rope(cache: KVCache, rope: Rope, k_new, v_new, T, positions=Non
     device, dtype = cache.device_index, cache.dtype
     if rope.device_index != device:
         raise GMCError("rope: its table is on the cache's device")
-    if k_new.dim() != 3 or k_new.dtype != dtype or k_new.get_device() != device:
+    if k_new.dtype != dtype or k_new.get_device() != device \
+            or (v_new is not None and (v_new.dtype != dtype or v_new.get_device() != device)):
         raise GMCError("new rows: [rows, Hkv, d] of the cache's type, on its device")
-    new_row = _rows_apart(k_new, cache._row_shape, "new rows: dense [Hkv, d] of the cache's type")
-    rows = k_new.shape[0]
-    if v_new is None:
-        if not k_new.is_contiguous():
-            raise GMCError("new rows: keys and values in one dense tensor")
-        rows //= 2
-        new_row = cache.Hkv * cache.d
-    elif v_new.shape != k_new.shape or v_new.dtype != dtype or v_new.get_device() != device \
-            or _rows_apart(v_new, cache._row_shape, "new rows: values as keys") != new_row:
-        raise GMCError("new rows: as many values as keys, alike")
-    H = q_row = out_row = 0
-    q_at = out_at = None
+    if (q is None) != (out is None):
+        raise GMCError("queries and outputs: both or neither")
+    v_at = q_at = out_at = q_key = v_key = None
+    if v_new is not None:
+        v_key, v_at = (v_new.shape, v_new.stride()), v_new.data_ptr()
     if q is not None:
-        if out is None or q.dim() != 3 or q.shape != out.shape or q.shape[0] != rows \
-                or q.dtype != dtype or out.dtype != dtype or q.get_device() != device \
+        if q.dtype != dtype or out.dtype != dtype or q.get_device() != device \
                 or out.get_device() != device:
             raise GMCError("queries and outputs: [rows, H, d] of the cache's type, on its device")
-        H = q.shape[1]
-        q_row = _rows_apart(q, (H, cache.d), "queries: dense [H, d] rows")
-        out_row = _rows_apart(out, (H, cache.d), "outputs: dense [H, d] rows")
+        q_key = (q.shape, q.stride(), out.shape, out.stride())
         q_at, out_at = q.data_ptr(), out.data_ptr()
-    elif out is not None:
-        raise GMCError("outputs without queries")
+    key = (cache._row_shape, k_new.shape, k_new.stride(), v_key, q_key)
+    layout = rope.layouts.get(key)  # of these shapes and strides: rows, gmc_rope
+    if layout is None:
+        layout = rope.layouts[key] = _rope_layout(cache, rope, k_new, v_new, q, out)
+    rows, ref = layout
     rc = lib().gmc_cache_append_rope(
-        cache.ref, rope.ref(H, q_row, out_row, new_row),
-        _int32_at(cache, positions, rope.rows * rows, "positions: dense int32, "
-                  "one (with sections three) a row"),
-        k_new.data_ptr(), None if v_new is None else v_new.data_ptr(), q_at, out_at,
+        cache.ref, ref, _int32_at(cache, positions, rope.rows * rows, "positions: dense int32, "
+                                  "one (with sections three) a row"),
+        k_new.data_ptr(), v_at, q_at, out_at,
         _int32_at(cache, offsets, cache.B + 1, "offsets: dense int32 [B + 1]"), rows, T,
         cache.stream(stream))
     if rc:
