@@ -95,7 +95,7 @@ struct EvSmem {
   int hist[2][EV_BINS * EV_COPIES];  // one is cleared while the other counts
   int list[EV_LIST];
   long long src[EV_THREADS], dst[EV_THREADS];
-  int src_z[EV_THREADS], dst_z[EV_THREADS];  // of 4 bits: from a row's codes to its scales
+  long long src_z[EV_THREADS], dst_z[EV_THREADS];  // of 4 bits: the rows' scales
   int wsum[2][EV_WARPS];
   uint32_t prefix;
   int need;
@@ -301,8 +301,8 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
       s->src[tid] = so < 0 || dto < 0 ? -1 : so * esize;
       s->dst[tid] = dto * esize;
       if constexpr (FP4) {
-        s->src_z[tid] = (int)(fp4_scale_at(a.src, from.slot) - (long long)from.slot * (a.src.d / 2));
-        s->dst_z[tid] = (int)(fp4_scale_at(a.dst, to.slot) - (long long)to.slot * (a.dst.d / 2));
+        s->src_z[tid] = so + fp4_scale_at(a.src, from.slot) - (long long)from.slot * (a.src.d / 2);
+        s->dst_z[tid] = dto + fp4_scale_at(a.dst, to.slot) - (long long)to.slot * (a.dst.d / 2);
       }
     }
     __syncthreads();
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
           const int row = y / rc, z = (y - row * rc) * 16;
           if (FP4 && z == codes * 16) {
             if (s->src[row] >= 0) {
-              const long long from = s->src[row] + s->src_z[row], to = s->dst[row] + s->dst_z[row];
+              const long long from = s->src_z[row], to = s->dst_z[row];
               for (int x = 0; x < a.src.d / 16; x += 4) {
                 *(int*)(a.dst.k + to + x) = *(const int*)(a.src.k + from + x);
                 *(int*)(a.dst.v + to + x) = *(const int*)(a.src.v + from + x);

@@ -124,7 +124,7 @@ __device__ __forceinline__ void fill_rows(const DecodeArgs& a, const Walk<32>& w
   if (in && !fixed && !there) set_status(a.c.status, CACHE_BAD);
   if (!fixed) {
     const long long part = there ? page * a.c.page_stride + w.h * a.c.head_stride : 0;
-    const long long codes = there ? part + slot * S::CB : 0;
+    const long long codes = there ? part + (long long)slot * S::CB : 0;
 #pragma unroll
     for (int pc = 0; pc < S::P; ++pc) {
       cp_async16(base + lane * S::CB + pc * 16, a.c.k + codes + pc * 16, there);
@@ -166,7 +166,8 @@ __device__ __forceinline__ void fill(const DecodeArgs& a, const Walk<32>& w, Fp4
     const long long p0 = head + x.page[0] * a.c.page_stride,
                     p1 = head + x.page[1] * a.c.page_stride;
     const int slot1 = x.slot + 16 < a.c.ps ? x.slot + 16 : 0;
-    const long long o0 = p0 + x.slot * S::CB + l16, o1 = p1 + slot1 * S::CB + l16;
+    const long long o0 = p0 + (long long)x.slot * S::CB + l16,
+                    o1 = p1 + (long long)slot1 * S::CB + l16;
 #pragma unroll
     for (int y = 0; y < STEPS; ++y) {
       cp_async16(base + l16 + y * 512, a.c.k + o0 + y * 512);
@@ -177,8 +178,8 @@ __device__ __forceinline__ void fill(const DecodeArgs& a, const Walk<32>& w, Fp4
 #pragma unroll
     for (int y = 0; y < 2 * RP; y += 32) {
       const int z = y + lane, run = z / S::SB, pc = z % S::SB;  // runs: keys' two, values' two
-      const long long o = (run & 1 ? p1 + slot1 * S::SB : p0 + x.slot * S::SB) +
-                          (long long)a.c.ps * S::CB + pc * 16;
+      const long long o = (run & 1 ? p1 : p0) +
+                          fp4_scale_at(a.c, run & 1 ? slot1 : x.slot) + pc * 16;
       if (2 * RP >= 32 || z < 2 * RP)
         cp_async16(base + S::KS + z * 16, (run & 2 ? a.c.v : a.c.k) + o);
     }
@@ -186,8 +187,8 @@ __device__ __forceinline__ void fill(const DecodeArgs& a, const Walk<32>& w, Fp4
   }
   if (!x.found) {
     const long long part = w.h * a.c.head_stride + x.page[0] * a.c.page_stride;
-    x.codes = part + x.slot * S::CB + l16;
-    x.scales = part + (long long)a.c.ps * S::CB + x.slot * S::SB + (lane & (RP - 1)) * 16;
+    x.codes = part + (long long)x.slot * S::CB + l16;
+    x.scales = part + fp4_scale_at(a.c, x.slot) + (lane & (RP - 1)) * 16;
     x.found = true;
   }
   const char *k = a.c.k + x.codes, *v = a.c.v + x.codes;

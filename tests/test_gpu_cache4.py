@@ -140,6 +140,18 @@ def test_read_of_other_caches(dtype):
             assert torch.equal(got[:74].cpu(), want) and bool((got[74:] == 7.0).all())
 
 
+def test_read_into_rows_of_16_byte_alignment():
+    C, gmc = _h(), _gmc()
+    c = C.Case4([50], 1, 1, 64, 16)
+    cache = c.cache()
+    room = torch.empty(2 * 50 * 64 + 32, dtype=torch.bfloat16, device="cuda")
+    k, v = (room[8 + i * 50 * 64:][:50 * 64].reshape(50, 1, 64) for i in range(2))
+    gmc.cache_read(cache, k, v, 50)
+    torch.cuda.synchronize()
+    assert k.data_ptr() % 32 == 16
+    assert torch.equal(k.cpu(), c.K[0]) and torch.equal(v.cpu(), c.V[0])
+
+
 def test_read_leaves_rows_it_cannot_find():
     C, gmc = _h(), _gmc()
     c = C.Case4([5], 1, 1, 64, 16)
@@ -181,17 +193,17 @@ DECODE = [
 ]
 
 
-def _decode(c, window, sinks, append, scores, **kw):
+def _decode(c, window, sinks, append, scores, max_len=None, **kw):
     gmc = _gmc()
     if append:
         for b, n in enumerate(c.lens):
             if n and int(c.table[b, (n - 1) // c.page]) < len(c.pool_k):
                 c.blank(b, n - 1)
-    cache = c.cache(max_len=min(max(c.lens) + 3, c.table.shape[1] * c.page))
+    cache = c.cache(max_len=max_len or min(max(c.lens) + 3, c.table.shape[1] * c.page))
     zero = torch.zeros(c.Hkv, c.d, dtype=torch.bfloat16)
     k = torch.stack([x[-1] if len(x) else zero for x in c.raw_K]).cuda()
     v = torch.stack([x[-1] if len(x) else zero for x in c.raw_V]).cuda()
-    places = max(c.lens) + 5
+    places = (max_len or max(c.lens)) + 5
     g = torch.Generator().manual_seed(3)
     before = torch.rand(c.B, c.Hkv, places, generator=g)
     new = torch.full((c.B, c.Hkv, places), 9.0, device="cuda")
@@ -203,16 +215,15 @@ def _decode(c, window, sinks, append, scores, **kw):
     return out, lse, before, new
 
 
-@pytest.mark.parametrize("lens,H,Hkv,d,page,window,sinks,append,scores", DECODE)
-def test_decode_matches_its_definition(lens, H, Hkv, d, page, window, sinks, append, scores):
+def _check_decode(c, window, sinks, append, scores, max_len=None):
     from tests import cache_harness as A
     C = _h()
-    c = C.Case4(lens, H, Hkv, d, page, spread=2.0)
-    out, lse, before, new = _decode(c, window, sinks, append, scores)
+    H, Hkv, d, G = c.H, c.Hkv, c.d, c.H // c.Hkv
+    out, lse, before, new = _decode(c, window, sinks, append, scores, max_len)
     torch.cuda.synchronize()
     assert int(c.status.item()) == 0
-    G = H // Hkv
-    for b, n in enumerate(lens):
+    new, dk, dv = new.cpu(), c.dk.cpu(), c.dv.cpu()
+    for b, n in enumerate(c.lens):
         ref, z, w, bound, size = A.attention(c.K[b], c.V[b], c.q[b], n - 1, window, sinks)
         tol = C.tolerance(c, size)
         small = 2.0 ** -25 * c.V[b].double().abs().sum(0).repeat_interleave(G, 0)  # tiny weights
@@ -230,8 +241,41 @@ def test_decode_matches_its_definition(lens, H, Hkv, d, page, window, sinks, app
                    A.lse_tolerance(d, size) * 8, "scores")
             assert bool((new[b, :, n:] == 9.0).all())
         if append:
-            for pool, raw in ((c.dk, c.raw_K), (c.dv, c.raw_V)):
-                C.same_rows(c.rows(pool.cpu(), b, [n - 1]), C.pack(raw[b][-1:]), "appended")
+            for pool, raw in ((dk, c.raw_K), (dv, c.raw_V)):
+                C.same_rows(c.rows(pool, b, [n - 1]), C.pack(raw[b][-1:]), "appended")
+
+
+@pytest.mark.parametrize("lens,H,Hkv,d,page,window,sinks,append,scores", DECODE)
+def test_decode_matches_its_definition(lens, H, Hkv, d, page, window, sinks, append, scores):
+    c = _h().Case4(lens, H, Hkv, d, page, spread=2.0)
+    _check_decode(c, window, sinks, append, scores)
+
+
+@pytest.mark.parametrize("lens,H,Hkv,d,page,window,sinks,append,scores", DECODE)
+def test_decode_with_room(lens, H, Hkv, d, page, window, sinks, append, scores):
+    """Short sequences in a cache with room for long ones: stretches of the batch, joined."""
+    width = -(-6000 // page)
+    c = _h().Case4(lens, H, Hkv, d, page, spread=2.0, width=width)
+    _check_decode(c, window, sinks, append, scores, max_len=width * page)
+
+
+@pytest.mark.parametrize("B,H,Hkv,d,page,window,sinks,append,scores", [
+    (90, 8, 4, 64, 16, 0, 0, True, True),        # two or three pairs a block
+    (300, 8, 4, 64, 32, 0, 0, True, False),      # many pairs a block, runs across their borders
+    (260, 6, 6, 128, 16, 0, 0, False, True),
+    (200, 9, 1, 256, 48, 40, 2, True, True),     # two launches
+    (64, 3, 3, 64, 7, 33, 5, True, True)])
+def test_decode_of_many_sequences(B, H, Hkv, d, page, window, sinks, append, scores):
+    lens = [(17 * b * b + 5 * b) % 131 for b in range(B)]  # some of none
+    c = _h().Case4(lens, H, Hkv, d, page, spread=2.0)
+    _check_decode(c, window, sinks, append, scores)
+
+
+@pytest.mark.parametrize("window,sinks", [(2 ** 30, 3), (2 ** 31 - 1, 2 ** 31 - 1), (40, 2 ** 30),
+                                          (31, 32), (32, 31), (64, 64), (33, 33)])
+def test_decode_windows_and_sinks_at_the_borders_of_turns(window, sinks):
+    c = _h().Case4([700, 64, 65, 1], 4, 2, 128, 32, spread=2.0)
+    _check_decode(c, window, sinks, True, True)
 
 
 def test_decode_of_hard_queries():
@@ -293,6 +337,7 @@ ATTEND = [
     ([700], [2], 7, 1, 128, 64, 1, 0),
     ([200, 140], [90, 20], 2, 1, 256, 16, 70, 2),
     ([2000], [5], 4, 2, 128, 64, 0, 0),
+    ([130, 0, 4], [2, 0, 6], 4, 2, 128, 16, 0, 0),  # more new tokens than tokens: queries before
 ]
 
 
@@ -326,8 +371,33 @@ def test_attend_matches_its_definition(lens, news, H, Hkv, d, page, window, sink
                                                  sinks)
             _close(out[at + x], ref, bound, A.tolerance(c.dt, d, size, roundings=2),
                    f"sequence {b}, new token {x}")
+            if n - t + x < 0:
+                assert bool((lse[at + x] == -math.inf).all())
+                continue
             _close(lse[at + x], z, torch.ones_like(z), A.lse_tolerance(d, size) * 4, "lse")
         at += t
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 3)])
+def test_attend_of_one_token_a_sequence(window, sinks):
+    """Without offsets it goes the way of decode."""
+    from tests import cache_harness as A
+    C, gmc = _h(), _gmc()
+    c = C.Case4([500, 1, 0, 2000], 14, 2, 128, 64, spread=2.0)
+    cache, q = c.cache(), c.q.cuda()
+    out, lse = torch.empty_like(q), torch.empty(4, 14, device="cuda")
+    gmc.attend(cache, q, out, 1, window=window, sinks=sinks, lse=lse)
+    torch.cuda.synchronize()
+    assert int(c.status.item()) == 0
+    for b, n in enumerate(c.lens):
+        ref, z, _, bound, size = A.attention(c.K[b], c.V[b], c.q[b], n - 1, window, sinks)
+        tol = C.tolerance(c, size)
+        small = 2.0 ** -25 * c.V[b].double().abs().sum(0).repeat_interleave(7, 0)
+        _close(out[b], ref, bound + small / tol, tol, f"sequence {b}")
+        if n:
+            _close(lse[b], z, torch.ones_like(z), A.lse_tolerance(128, size) * 4, "lse")
+        else:
+            assert bool((lse[b] == -math.inf).all())
 
 
 def test_attend_equals_attend_of_the_unpacked_cache():
