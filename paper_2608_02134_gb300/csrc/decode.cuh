@@ -455,12 +455,13 @@ __global__ void __launch_bounds__(JN_THREADS) k_decode_join(DecodeArgs a, int W,
   add_scores(a, w, fin, x0 + threadIdx.x, blocks * JN_THREADS);
 }
 // Query heads of a launch; key heads that have more take one launch after another.
-inline int heads_per_launch(int dtype, int G) {
-  return dtype == GMC_BF16 ? std::min(G, 16) : dtype == GMC_FP4 || G > 4 ? std::min(G, 8) : G;
+inline int heads_per_launch(int dtype, int G, int d) {
+  if (dtype == GMC_FP4) return std::min(G, d > 128 ? 8 : 16);
+  return dtype == GMC_BF16 ? std::min(G, 16) : G > 4 ? std::min(G, 8) : G;
 }
 // Floats of a key's logits: whole 16-byte pieces, as many as rows hold them.
-inline int logit_heads(int dtype, int G) {
-  const int h = heads_per_launch(dtype, G);
+inline int logit_heads(int dtype, int G, int d) {
+  const int h = heads_per_launch(dtype, G, d);
   return h > 8 ? 16 : h > 4 ? 8 : h > 2 ? 4 : h;
 }
 inline int decode_dp(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
@@ -473,7 +474,7 @@ struct DecodeWs {
   size_t ml, part, logits, all;
 };
 inline DecodeWs decode_carve(const KV& c, int dtype, int H) {
-  const int G = H / c.Hkv, heads = heads_per_launch(dtype, G);
+  const int G = H / c.Hkv, heads = heads_per_launch(dtype, G, c.d);
   const size_t pairs = (size_t)c.B * c.Hkv, parts = pairs + (size_t)sm_count() * decode_warps(dtype);
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   DecodeWs w;
@@ -481,7 +482,7 @@ inline DecodeWs decode_carve(const KV& c, int dtype, int H) {
   w.part = up(parts * heads * 8);
   w.logits = w.part + up(parts * heads * decode_dp(c.d) * 4);
   const int turn = decode_turn(dtype);
-  w.all = w.logits + pairs * logit_heads(dtype, G) * 4 * (size_t)(ceil_div(c.cap, turn) * turn);
+  w.all = w.logits + pairs * logit_heads(dtype, G, c.d) * 4 * (size_t)(ceil_div(c.cap, turn) * turn);
   return w;
 }
 // kernels: a CTA a pair, and equal stretches.

@@ -536,12 +536,12 @@ cudaError_t decode_f32(int heads, const DecodeArgs& a, cudaStream_t st, int* lau
 size_t decode_workspace(const KV& c, int dtype, int H) { return decode_carve(c, dtype, H).all; }
 
 cudaError_t launch_decode(DecodeArgs a, int dtype, void* ws, cudaStream_t st, int* launches) {
-  const int hm = heads_per_launch(dtype, a.G), dp = decode_dp(a.c.d);
+  const int hm = heads_per_launch(dtype, a.G, a.c.d), dp = decode_dp(a.c.d);
   const DecodeWs w = decode_carve(a.c, dtype, a.H);
   a.ml = reinterpret_cast<float2*>((char*)ws + w.ml);
   a.part = reinterpret_cast<float*>((char*)ws + w.part);
   a.logits = reinterpret_cast<float*>((char*)ws + w.logits);
-  a.hs = logit_heads(dtype, a.G);
+  a.hs = logit_heads(dtype, a.G, a.c.d);
   const int turn = decode_turn(dtype);
   a.places = ceil_div(a.c.cap, turn) * turn;
   const long long esize = dtype == GMC_FP4 ? 1 : dtype == GMC_BF16 ? 2 : 4;

@@ -5,7 +5,8 @@
 // leave a key 6 clocks of an SM, so instructions are the second bound: codes go from shared
 // memory to the tensor cores' operands in registers, without a tile of values in between.
 //
-//   S = K q^T: the rows of mma m16n8k16 are 16 keys, its columns up to 8 query heads.  A
+//   S = K q^T: the rows of mma m16n8k16 are 16 keys, its columns up to 8 query heads (of 9 to 16
+//   with d <= 128 a second product takes the same fragments).  A
 //   product sums over channels in any order, so a thread takes the fragments of a row from
 //   d / 4 consecutive channels: two bytes a step, one conversion a pair, one product a pair
 //   with the block's scale.  Values and q are exact in half precision: the row of q is
@@ -208,58 +209,62 @@ __device__ __forceinline__ void fill(const DecodeArgs& a, const Walk<32>& w, Fp4
   --x.more;
 }
 
-template <int DP> struct HeadsFp4 {
-  static constexpr int HM = 8;
+// NT x 8 query heads.
+template <int DP, int NT> struct HeadsFp4 {
+  static constexpr int HM = 8 * NT;
   typedef __nv_bfloat16 T;
   typedef Fp4Stage<DP> S;
   static constexpr int CT = DP / 4;  // channels of a thread in a key
   static constexpr int CV = DP / 8;  // and in a value
-  // Lane (g, t) = (lane / 4, lane % 4).  qf: head g, channels t CT ..; o: heads 2t and 2t + 1,
-  // channels g CV .. in pairs.
-  uint32_t qf[DP / 16][2];
-  float o[DP / 16][4], m[2], l[2], factor[2], room[2];
+  // Lane (g, t) = (lane / 4, lane % 4).  Of eight heads qf: head g, channels t CT ..; o: heads 2t
+  // and 2t + 1, channels g CV .. in pairs.
+  uint32_t qf[NT][DP / 16][2];
+  float o[NT][DP / 16][4], m[NT][2], l[NT][2], factor[NT][2], room[NT][2];
   __device__ __forceinline__ void begin(const DecodeArgs& a, const Walk<32>& w, int lane) {
-    const int g = lane >> 2, t = lane & 3;
-    uint2 raw[DP / 16];
-    const T* q = reinterpret_cast<const T*>(a.q) + w.b * a.q_row +
-                 (long long)(w.h * a.G + a.h0 + min(g, a.heads - 1)) * a.q_head + t * CT;
-    uint32_t top = 0;
 #pragma unroll
-    for (int s = 0; s < DP / 16; s += 2) {
-      const uint4 v = *reinterpret_cast<const uint4*>(q + s * 4);
-      raw[s] = make_uint2(v.x, v.y);
-      raw[s + 1] = make_uint2(v.z, v.w);
-      const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+    for (int z = 0; z < NT; ++z) {
+      const int g = (lane >> 2) + 8 * z, t = lane & 3;
+      uint2 raw[DP / 16];
+      const T* q = reinterpret_cast<const T*>(a.q) + w.b * a.q_row +
+                   (long long)(w.h * a.G + a.h0 + min(g, a.heads - 1)) * a.q_head + t * CT;
+      uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        top = max(top, max(y[i] & 0x7fffu, (y[i] >> 16) & 0x7fffu));
+      for (int s = 0; s < DP / 16; s += 2) {
+        const uint4 v = *reinterpret_cast<const uint4*>(q + s * 4);
+        raw[s] = make_uint2(v.x, v.y);
+        raw[s + 1] = make_uint2(v.z, v.w);
+        const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          top = max(top, max(y[i] & 0x7fffu, (y[i] >> 16) & 0x7fffu));
+      }
+      top = max(top, __shfl_xor_sync(FULL, top, 1));
+      top = max(top, __shfl_xor_sync(FULL, top, 2));
+      // 2^k that puts the largest magnitude into [2^14, 2^15); none for zeros and what is not
+      // finite
+      const int e = (int)(top >> 7) - 127;
+      const int k = top == 0 || top >= 0x7f80u ? 0 : min(14 - e, 126);
+      const float up = __uint_as_float((uint32_t)(k + 127) << 23);
+#pragma unroll
+      for (int s = 0; s < DP / 16; ++s) {
+        const uint32_t y[2] = {raw[s].x, raw[s].y};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          qf[z][s][i] = g < a.heads ? pack_half(__uint_as_float(y[i] << 16) * up,
+                                                __uint_as_float(y[i] & 0xffff0000u) * up)
+                                    : 0u;
+      }
+      // logits are multiplied by the scale and 2^-k of their heads
+      const float down = fmaxf(a.scale2 * __uint_as_float((uint32_t)(127 - k) << 23), 1e-37f);
+      factor[z][0] = __shfl_sync(FULL, down, t * 8);
+      factor[z][1] = __shfl_sync(FULL, down, t * 8 + 4);
+#pragma unroll
+      for (int x = 0; x < DP / 16; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) o[z][x][y] = 0.f;
+      m[z][0] = m[z][1] = room[z][0] = room[z][1] = -INFINITY;
+      l[z][0] = l[z][1] = 0.f;
     }
-    top = max(top, __shfl_xor_sync(FULL, top, 1));
-    top = max(top, __shfl_xor_sync(FULL, top, 2));
-    // 2^k that puts the largest magnitude into [2^14, 2^15); none for zeros and what is not
-    // finite
-    const int e = (int)(top >> 7) - 127;
-    const int k = top == 0 || top >= 0x7f80u ? 0 : min(14 - e, 126);
-    const float up = __uint_as_float((uint32_t)(k + 127) << 23);
-#pragma unroll
-    for (int s = 0; s < DP / 16; ++s) {
-      const uint32_t y[2] = {raw[s].x, raw[s].y};
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        qf[s][i] = g < a.heads ? pack_half(__uint_as_float(y[i] << 16) * up,
-                                           __uint_as_float(y[i] & 0xffff0000u) * up)
-                               : 0u;
-    }
-    // logits are multiplied by the scale and 2^-k of their heads
-    const float down = fmaxf(a.scale2 * __uint_as_float((uint32_t)(127 - k) << 23), 1e-37f);
-    factor[0] = __shfl_sync(FULL, down, t * 8);
-    factor[1] = __shfl_sync(FULL, down, t * 8 + 4);
-#pragma unroll
-    for (int x = 0; x < DP / 16; ++x)
-#pragma unroll
-      for (int y = 0; y < 4; ++y) o[x][y] = 0.f;
-    m[0] = m[1] = room[0] = room[1] = -INFINITY;
-    l[0] = l[1] = 0.f;
   }
   // The key's codes and scales of a thread: CT / 8 words, CT / 16 scales.
   static __device__ __forceinline__ void load_key(uint32_t stage, int row, int t, uint32_t* w,
@@ -292,11 +297,12 @@ template <int DP> struct HeadsFp4 {
     const uint32_t stage = tc::smem_u32(from);
     const int g = lane >> 2, t = lane & 3;
     const int kg = key_of_row<DP>(g), k0 = key_of_row<DP>(2 * t), k1 = key_of_row<DP>(2 * t + 1);
-    float s[2][4];  // keys kg and kg + 8 of two groups of 16
+    float s[NT][2][4];  // keys kg and kg + 8 of two groups of 16
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      float* d = s[n];
-      d[0] = d[1] = d[2] = d[3] = 0.f;
+#pragma unroll
+      for (int z = 0; z < NT; ++z)
+        s[z][n][0] = s[z][n][1] = s[z][n][2] = s[z][n][3] = 0.f;
       uint32_t w0[CT / 8], w1[CT / 8], s0[CT / 16], s1[CT / 16];
       load_key(stage, n * 16 + kg, t, w0, s0);
       load_key(stage, n * 16 + kg + 8, t, w1, s1);
@@ -309,7 +315,9 @@ template <int DP> struct HeadsFp4 {
         for (int j = 0; j < 2; ++j) {
           const uint32_t x[4] = {hmul2(h0[2 * j], s0[i / 2]), hmul2(h1[2 * j], s1[i / 2]),
                                  hmul2(h0[2 * j + 1], s0[i / 2]), hmul2(h1[2 * j + 1], s1[i / 2])};
-          mma_f16(d, x, qf[2 * i + j][0], qf[2 * i + j][1]);
+#pragma unroll
+          for (int z = 0; z < NT; ++z)
+            mma_f16(s[z][n], x, qf[z][2 * i + j][0], qf[z][2 * i + j][1]);
         }
       }
     }
@@ -320,71 +328,93 @@ template <int DP> struct HeadsFp4 {
         for (int y = 0; y < 4; ++y) {
           const int x = w.t * 32 + n * 16 + (y >> 1) * 8 + kg;
           if (x >= w.nv || !sees(w.n - 1, w.seen.place(x), a.window, a.sinks))
-            s[n][y] = -INFINITY;
+#pragma unroll
+            for (int z = 0; z < NT; ++z) s[z][n][y] = -INFINITY;
         }
     }
     if (a.scores) {
-      float* lg = logits_of(a, w) + kg * a.hs + t * 2;
+#pragma unroll
+      for (int z = 0; z < NT; ++z) {
+        const int head = 8 * z + t * 2;
+        float* lg = logits_of(a, w) + kg * a.hs + head;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            float* to = lg + (n * 16 + y * 8) * a.hs;
+            const float x0 = s[z][n][2 * y] * factor[z][0],
+                        x1 = s[z][n][2 * y + 1] * factor[z][1];
+            if (head + 1 < a.hs)
+              *reinterpret_cast<float2*>(to) = make_float2(x0, x1);
+            else if (head < a.hs)
+              *to = x0;
+          }
+      }
+    }
+    // the maximum that weights are taken against follows the running one when that has grown
+    // by 2^8 (`room`: that much more as a sum of products): lanes only meet then
+    float top[NT][2];
+    bool grew = false;
+#pragma unroll
+    for (int z = 0; z < NT; ++z)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        top[z][r] = fmaxf(fmaxf(s[z][0][r], s[z][0][2 + r]), fmaxf(s[z][1][r], s[z][1][2 + r]));
+        grew |= top[z][r] > room[z][r];
+      }
+    if (__any_sync(FULL, grew)) {
+#pragma unroll
+      for (int z = 0; z < NT; ++z)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float mn = fmaxf(top[z][r] * factor[z][r], m[z][r]);
+          mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 4));
+          mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 8));
+          mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 16));
+          const float f = exp2_fast(m[z][r] - (mn == -INFINITY ? 0.f : mn));
+          l[z][r] *= f;
+#pragma unroll
+          for (int y = 0; y < DP / 16; ++y) {
+            o[z][y][r] *= f;
+            o[z][y][2 + r] *= f;
+          }
+          m[z][r] = mn;
+          room[z][r] = (mn + 8.f) / factor[z][r];
+        }
+    }
+    uint32_t p[NT][2][2];  // weights: of group n the first and the second eight keys'
+#pragma unroll
+    for (int z = 0; z < NT; ++z) {
+      const f32x2 scale = pair(factor[z][0], factor[z][1]),
+                  off = pair(m[z][0] == -INFINITY ? 0.f : -m[z][0],
+                             m[z][1] == -INFINITY ? 0.f : -m[z][1]);
+      f32x2 sum = pair(l[z][0], l[z][1]);
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          float* z = lg + (n * 16 + y * 8) * a.hs;
-          const float x0 = s[n][2 * y] * factor[0], x1 = s[n][2 * y + 1] * factor[1];
-          if (t * 2 + 1 < a.hs)
-            *reinterpret_cast<float2*>(z) = make_float2(x0, x1);
-          else if (t * 2 < a.hs)
-            *z = x0;
+          const float2 x =
+              unpair(fma2(pair(s[z][n][2 * y], s[z][n][2 * y + 1]), scale, off));
+          const float p0 = exp2_fast(x.x), p1 = exp2_fast(x.y);
+          sum = add2(sum, pair(p0, p1));
+          p[z][n][y] = transpose8(pack_half(p0, p1));
         }
+      const float2 all = unpair(sum);
+      l[z][0] = all.x;
+      l[z][1] = all.y;
     }
-    // the maximum that weights are taken against follows the running one when that has grown
-    // by 2^8 (`room`: that much more as a sum of products): lanes only meet then
-    float top[2];
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-      top[r] = fmaxf(fmaxf(s[0][r], s[0][2 + r]), fmaxf(s[1][r], s[1][2 + r]));
-    if (__any_sync(FULL, top[0] > room[0] || top[1] > room[1])) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        float mn = fmaxf(top[r] * factor[r], m[r]);
-        mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 4));
-        mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 8));
-        mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 16));
-        const float f = exp2_fast(m[r] - (mn == -INFINITY ? 0.f : mn));
-        l[r] *= f;
-#pragma unroll
-        for (int y = 0; y < DP / 16; ++y) {
-          o[y][r] *= f;
-          o[y][2 + r] *= f;
-        }
-        m[r] = mn;
-        room[r] = (mn + 8.f) / factor[r];
-      }
-    }
-    const f32x2 scale = pair(factor[0], factor[1]),
-                off = pair(m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]);
-    f32x2 sum = pair(l[0], l[1]);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-#pragma unroll
-      for (int y = 0; y < 4; y += 2) {
-        const float2 x = unpair(fma2(pair(s[n][y], s[n][y + 1]), scale, off));
-        s[n][y] = exp2_fast(x.x);
-        s[n][y + 1] = exp2_fast(x.y);
-        sum = add2(sum, pair(s[n][y], s[n][y + 1]));
-      }
-      const uint32_t p0 = transpose8(pack_half(s[n][0], s[n][1]));
-      const uint32_t p1 = transpose8(pack_half(s[n][2], s[n][3]));
-      // values of keys k0, k1 (the k of p0) and k0 + 8, k1 + 8 (of p1)
-      uint32_t v[4][CV / 8], z[4];
+      // values of keys k0, k1 (the k of p[.][n][0]) and k0 + 8, k1 + 8 (of p[.][n][1])
+      uint32_t v[4][CV / 8], z4[4];
 #pragma unroll
       for (int y = 0; y < 4; ++y)
-        load_value(stage, n * 16 + (y >> 1) * 8 + (y & 1 ? k1 : k0), g, v[y], &z[y]);
+        load_value(stage, n * 16 + (y >> 1) * 8 + (y & 1 ? k1 : k0), g, v[y], &z4[y]);
 #pragma unroll
       for (int i = 0; i < CV / 8; ++i) {
         const int sh = DP == 256 ? (i >> 1) * 8 : 0;
-        const uint32_t s0 = fp4_scales((z[0] >> sh) & 0xffu, (z[1] >> sh) & 0xffu),
-                       s1 = fp4_scales((z[2] >> sh) & 0xffu, (z[3] >> sh) & 0xffu);
+        const uint32_t s0 = fp4_scales((z4[0] >> sh) & 0xffu, (z4[1] >> sh) & 0xffu),
+                       s1 = fp4_scales((z4[2] >> sh) & 0xffu, (z4[3] >> sh) & 0xffu);
         constexpr uint32_t LO = 0x0f0f0f0fu;
         uint32_t h[4][4];  // even and odd channels of the first pair of keys, of the second
         fp4_halves((v[0][i] & LO) | ((v[1][i] << 4) & ~LO), h[0]);
@@ -395,31 +425,31 @@ template <int DP> struct HeadsFp4 {
         for (int j = 0; j < 4; ++j) {
           const uint32_t x[4] = {hmul2(h[0][j], s0), hmul2(h[1][j], s0), hmul2(h[2][j], s1),
                                  hmul2(h[3][j], s1)};
-          mma_f16(o[i * 4 + j], x, p0, p1);
+#pragma unroll
+          for (int z = 0; z < NT; ++z) mma_f16(o[z][i * 4 + j], x, p[z][n][0], p[z][n][1]);
         }
       }
     }
-    const float2 all = unpair(sum);
-    l[0] = all.x;
-    l[1] = all.y;
   }
   // Maxima and sums, and the unnormalised output rows [heads][DP].
   __device__ __forceinline__ void leave(const DecodeArgs& a, float2* ml, float* out, int lane) {
     const int g = lane >> 2, t = lane & 3;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      l[r] += __shfl_xor_sync(FULL, l[r], 4);
-      l[r] += __shfl_xor_sync(FULL, l[r], 8);
-      l[r] += __shfl_xor_sync(FULL, l[r], 16);
-      const int head = t * 2 + r;
-      if (head < a.heads) {
-        if (g == 0) ml[head] = make_float2(m[r], l[r]);
+    for (int z = 0; z < NT; ++z)
 #pragma unroll
-        for (int x = 0; x < DP / 16; ++x)
-          *reinterpret_cast<float2*>(out + head * DP + g * CV + x * 2) =
-              make_float2(o[x][r], o[x][2 + r]);
+      for (int r = 0; r < 2; ++r) {
+        l[z][r] += __shfl_xor_sync(FULL, l[z][r], 4);
+        l[z][r] += __shfl_xor_sync(FULL, l[z][r], 8);
+        l[z][r] += __shfl_xor_sync(FULL, l[z][r], 16);
+        const int head = 8 * z + t * 2 + r;
+        if (head < a.heads) {
+          if (g == 0) ml[head] = make_float2(m[z][r], l[z][r]);
+#pragma unroll
+          for (int x = 0; x < DP / 16; ++x)
+            *reinterpret_cast<float2*>(out + head * DP + g * CV + x * 2) =
+                make_float2(o[z][x][r], o[z][x][2 + r]);
+        }
       }
-    }
   }
   // The appended row goes to its page, as it was packed: the warp that has the pair's last turn.
   static __device__ __forceinline__ void append(const DecodeArgs& a, const Walk<32>& w,
@@ -453,14 +483,14 @@ template <int DP> struct HeadsFp4 {
 // it joins its warps' parts: they are balanced whatever the borders, and few are left.  (A pair's
 // turns shared out among all warps, pair after pair, took 28.7 us for 8 x 16,005 keys: a border
 // costs a barrier, and the parts' rounding up.)  OWN: a CTA takes a whole pair, and no other.
-template <int DP, int W, int NST, bool OWN>
+template <int DP, int NT, int W, int NST, bool OWN>
 __global__ void __launch_bounds__(W * 32, 1) k_decode_fp4(DecodeArgs a) {
-  typedef HeadsFp4<DP> H;
+  typedef HeadsFp4<DP, NT> H;
   typedef typename H::T T;
   typedef Fp4Stage<DP> S;
   constexpr int HM = H::HM, ROWS = HM * DP * 4, SLOTS = W + 2;  // bytes of a part, parts
   extern __shared__ __align__(512) char smem[];
-  __shared__ float2 fin[OWN ? 8 : 1];
+  __shared__ float2 fin[OWN ? HM : 1];
   char* rows = smem + W * NST * S::BYTES;                       // [SLOTS][HM][DP]
   float2* ml = reinterpret_cast<float2*>(rows + SLOTS * ROWS);  // [SLOTS][HM]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -557,26 +587,29 @@ __global__ void __launch_bounds__(W * 32, 1) k_decode_fp4(DecodeArgs a) {
   }
 }
 
-template <int DP, int W, int NST>
+template <int DP, int NT, int W, int NST>
 cudaError_t decode_fp4_go(const DecodeArgs& a, cudaStream_t st, int* launches) {
   static_assert(W <= 16, "the workspace holds a part a warp");
-  constexpr size_t smem =
-      (size_t)W * NST * Fp4Stage<DP>::BYTES + (size_t)(W + 2) * (8 * DP * 4 + 8 * sizeof(float2));
+  constexpr size_t smem = (size_t)W * NST * Fp4Stage<DP>::BYTES +
+                          (size_t)(W + 2) * 8 * NT * (DP * 4 + sizeof(float2));
   static_assert(smem <= 226 * 1024, "shared memory of a CTA");
   // own pairs, with 128 channels and 4 key heads: 32 sequences of 512 keys and scores 8.2 us, in
   // stretches 14.0; of up to 3,000 25.7 and 27.6; 20 of 4,000 21.7 and 21.2.  One of 322 keys 5.6
   // and 9.7, of 1,500 9.9 and 11.8; two of 3,000 15.5 and 14.7.
-  return decode_launch<__nv_bfloat16, 32, DP, W>(a, k_decode_fp4<DP, W, NST, true>,
-                                                 k_decode_fp4<DP, W, NST, false>,
+  return decode_launch<__nv_bfloat16, 32, DP, W>(a, k_decode_fp4<DP, NT, W, NST, true>,
+                                                 k_decode_fp4<DP, NT, W, NST, false>,
                                                  OwnTurns{8 * 12 / W, 4 * 12 / W}, smem, st, launches);
 }
 
 }  // namespace
 
 cudaError_t launch_decode_fp4(const DecodeArgs& a, cudaStream_t st, int* launches) {
-  return a.c.d == 64    ? decode_fp4_go<64, 12, 4>(a, st, launches)
-         : a.c.d == 128 ? decode_fp4_go<128, 12, 2>(a, st, launches)
-                        : decode_fp4_go<256, 6, 2>(a, st, launches);
+  if (a.heads > 8)
+    return a.c.d == 64 ? decode_fp4_go<64, 2, 12, 4>(a, st, launches)
+                       : decode_fp4_go<128, 2, 8, 3>(a, st, launches);
+  return a.c.d == 64    ? decode_fp4_go<64, 1, 12, 4>(a, st, launches)
+         : a.c.d == 128 ? decode_fp4_go<128, 1, 12, 2>(a, st, launches)
+                        : decode_fp4_go<256, 1, 6, 2>(a, st, launches);
 }
 
 }  // namespace gmc

@@ -187,6 +187,9 @@ DECODE = [
     ([1999], 16, 1, 64, 64, 300, 17, True, True),
     ([1500, 40], 11, 1, 256, 32, 64, 3, True, True),
     ([600], 40, 1, 128, 128, 1, 0, True, True),
+    ([700, 90], 18, 2, 128, 16, 0, 0, True, True),
+    ([700, 90], 32, 2, 128, 64, 100, 5, False, True),
+    ([500, 33, 64], 26, 2, 64, 16, 0, 0, True, True),
     ([600, 599], 3, 3, 64, 16, 33, 0, False, True),
     ([6000], 2, 1, 128, 256, 0, 0, False, True),
     ([5000, 1, 2500], 7, 1, 64, 64, 4096, 4, True, False),
