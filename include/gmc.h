@@ -547,9 +547,11 @@ int gmc_clients(const gmc_problem* prob, const gmc_params* params, const gmc_vie
  * bytes; slot_stride is 0; the parts must not overlap (GMC_ERR_ARG).
  * gmc_cache_append, gmc_cache_append_rope and gmc_decode pack what they append;
  * all attention is over the values that the codes stand for, a decoded token's
- * own included.  gmc_attend unpacks the seen rows to bf16 (which holds them
- * exactly) in its workspace, which grows by B * cap * Hkv * d * 4 bytes, cap being
- * max_len rounded up to 128.
+ * own included.  Its products are exact in half precision (queries within 2^-39
+ * of their row's largest value), weights are rounded to half.  gmc_attend reads
+ * the codes itself for few tokens; for more it unpacks the seen rows to bf16 (which
+ * holds them exactly) in its workspace, which grows by B * cap * Hkv * d * 4 bytes,
+ * cap being max_len rounded up to 128, and goes on as with bf16 (d = 256: always).
  */
 typedef struct gmc_kv_cache {
   int B;                     /* sequences, >= 1 */
@@ -577,7 +579,7 @@ typedef struct gmc_kv_cache {
  * head h / (H / Hkv).  Products accumulate in fp32, softmax statistics are
  * fp32; on bf16 caches with d <= 128 and pages of a multiple of 8 slots gmc_attend
  * rounds the weights to bf16 for their product with v (its other forms and
- * gmc_decode do not).  Keys and values that a query does not
+ * gmc_decode do not; of GMC_FP4 see there).  Keys and values that a query does not
  * see do not reach its output, whatever they hold, and pages of which no query
  * of the call sees a key are not looked up: a program that gives back the pages
  * behind its window may leave anything in the table.
@@ -668,8 +670,9 @@ size_t gmc_cache4_part_size(int page_size, int d);
  * of 8 slots, run on the tcgen05 tensor cores, the others on the CUDA cores.  The
  * bf16 kernel takes whole pages into turns of 128 keys: pages of 8, 16, 32, 64 or a
  * multiple of 128 slots fill them, others leave a part of each turn idle (48 slots
- * a quarter).  One launch, or two where the key axis is split.  No score is added
- * to: only gmc_decode does that.
+ * a quarter).  One launch, or two where the key axis is split (of GMC_FP4 one more
+ * where rows are unpacked; one token a sequence without q_offsets goes the way of
+ * gmc_decode).  No score is added to: only gmc_decode does that.
  */
 size_t gmc_attend_workspace_size(const gmc_kv_cache* cache, int H, int T);
 int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
@@ -690,7 +693,8 @@ int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,
  *               `scores` itself; both or neither are NULL.
  * out does not overlap q.  A sequence of no tokens gets out = 0 and lse = -inf, and
  * nothing is appended to it.  One launch where max_len is short, two otherwise (for
- * every 16 query heads of a key head with bf16, 8 with fp32).  The workspace has
+ * every 16 query heads of a key head with bf16 and GMC_FP4, 8 with fp32 or d = 256
+ * of GMC_FP4).  The workspace has
  * room for the logits of scores, with or without them.
  * A page's rows must lie within 64 GB (GMC_ERR_UNSUPPORTED).
  */

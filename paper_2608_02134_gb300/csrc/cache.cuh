@@ -206,6 +206,8 @@ cudaError_t launch_attend_f32(const AttnArgs&, cudaStream_t);
 cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t);  // of part and ml
 cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t, int* launches);
 size_t attend_fp4_workspace(const KV&, int H, int T);
+int attend_direct_splits(const KV&, int G, int T);
+cudaError_t launch_attend_direct(const AttnArgs&, cudaStream_t);
 cudaError_t launch_attend_fp4(AttnArgs a, void* ws, cudaStream_t, int* launches);
 
 struct DecodeArgs {

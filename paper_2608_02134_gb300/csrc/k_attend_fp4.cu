@@ -99,12 +99,46 @@ Unpacked unpacked(const KV& c) {
 }
 }  // namespace
 
+namespace {
+// Whether the attending kernel reads the codes itself (k_attend_fp4_tc.cu).  It takes about 1 us
+// for a turn of 64 keys of one of its tiles; unpacking takes 1.1 us for every 64 keys and half
+// of that time for a turn, and 5 us more for its launch.  28 query and 4 key heads of 128, us so
+// and so: 8 x 16,004 keys and 16 tokens (one tile) 67 and 113, 32 tokens 124 and 132, 64 (four
+// tiles) 229 and 185; 8 x 2,000 and 64 tokens 35 and 42, 128 tokens 69 and 44; one sequence of
+// 16,004 and 64 tokens 37 and 40, 128 tokens 66 and 50; of 2,000 and 256 tokens (15 tiles) 26
+// and 26.5.
+bool direct(const KV& c, int G, int T) {
+  if (c.d > 128) return false;
+  const long long tiles = ceil_div(T, 128 / G);
+  const long long load = (long long)c.B * c.Hkv * tiles * ceil_div(c.cap, 64) / sm_count();
+  return load * (9 * tiles - 22) < 100 * tiles;
+}
+}  // namespace
+
 size_t attend_fp4_workspace(const KV& c, int H, int T) {
+  if (direct(c, H / c.Hkv, T)) {
+    const int s = attend_direct_splits(c, H / c.Hkv, T);
+    const size_t rows = (size_t)c.B * T * H * s;
+    return s == 1 ? 256 : 256 + ((rows * 8 + 255) & ~(size_t)255) + rows * c.d * 4;
+  }
   const Unpacked u = unpacked(c);
   return u.all + attend_workspace(u.c, GMC_BF16, H, T);
 }
 
 cudaError_t launch_attend_fp4(AttnArgs a, void* ws, cudaStream_t st, int* launches) {
+  if (direct(a.c, a.G, a.T)) {
+    a.splits = attend_direct_splits(a.c, a.G, a.T);
+    if (a.splits > 1) {
+      const size_t rows = (size_t)a.c.B * a.T * a.H * a.splits;
+      a.ml = reinterpret_cast<float2*>(ws);
+      a.part = reinterpret_cast<float*>((char*)ws + ((rows * 8 + 255) & ~(size_t)255));
+    }
+    cudaError_t e = launch_attend_direct(a, st);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    if (a.splits > 1 && (e = launch_attend_join(a, GMC_BF16, st)) == cudaSuccess) ++*launches;
+    return e;
+  }
   Unpacked u = unpacked(a.c);
   u.c.table = reinterpret_cast<int32_t*>(ws);
   u.c.k = (char*)ws + u.table;

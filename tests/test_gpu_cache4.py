@@ -341,6 +341,11 @@ ATTEND = [
     ([200, 140], [90, 20], 2, 1, 256, 16, 70, 2),
     ([2000], [5], 4, 2, 128, 64, 0, 0),
     ([130, 0, 4], [2, 0, 6], 4, 2, 128, 16, 0, 0),  # more new tokens than tokens: queries before
+    ([3000, 2999], [20, 1], 28, 4, 128, 64, 0, 0),   # two tiles, the key axis in parts
+    ([1500], [40], 32, 32, 64, 16, 0, 0),
+    ([900, 65], [3, 2], 100, 1, 128, 16, 200, 33),   # a tile a token
+    ([700] * 6, [150] * 6, 14, 2, 128, 64, 0, 0),    # unpacked
+    ([700] * 6, [150] * 6, 6, 2, 64, 48, 90, 7),
 ]
 
 
@@ -403,15 +408,59 @@ def test_attend_of_one_token_a_sequence(window, sinks):
             assert bool((lse[b] == -math.inf).all())
 
 
+@pytest.mark.parametrize("lens,news,H,Hkv", [([150, 200], [20, 7], 7, 1),
+                                             ([700] * 6, [150] * 6, 14, 2)])
+@pytest.mark.parametrize("which", ["k", "v", "both"])
+def test_attend_does_not_see_what_it_should_not(lens, news, H, Hkv, which):
+    """A key or value that is NaN reaches the rows that see it, and no others; both ways."""
+    C = _h()
+    c = C.Case4(lens, H, Hkv, 128, 16, news)
+    plain, _ = _attend(c, 0, 0)
+    bad = lens[0] - 4  # of the first sequence: its last four new tokens see it
+    for pool, n in ((c.pool_k, "k"), (c.pool_v, "v")):
+        if which in (n, "both"):
+            for x in c.halves(pool):
+                x[int(c.table[0, bad // c.page]), :, bad % c.page] = 0xf9
+    out, _ = _attend(c, 0, 0)
+    torch.cuda.synchronize()
+    assert int(c.status.item()) == 0
+    t = news[0]
+    assert bool(torch.isnan(out[t - 4:t]).all())
+    assert torch.isfinite(out[:t - 4]).all() and torch.equal(out[t:], plain[t:])
+    # rows computed one by one: products in fp32, weights not rounded
+    a, b = out[:t - 4].double(), plain[:t - 4].double()
+    scale = float(b.abs().max())
+    assert float((a - b).abs().max()) <= 2 * 2.0 ** -8 * scale
+
+
+@pytest.mark.parametrize("news", [[3, 2], [300, 280]])
+def test_attend_bad_pages_and_strides(news):
+    C, gmc = _h(), _gmc()
+    c = C.Case4([400, 300], 6, 2, 64, 16, news)
+    good, _ = _attend(c, 0, 0)
+    wide = torch.full((sum(news), 9, 72), math.nan, dtype=torch.bfloat16, device="cuda")
+    q = wide[:, 1:7, :64]
+    q.copy_(c.q)
+    out = torch.full((6, sum(news), 64), 7.0, dtype=torch.bfloat16, device="cuda").permute(1, 0, 2)
+    gmc.attend(c.cache(), q, out, max(news), q_offsets=c.offsets())
+    torch.cuda.synchronize()
+    assert torch.equal(out, good[:-1])
+    c.table[1, 3] = -7
+    out, _ = _attend(c, 0, 0)
+    torch.cuda.synchronize()
+    assert int(c.status.item()) == gmc.STATUS_CACHE and torch.equal(out[:news[0]], good[:news[0]])
+
+
 def test_attend_equals_attend_of_the_unpacked_cache():
     """Unpacked to bf16 the cache gives the same bits: the values are exact."""
     from tests.cache_harness import Case
     C, gmc = _h(), _gmc()
-    c = C.Case4([600, 333], 28, 4, 128, 64, [40, 333])
+    lens, news = [600, 333] * 4, [40, 333] * 4
+    c = C.Case4(lens, 28, 4, 128, 64, news)
     out, lse = _attend(c, 0, 0)
-    p = Case([600, 333], 28, 4, 128, "bf16", 128, [40, 333])
+    p = Case(lens, 28, 4, 128, "bf16", 128, news)
     p.K, p.V = c.K, c.V
-    for b in range(2):
+    for b in range(8):
         p.put(b, range(p.lens[b]))
     cache = p.cache(max_len=601)
     want, z = torch.empty_like(out[:-1]), torch.empty_like(lse)
