@@ -76,10 +76,17 @@ def test_sizes(gmc):  # noqa: F811
             ((16, 128), (1, 64), (1, 128), (7, 64), (64, 256), (0, 64), (16, 96))] == \
         [1152, 48, 80, 256, 9216, 0, 0]
     bf16, c = _cache(gmc), _cache4(gmc)
-    # the unpacked rows: 2 sequences of one page of 128
-    assert gmc.lib().gmc_attend_workspace_size(ctypes.byref(c), 28, 3) >= 2 * 128 * 4 * 128 * 4
-    need = gmc.lib().gmc_attend_workspace_size(ctypes.byref(c), 28, 3)
-    assert _attend(gmc, c, _attn(gmc), n=need - 1) == gmc.GMC_ERR_WORKSPACE
+    size = gmc.lib().gmc_attend_workspace_size
+    # the unpacked rows: 2 sequences of one page of 128; 64 sequences of 32 pages
+    wide = _cache4(gmc, d=256, page_stride=4 * 16 * 144, head_stride=16 * 144)
+    assert size(ctypes.byref(wide), 28, 3) >= 2 * 128 * 4 * 256 * 4
+    long = _cache4(gmc, B=64, max_pages=256)
+    assert size(ctypes.byref(long), 28, 200) >= 64 * 4096 * 4 * 128 * 4
+    # few tokens need none of it
+    assert 0 < size(ctypes.byref(long), 28, 16) < 64 * 4096 * 4
+    for cache in (wide, c, long):
+        need, rows = size(ctypes.byref(cache), 28, 3), 3 * cache.B
+        assert _attend(gmc, cache, _attn(gmc), rows=rows, n=need - 1) == gmc.GMC_ERR_WORKSPACE
     need = gmc.lib().gmc_decode_workspace_size(ctypes.byref(c), 28)
     assert need > 0 and _decode(gmc, c, _attn(gmc), n=need - 1) == gmc.GMC_ERR_WORKSPACE
     assert gmc.lib().gmc_evict_workspace_size(ctypes.byref(c), 4) == \
