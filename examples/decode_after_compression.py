@@ -11,7 +11,11 @@ of its weights (the calls are those of a real layer; only the projections are ma
 5. whenever a sequence would outgrow its pages, ``evict`` keeps the rows that gathered the
    most attention, and decoding goes on from the smaller cache.
 
-Run:  python examples/decode_after_compression.py
+With ``--four-bits`` the cache holds 4 bits a value, and question and decoded tokens come as a
+projection's output: queries and keys are turned by their (t, h, w) positions on the way
+(``cache_append_rope``), then attended or decoded.
+
+Run:  python examples/decode_after_compression.py [--four-bits]
 """
 
 from __future__ import annotations
@@ -35,7 +39,27 @@ def fresh_cache(B, Hkv, d, page, places, dtype, status):
     return gmc.KVCache(k, torch.zeros_like(k), table, lens, status=status)
 
 
-def main(prompts=2, question=24, steps=60, places=384, keep=300, page=16, seed=0, verbose=True):
+def fresh_cache4(B, Hkv, d, page, places, status):
+    """The same with pages of 4 bits a value."""
+    per = -(-places // page)
+    k = torch.zeros(B * per, Hkv, gmc.cache4_part_size(page, d), dtype=torch.uint8, device="cuda")
+    table = torch.randperm(B * per, device="cuda").to(torch.int32).reshape(B, per).contiguous()
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    return gmc.KVCache4(k, torch.zeros_like(k), table, lens, page, d, status=status)
+
+
+def rotation(positions, d, base=1e6):
+    """cos and sin of the pairs' angles at every position, from 64 bits; a quarter of the pairs
+    turns by t, three eighths each by h and w."""
+    n = d // 2
+    rate = base ** (-torch.arange(n, dtype=torch.float64) / n)
+    angle = torch.arange(positions, dtype=torch.float64)[:, None] * rate
+    table = torch.cat([angle.cos(), angle.sin()], 1).float().cuda()
+    return gmc.Rope(table, sections=(n // 4, 3 * n // 8, 3 * n // 8))
+
+
+def main(prompts=2, question=24, steps=60, places=384, keep=300, page=16, seed=0, verbose=True,
+         four_bits=False):
     torch.manual_seed(seed)
     wl = workloads.make("qwen", B=prompts)
     arr = wl.abi_arrays()
@@ -51,7 +75,13 @@ def main(prompts=2, question=24, steps=60, places=384, keep=300, page=16, seed=0
     B, H, Hkv, d, rows = wl.B, wl.H, wl.Hkv, wl.d, out.K + wl.T_max
 
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
-    cache = fresh_cache(B, Hkv, d, page, places, torch.bfloat16, status)
+
+    def fresh():
+        if four_bits:
+            return fresh_cache4(B, Hkv, d, page, places, status)
+        return fresh_cache(B, Hkv, d, page, places, torch.bfloat16, status)
+
+    cache = fresh()
     # the compressed prompt: every sequence's K carriers and its text
     cache.lens += rows
     gmc.cache_append(cache, out.kv, None, rows)
@@ -61,9 +91,27 @@ def main(prompts=2, question=24, steps=60, places=384, keep=300, page=16, seed=0
 
     # a second question: appended, then attended over everything before it
     cache.lens += question
-    gmc.cache_append(cache, states(B * question, Hkv), states(B * question, Hkv), question)
-    q = states(B * question, H)
-    answer = torch.empty_like(q)
+    answer = torch.empty(B * question, H, d, dtype=torch.bfloat16, device="cuda")
+    if four_bits:
+        # text positions go on behind the largest one of the prompt, (p, p, p) each
+        last = out.pos.reshape(B, -1).amax(1)
+        rope = rotation(int(last.max()) + 1 + question + steps, d)
+
+        def positions(first, n):
+            p = (last[:, None] + 1 + first + torch.arange(n, device="cuda")).to(torch.int32)
+            return p[:, None].expand(B, 3, n).reshape(-1).contiguous()
+
+        def turned(n, first):
+            x = states(B * n, H + 2 * Hkv)  # a projection's output
+            q = torch.empty(B * n, H, d, dtype=torch.bfloat16, device="cuda")
+            gmc.cache_append_rope(cache, rope, x[:, H:H + Hkv], x[:, H + Hkv:], n,
+                                  positions(first, n), x[:, :H], q)
+            return q
+
+        q = turned(question, 0)
+    else:
+        gmc.cache_append(cache, states(B * question, Hkv), states(B * question, Hkv), question)
+        q = states(B * question, H)
     gmc.attend(cache, q, answer, question)
 
     # decoding; the scores start from the weights of the decoded tokens alone
@@ -71,9 +119,9 @@ def main(prompts=2, question=24, steps=60, places=384, keep=300, page=16, seed=0
     token = torch.empty(B, H, d, dtype=torch.bfloat16, device="cuda")
     workspace = gmc.alloc_workspace(gmc.decode_workspace_size(cache, H))
     length, evictions = rows + question, 0
-    for _ in range(steps):
+    for step in range(steps):
         if length == places:
-            kept = fresh_cache(B, Hkv, d, page, places, torch.bfloat16, status)
+            kept = fresh()
             idx = torch.empty(B, Hkv, keep, dtype=torch.int32, device="cuda")
             best = torch.empty(B, Hkv, keep, device="cuda")
             gmc.evict(cache, kept, scores, keep, idx, best, sinks=4, recent=64)
@@ -82,8 +130,12 @@ def main(prompts=2, question=24, steps=60, places=384, keep=300, page=16, seed=0
             cache, length, evictions = kept, keep, evictions + 1
         cache.lens += 1
         length += 1
-        gmc.decode(cache, states(B, H), token, k_new=states(B, Hkv), v_new=states(B, Hkv),
-                   scores=scores, out_scores=scores, workspace=workspace)
+        if four_bits:
+            gmc.decode(cache, turned(1, question + step), token, scores=scores, out_scores=scores,
+                       workspace=workspace)
+        else:
+            gmc.decode(cache, states(B, H), token, k_new=states(B, Hkv), v_new=states(B, Hkv),
+                       scores=scores, out_scores=scores, workspace=workspace)
     torch.cuda.synchronize()
     assert int(status.item()) == 0 and comp.status() == 0
     assert bool(torch.isfinite(answer.float()).all()) and bool(torch.isfinite(token.float()).all())
@@ -94,4 +146,4 @@ def main(prompts=2, question=24, steps=60, places=384, keep=300, page=16, seed=0
 
 
 if __name__ == "__main__":
-    main()
+    main(four_bits="--four-bits" in sys.argv[1:])
