@@ -195,16 +195,19 @@ cudaError_t launch_cache_read(const KV&, int dtype, char* k_out, char* v_out,
 cudaError_t launch_cache_append(const KV&, int dtype, const void* k_new, const void* v_new,
                                 const int32_t* offsets, int rows, int T, cudaStream_t);
 
-size_t attend_workspace(const KV&, int dtype, int H, int T);
+// splits: parts of the key axis, 0: as many as the shape's rule says
+size_t attend_workspace(const KV&, int dtype, int H, int T, int splits = 0);
 void* tensor_map_encoder();  // cuTensorMapEncodeTiled, or NULL
 bool attend_tc_takes(const KV&, int dtype, int G);
 int attend_tc_splits(const KV&, int G, int T);
+int attend_tc_wave_parts(const KV&, int G, int T, long long most);
 cudaError_t launch_attend_tc(const AttnArgs&, cudaStream_t);
 bool attend_f32_takes(const KV&, int dtype);
 int attend_f32_splits(const KV&, int G, int T);
 cudaError_t launch_attend_f32(const AttnArgs&, cudaStream_t);
 cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t);  // of part and ml
-cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t, int* launches);
+cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t, int* launches,
+                          int splits = 0);
 size_t attend_fp4_workspace(const KV&, int H, int T);
 int attend_direct_splits(const KV&, int G, int T);
 cudaError_t launch_attend_direct(const AttnArgs&, cudaStream_t);

@@ -344,9 +344,9 @@ int attend_splits(const KV& c, int dtype, int G, int T) {
 }
 }  // namespace
 
-size_t attend_workspace(const KV& c, int dtype, int H, int T) {
+size_t attend_workspace(const KV& c, int dtype, int H, int T, int splits) {
   const int G = H / c.Hkv;
-  const int s = attend_splits(c, dtype, G, T);
+  const int s = splits ? splits : attend_splits(c, dtype, G, T);
   if (s == 1) return 256;
   const size_t rows = (size_t)c.B * T * H * s;
   return 256 + ((rows * 8 + 255) & ~(size_t)255) + rows * c.d * 4;
@@ -359,10 +359,11 @@ cudaError_t launch_attend_join(const AttnArgs& a, int dtype, cudaStream_t st) {
              : launch_k(k_attend_join<float>, dim3(grid), dim3(256), 0, st, 1, a);
 }
 
-cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t st, int* launches) {
+cudaError_t launch_attend(AttnArgs a, int dtype, void* ws, cudaStream_t st, int* launches,
+                          int splits) {
   const int R = AT_ROWS, gsub = std::min(a.G, R), ng = ceil_div(a.G, gsub);
   const int ntile = ceil_div(a.T, R / gsub);
-  a.splits = attend_splits(a.c, dtype, a.G, a.T);
+  a.splits = splits ? splits : attend_splits(a.c, dtype, a.G, a.T);
   if (a.splits > 1) {
     const size_t rows = (size_t)a.c.B * a.T * a.H * a.splits;
     a.ml = reinterpret_cast<float2*>(ws);

@@ -386,6 +386,21 @@ def test_attend_matches_its_definition(lens, news, H, Hkv, d, page, window, sink
         at += t
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (5000, 3), (100, 3)])
+def test_attend_in_parts_that_fill_the_last_wave(window, sinks):
+    """Unpacked, the key axis in parts although the tiles fill the GPU; some tokens of many."""
+    from tests import cache_harness as A
+    n, t = 8100, 2720
+    c = _h().Case4([n], 8, 1, 64, 64, [t], spread=2.0)
+    out, lse = _attend(c, window, sinks)
+    torch.cuda.synchronize()
+    assert int(c.status.item()) == 0 and bool((out[-1] == 7.0).all())
+    for x in [0, 1, 15, 16, 127, 128, *range(201, t, 211), t - 2, t - 1]:
+        ref, z, _, bound, size = A.attention(c.K[0], c.V[0], c.q[x], n - t + x, window, sinks)
+        _close(out[x], ref, bound, A.tolerance(c.dt, 64, size, roundings=2), f"new token {x}")
+        _close(lse[x], z, torch.ones_like(z), A.lse_tolerance(64, size) * 4, "lse")
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (100, 3)])
 def test_attend_of_one_token_a_sequence(window, sinks):
     """Without offsets it goes the way of decode."""
