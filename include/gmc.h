@@ -544,7 +544,8 @@ int gmc_clients(const gmc_problem* prob, const gmc_params* params, const gmc_vie
  * first the codes of its slots, d / 2 bytes each (channel 2x in the low half of
  * byte x, channel 2x + 1 in the high), then the scales of its slots, d / 16 bytes
  * each, together gmc_cache4_part_size bytes (rounded up to 16).  Strides are
- * bytes; slot_stride is 0; the parts must not overlap (GMC_ERR_ARG).
+ * bytes; slot_stride is 0; a page's heads lie between it and the next page, or a
+ * head's pages between it and the next head, none overlapping (GMC_ERR_ARG).
  * gmc_cache_append, gmc_cache_append_rope and gmc_decode pack what they append;
  * all attention is over the values that the codes stand for, a decoded token's
  * own included.  Its products are exact in half precision (queries within 2^-39

@@ -1,5 +1,6 @@
 // C-ABI entry points of the key-value cache and its attention (declared and
 // documented in include/gmc.h): argument checks, workspaces and launches.
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -57,8 +58,14 @@ int check_cache(const gmc_kv_cache* c) {
     return GMC_ERR_ARG;
   if (c->dtype == GMC_FP4) {  // slots lie as the format says, parts of pages apart
     const long long part = fp4_part(c->page_size, c->d);
-    if (c->slot_stride != 0 || (c->Hkv > 1 && c->head_stride < part) ||
-        (c->num_pages > 1 && c->page_stride < part))
+    // n parts `inner` apart lie within `outer`
+    auto within = [part](long long inner, int n, long long outer) {
+      return outer >= part && (n == 1 || (inner >= part && inner <= (outer - part) / (n - 1)));
+    };
+    const long long head = c->Hkv > 1 ? c->head_stride : LLONG_MAX,
+                    page = c->num_pages > 1 ? c->page_stride : LLONG_MAX;
+    if (c->slot_stride != 0 ||
+        !(within(head, c->Hkv, page) || within(page, c->num_pages, head)))
       return GMC_ERR_ARG;
   }
   return GMC_OK;

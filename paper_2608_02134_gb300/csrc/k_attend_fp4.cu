@@ -3,6 +3,8 @@
 // gmc_attend's kernels for bf16 run on these.
 //
 // The unpacking is bound by memory: 72 bytes a row of 128 channels read, 256 written.
+#include <math.h>
+
 #include <algorithm>
 
 #include "cache.cuh"
@@ -109,8 +111,8 @@ namespace {
 // and 26.5.
 bool direct(const KV& c, int G, int T) {
   if (c.d > 128) return false;
-  const long long tiles = ceil_div(T, 128 / G);
-  const long long load = (long long)c.B * c.Hkv * tiles * ceil_div(c.cap, 64) / sm_count();
+  const double tiles = ceil_div(T, 128 / G);
+  const double load = floor((double)c.B * c.Hkv * tiles * ceil_div(c.cap, 64) / sm_count());
   return load * (9 * tiles - 22) < 100 * tiles;
 }
 // Parts of the key axis of the unpacked rows, whose attention need not add up as bf16's does: also

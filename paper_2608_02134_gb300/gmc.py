@@ -742,6 +742,8 @@ def cache_append_rope(cache: KVCache, rope: Rope, k_new, v_new, T, positions=Non
     key = (cache._row_shape, k_new.shape, k_new.stride(), v_key, q_key)
     layout = rope.layouts.get(key)  # of these shapes and strides: rows, gmc_rope
     if layout is None:
+        if len(rope.layouts) >= 1024:  # ragged batches have ever new ones
+            rope.layouts.clear()
         layout = rope.layouts[key] = _rope_layout(cache, rope, k_new, v_new, q, out)
     rows, ref = layout
     rc = lib().gmc_cache_append_rope(

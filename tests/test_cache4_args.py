@@ -71,6 +71,20 @@ def test_strides_of_a_single_head_or_page_are_anything(gmc):  # noqa: F811
     assert _attend(gmc, _cache4(gmc), _attn(gmc, q_row_stride=3588)) == gmc.GMC_ERR_ARG
 
 
+def test_parts_of_pages_lie_apart(gmc):  # noqa: F811
+    part, N = 16 * 72, _cache4(gmc).num_pages
+    rows = lambda **kw: _read(gmc, _cache4(gmc, k=FAKE, **kw), rows=0, T=1,  # noqa: E731
+                              off=FAKE)
+    assert rows(page_stride=part, head_stride=N * part) == gmc.GMC_OK         # head after head
+    assert rows(page_stride=9 * part, head_stride=2 * part) == gmc.GMC_OK     # with room between
+    assert rows(page_stride=7 * part, head_stride=2 * part) == gmc.GMC_OK
+    for page, head in ((1, 1), (3, 1), (2, 3), (6, 2), (1, N - 1), (2, 2 * N - 2), (4, 2)):
+        assert rows(page_stride=page * part, head_stride=head * part) == gmc.GMC_ERR_ARG
+    top = 1 << 62
+    assert rows(page_stride=top, head_stride=top) == gmc.GMC_ERR_ARG
+    assert rows(page_stride=16, head_stride=top) == gmc.GMC_ERR_ARG
+
+
 def test_sizes(gmc):  # noqa: F811
     assert [gmc.cache4_part_size(p, d) for p, d in
             ((16, 128), (1, 64), (1, 128), (7, 64), (64, 256), (0, 64), (16, 96))] == \
@@ -226,3 +240,14 @@ def test_binding_refuses_odd_calls(launchless):  # noqa: F811
         g.cache_read(cache, OnDevice(torch.zeros(B, 2 * HKV, D, dtype=torch.bfloat16)[:, :HKV], 0),
                      o["v_new"], 1)
     assert g.library.calls == 0
+
+
+def test_a_rope_keeps_few_layouts(launchless):  # noqa: F811
+    """Every number of rows is a layout of its own."""
+    g, o = launchless, _tensors()
+    cache, rope = _handles(g, o)
+    new = torch.zeros(3000, HKV, D, dtype=torch.bfloat16)
+    for n in range(3000):
+        g.cache_append_rope(cache, rope, OnDevice(new[:n], 0), OnDevice(new[:n], 0), 1,
+                            offsets=o["offsets"])
+    assert len(rope.layouts) <= 1024 and g.library.calls == 3000
