@@ -102,18 +102,26 @@ Unpacked unpacked(const KV& c) {
 }  // namespace
 
 namespace {
-// Whether the attending kernel reads the codes itself (k_attend_fp4_tc.cu).  It takes about 1 us
-// for a turn of 64 keys of one of its tiles; unpacking takes 1.1 us for every 64 keys and half
-// of that time for a turn, and 5 us more for its launch.  28 query and 4 key heads of 128, us so
-// and so: 8 x 16,004 keys and 16 tokens (one tile) 67 and 113, 32 tokens 124 and 132, 64 (four
-// tiles) 229 and 185; 8 x 2,000 and 64 tokens 35 and 42, 128 tokens 69 and 44; one sequence of
-// 16,004 and 64 tokens 37 and 40, 128 tokens 66 and 50; of 2,000 and 256 tokens (15 tiles) 26
-// and 26.5.
+// Whether the attending kernel reads the codes itself (k_attend_fp4_tc.cu): where it takes less
+// than unpacking and attending, in us by these two sums.  28 query and 4 key heads of 128, us so
+// and so: 8 x 16,004 keys and 16 tokens (one tile) 57 and 114, 32 tokens 103 and 132, 48 (three
+// tiles, a second wave) 189 and 149; 8 x 2,000 and 64 tokens 31 and 43, 96 tokens 59 and 44; one
+// sequence of 16,004 and 64 tokens 33 and 40, 128 tokens 57 and 50; of 2,000 and 256 tokens (15
+// tiles) 24 and 27; 32 x 500 and 18 tokens 14 and 23, 64 tokens 50 and 38.
 bool direct(const KV& c, int G, int T) {
   if (c.d > 128) return false;
-  const double tiles = ceil_div(T, 128 / G);
-  const double load = floor((double)c.B * c.Hkv * tiles * ceil_div(c.cap, 64) / sm_count());
-  return load * (9 * tiles - 22) < 100 * tiles;
+  const double sms = sm_count(), pairs = (double)c.B * c.Hkv, tiles = pairs * ceil_div(T, 128 / G);
+  // a turn of 64 keys, and what a CTA has besides; joining as in cheapest_parts
+  const int s = attend_direct_splits(c, G, T);
+  double codes = ceil(tiles * s / sms) * (5.5 + 0.76 * ceil_div(ceil_div(c.cap, 64), s));
+  if (s > 1) codes += 2.5 + 8. * s * c.B * T * G * c.Hkv * c.d / 5e6;
+  // 2.56 bytes a value read and written, 2 read again, or a turn of 128 keys; joining
+  const double values = pairs * c.cap * c.d * 2;
+  double rows = 9 + values * 2.5625 / 6e6 +
+                fmax(values * 2 / 6e6, tiles * ceil_div(c.cap, 128) / sms) +
+                5 * ceil(tiles / (2 * sms));
+  if (tiles < sms) rows += 5;
+  return codes < rows;
 }
 // Parts of the key axis of the unpacked rows, whose attention need not add up as bf16's does: also
 // where that fills a last wave (2,048 tokens on 16,004 keys: 392 us in one part, 364 in two).

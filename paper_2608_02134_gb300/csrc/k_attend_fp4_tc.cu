@@ -5,17 +5,22 @@
 // heads of a key head and 128 / G consecutive tokens), and walks the seen keys 64 at a time.
 // Four warps copy keys' codes, four values', seven turns ahead into rings of their own, multiply
 // them with their scales and write them to shared memory as halves, which hold them exactly, the
-// way the tensor cores read them.  One warp issues products; eight turn logits into weights, two
-// threads a row, each with half of the turn's keys.  The queries lie in tensor memory as halves,
+// way the tensor cores read them.  One warp issues products; four warps turn the logits of even
+// turns into weights, four those of odd ones, a row a thread, with an output and a maximum of
+// their own in tensor memory and registers, so that neither waits for the other; the two outputs
+// become one at the end.  The queries lie in tensor memory as halves,
 // every row multiplied by a power of two that puts its largest value into [2^14, 2^15): what that
 // makes too small for a half is 2^-39 of the largest.  Weights are rounded to half (2^-12), their
 // sum is the unrounded ones'.  The maximum that weights are taken against follows the running one
 // only when it has grown by 2^8; then the output in tensor memory is rescaled.
 //
-// Measured: 16 tokens (28 query heads, 4 key heads of 128) on 8 x 16,004 keys 67 us, on one
-// sequence of 16,004 21.  A turn takes 1,750 clocks, the chain from logits to weights; the codes
-// alone would allow 400.  With two warps each for keys and values 75 and 21 us; copied one turn
-// ahead, in registers, 100 (a turn's 9 KB are not enough under way).
+// Measured: 16 tokens (28 query heads, 4 key heads of 128) on 8 x 16,004 keys 57 us, on one
+// sequence of 16,004 20.  A turn takes 1,450 clocks, at half of the instructions that the SM could
+// issue; the codes alone would allow 400.  Without converting and copying it would take 1,050.  On
+// the way here, in us of the first: all eight weighing warps on one turn 67, taking turns 65; the
+// loads of a turn's codes before its first store 64; rows in runs of a page 63; stores whose lanes
+// need not swap halves 60; shared memory by 32-bit addresses 57.  Sixteen copying warps, in 72
+// registers, 75 for 64; three or four turns of halves instead of two 60 and 65 for 57 and 63.
 //
 // Every tile of a sequence converts the same codes again, so this pays for few tiles: `direct` in
 // k_attend_fp4.cu says where the rows are unpacked first instead.
@@ -40,11 +45,13 @@ constexpr int Q_COPY = 8;    // warps that copy and convert
 constexpr int Q_ISSUE = Q_WEIGH + Q_COPY;
 constexpr int Q_THREADS = (Q_ISSUE + 1) * 32;
 constexpr int Q_RING = 8;    // turns of a copying warp's ring
+constexpr int Q_AHEAD = 2;   // turns of keys and values as halves
 constexpr int Q_STAGE = 96;  // columns of a turn in tensor memory: 64 logits, 32 of weights
 
 struct QCtl {
-  uint64_t qfull, kfull[2], kempty[2], vfull[2], vempty[2], sfull[2], pfull[2], ofull, drained;
-  float top[2][2][TM], sum[2][TM];
+  uint64_t kfull[Q_AHEAD], kempty[Q_AHEAD], vfull[Q_AHEAD], vempty[Q_AHEAD];
+  uint64_t qfull, sfull[2], pfull[2], ofull, drained;
+  float top[2][TM], sum[2][TM];
   uint32_t tmem;
   volatile int abort;
   int strange;
@@ -54,14 +61,35 @@ template <int DP> constexpr int Q_PART = Q_ROWS * (DP / 2 + DP / 16);
 template <int DP> constexpr size_t q_smem() {
   // the output's rows pass through the keys' and values' place
   const size_t need =
-      1024 + 4 * (size_t)QK * DP * 2 + Q_COPY * Q_RING * Q_PART<DP> + sizeof(QCtl);
-  return need > 120 * 1024 ? need : 120 * 1024;  // one CTA an SM: a second would wait for tensor memory
+      1024 + 2 * Q_AHEAD * (size_t)QK * DP * 2 + Q_COPY * Q_RING * Q_PART<DP> + sizeof(QCtl);
+  // one CTA an SM: a second would wait for tensor memory
+  return need > 120 * 1024 ? need : 120 * 1024;
 }
+// Shared memory by its own addresses: 32 bits, and no detour over generic ones.
 template <int BYTES>
-__device__ __forceinline__ void cp_async_small(void* smem, const void* src, bool pred) {
-  const unsigned sa = (unsigned)__cvta_generic_to_shared(smem);
-  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(sa), "l"(src), "n"(BYTES),
-               "r"(pred ? BYTES : 0)
+__device__ __forceinline__ void cp_async_to(uint32_t smem, const void* src, bool pred) {
+  if constexpr (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(src),
+                 "r"(pred ? 16 : 0)
+                 : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(smem), "l"(src), "n"(BYTES),
+                 "r"(pred ? BYTES : 0)
+                 : "memory");
+}
+__device__ __forceinline__ uint2 lds8(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds1(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts16(uint32_t at, const uint32_t* v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]),
+               "r"(v[2]), "r"(v[3])
                : "memory");
 }
 // Two floats as halves, the first one low.
@@ -138,27 +166,29 @@ template <int DP>
 __global__ void __launch_bounds__(Q_THREADS, 1) k_attend_fp4(AttnArgs a, Div by_g, Div by_tokens,
                                                              Div by_ps) {
   constexpr int KT = QK * DP * 2, C = DP / 16, OC = DP / 2;
-  // tensor memory: the queries, two turns of logits and weights, the output
+  // tensor memory: the queries, two turns of logits and weights, two outputs
   constexpr int STAGE = DP / 2, SUM = STAGE + 2 * Q_STAGE;
-  static_assert(SUM + DP <= 512, "columns");
+  static_assert(SUM + 2 * DP <= 512, "columns");
   extern __shared__ char raw[];
   char* smem = reinterpret_cast<char*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-  char* Ks = smem;  // [2 turns][DP / 64][64 rows][64]
-  char* Vs = Ks + 2 * KT;
-  char* rings = Vs + 2 * KT;  // [copying warp][Q_RING]
+  char* Ks = smem;  // [Q_AHEAD][DP / 64][64 rows][64]
+  char* Vs = Ks + Q_AHEAD * KT;
+  char* rings = Vs + Q_AHEAD * KT;  // [copying warp][Q_RING]
   QCtl* ctl = reinterpret_cast<QCtl*>(rings + Q_COPY * Q_RING * Q_PART<DP>);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) {
     tc::mbar_init(&ctl->qfull, Q_WEIGH);
     tc::mbar_init(&ctl->ofull, 1);
     tc::mbar_init(&ctl->drained, 1);
-    for (int x = 0; x < 2; ++x) {
+    for (int x = 0; x < Q_AHEAD; ++x) {
       tc::mbar_init(&ctl->kfull[x], Q_COPY / 2);
       tc::mbar_init(&ctl->vfull[x], Q_COPY / 2);
       tc::mbar_init(&ctl->kempty[x], 1);
       tc::mbar_init(&ctl->vempty[x], 1);
+    }
+    for (int x = 0; x < 2; ++x) {
       tc::mbar_init(&ctl->sfull[x], 1);
-      tc::mbar_init(&ctl->pfull[x], Q_WEIGH);
+      tc::mbar_init(&ctl->pfull[x], Q_WEIGH / 2);
     }
     ctl->abort = 0;
     ctl->strange = 0;
@@ -192,24 +222,33 @@ __global__ void __launch_bounds__(Q_THREADS, 1) k_attend_fp4(AttnArgs a, Div by_
 
   if (turns > 0 && warp >= Q_WEIGH && warp < Q_ISSUE) {
     // ---- keys and values --------------------------------------------------------------
-    // half of the warps the keys, half the values: RW rows at a time, a block of 16 channels a lane
+    // half of the warps the keys, half the values, Q_ROWS consecutive ones a warp: RW rows at a
+    // time, a block of 16 channels a lane
     constexpr int W = Q_COPY / 2, RW = 32 / C, STEPS = QK / (W * RW);
-    static_assert(STEPS * RW == Q_ROWS && Q_ROWS <= 32, "a lane looks one row up");
-    const int kv = (warp - Q_WEIGH) / W, w = warp - Q_WEIGH - kv * W, c = lane % C, rw = lane / C;
-    const char* pool = kv ? a.c.v : a.c.k;
-    char* tiles = kv ? Vs : Ks;
+    static_assert(STEPS * RW == Q_ROWS && Q_ROWS == 16, "a lane looks one row up, runs of 16");
+    const int kv = (warp - Q_WEIGH) / W, w = warp - Q_WEIGH - kv * W;
+    // eight lanes: two rows and four blocks, whose pieces lie in other banks
+    const int c = C == 8 ? (lane & 3) | (lane >> 1 & 4) : lane & 3,
+              rw = C == 8 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+    const char* pool = (kv ? a.c.v : a.c.k) + h * a.c.head_stride;
+    const uint32_t tiles = tc::smem_u32(kv ? Vs : Ks);
     uint64_t *full = kv ? ctl->vfull : ctl->kfull, *empty = kv ? ctl->vempty : ctl->kempty;
     constexpr int CB = DP / 2, SB = DP / 16, P = CB / 16;  // bytes of a row, pieces of its codes
-    char* ring = rings + (warp - Q_WEIGH) * Q_RING * Q_PART<DP>;
-    // a lane finds row `lane` of the warp's, row (step, rw) = (lane / RW, lane % RW) of its
-    // steps: its page is read a turn before it is needed, and looked at only then
+    const uint32_t ring = tc::smem_u32(rings + (warp - Q_WEIGH) * Q_RING * Q_PART<DP>);
+    // a lane finds row `lane` of the warp's; where all 16 are seen and of one page, their first
+    // one.  Its page is read a turn before it is needed, and looked at only then
     struct Place {
       int page, slot;
+      bool run;
     };
+    const int odd = (a.c.ps & 15) ? -1 : 15;  // a run's first place is no multiple of 16
     auto look_up = [&](int x) {
-      Place p = {0, -1};
-      const int r = (lane / RW * W + w) * RW + lane % RW, j = key0(x) + r;
-      if (lane < Q_ROWS && x < turns && j < key1(x)) {
+      Place p = {0, -1, false};
+      if (x >= turns) return p;
+      int j = key0(x) + w * Q_ROWS;
+      p.run = (j & odd) == 0 && j + Q_ROWS <= key1(x);
+      if (!p.run) j += lane;
+      if (p.run || (lane < Q_ROWS && j < key1(x))) {
         const int y = by_ps.of(j);
         p.page = a.c.table[(long long)b * a.c.max_pages + y];
         p.slot = j - y * a.c.ps;
@@ -218,23 +257,30 @@ __global__ void __launch_bounds__(Q_THREADS, 1) k_attend_fp4(AttnArgs a, Div by_
     };
     auto copy = [&](int x, const Place& p) {  // of rows that are not seen zeros
       if (x < turns) {
-        char* to = ring + (x % Q_RING) * Q_PART<DP>;
-        long long at = -1, z = 0;
-        if (p.slot >= 0) {
-          if ((unsigned)p.page < (unsigned)a.c.num_pages) {
-            at = p.page * a.c.page_stride + h * a.c.head_stride;
-            z = at + fp4_scale_at(a.c, p.slot);
-            at += (long long)p.slot * CB;
-          } else {
-            set_status(a.c.status, CACHE_BAD);
-          }
-        }
+        const uint32_t to = ring + (x % Q_RING) * Q_PART<DP>;
+        const bool there = p.slot >= 0 && (unsigned)p.page < (unsigned)a.c.num_pages;
+        if (p.slot >= 0 && !there) set_status(a.c.status, CACHE_BAD);
+        const char* part = pool + (there ? p.page * a.c.page_stride : 0);
+        const long long codes = there ? (long long)p.slot * CB : 0,
+                        scales = there ? fp4_scale_at(a.c, p.slot) : 0;
+        if (p.run) {
 #pragma unroll
-        for (int r0 = 0; r0 < Q_ROWS; r0 += 32 / P) {
-          const long long o = __shfl_sync(FULL, at, r0 + lane / P);
-          cp_async16(to + r0 * CB + lane * 16, pool + (o >= 0 ? o + lane % P * 16 : 0), o >= 0);
+          for (int y = 0; y < Q_ROWS * CB; y += 512)
+            cp_async_to<16>(to + y + lane * 16, part + codes + (there ? y + lane * 16 : 0), there);
+          if (lane < SB)
+            cp_async_to<16>(to + Q_ROWS * CB + lane * 16, part + scales + (there ? lane * 16 : 0),
+                       there);
+        } else {
+          const long long at = there ? part + codes - pool : -1;
+#pragma unroll
+          for (int r0 = 0; r0 < Q_ROWS; r0 += 32 / P) {
+            const long long o = __shfl_sync(FULL, at, r0 + lane / P);
+            cp_async_to<16>(to + r0 * CB + lane * 16, pool + (o >= 0 ? o + lane % P * 16 : 0),
+                            o >= 0);
+          }
+          if (lane < Q_ROWS)
+            cp_async_to<SB>(to + Q_ROWS * CB + lane * SB, part + scales, there);
         }
-        if (lane < Q_ROWS) cp_async_small<SB>(to + Q_ROWS * CB + lane * SB, pool + z, at >= 0);
       }
       cp_async_commit();
     };
@@ -245,41 +291,47 @@ __global__ void __launch_bounds__(Q_THREADS, 1) k_attend_fp4(AttnArgs a, Div by_
 #pragma unroll
       for (int y = 0; y < Q_RING - 1; ++y) copy(y, first[y]);
     }
+    // of the lane's block of its warp's first row
+    const uint32_t place = (c >> 2) * QK * 128 + (w * Q_ROWS + rw) * 128 +
+                           (((2 * (c & 3)) ^ (rw & 7)) * 16);
     uint32_t worst = 0;  // of the scales: from 0xf8 on not finite
     Place next = look_up(Q_RING - 1);
     for (int x = 0; x < turns; ++x) {
-      if (x > 1 &&
-          !__all_sync(FULL, wait_for(&empty[x & 1], ((x >> 1) & 1) ^ 1, &ctl->abort)))
+      const int stage = x % Q_AHEAD;
+      if (x >= Q_AHEAD &&
+          !__all_sync(FULL, wait_for(&empty[stage], (x / Q_AHEAD & 1) ^ 1, &ctl->abort)))
         break;
       cp_async_wait<Q_RING - 2>();
       __syncwarp();
-      const char* from = ring + (x % Q_RING) * Q_PART<DP>;
-      char* dst = tiles + (x & 1) * KT;
+      const uint32_t from = ring + (x % Q_RING) * Q_PART<DP> + rw * CB + c * 8,
+                     from_z = ring + (x % Q_RING) * Q_PART<DP> + Q_ROWS * CB + rw * SB + c;
+      // rows 4 further on: the other half of a swizzle's eight
+      uint32_t dst[2];
+      dst[0] = tiles + stage * KT + place;
+      dst[1] = RW == 4 ? dst[0] ^ 64 : dst[0];
+      uint2 code[STEPS];
+      uint32_t scale[STEPS];
 #pragma unroll
       for (int k = 0; k < STEPS; ++k) {
-        const int r = (k * W + w) * RW + rw, y0 = k * RW + rw;
-        const uint2 code = *reinterpret_cast<const uint2*>(from + y0 * CB + c * 8);
-        const uint32_t scale = (uint8_t)from[Q_ROWS * CB + y0 * SB + c];
-        worst = max(worst, scale);
-        const uint32_t s2 = fp4_scale2(scale);
+        code[k] = lds8(from + k * RW * CB);
+        scale[k] = lds1(from_z + k * RW * SB);
+        worst = max(worst, scale[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < STEPS; ++k) {
+        const uint32_t s2 = fp4_scale2(scale[k]);
         uint32_t v[8];
-        fp4_halves(code.x, v);
-        fp4_halves(code.y, v + 4);
+        fp4_halves(code[k].x, v);
+        fp4_halves(code[k].y, v + 4);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = hmul2(v[e], s2);
-        // lanes of the upper channels write their second piece first: other banks
-        char* row = dst + (c >> 2) * QK * 128 + r * 128;
-        const int flip = c >> 2 & 1;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int y = e ^ flip;
-          *reinterpret_cast<uint4*>(row + (((2 * (c & 3) + y) ^ (r & 7)) * 16)) =
-              y ? make_uint4(v[4], v[5], v[6], v[7]) : make_uint4(v[0], v[1], v[2], v[3]);
-        }
+        const uint32_t row = dst[k & 1] + k * RW * 128;
+        sts16(row, v);
+        sts16(row ^ 16, v + 4);
       }
       fence_async();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&full[x & 1]);
+      if (lane == 0) tc::mbar_arrive(&full[stage]);
       copy(x + Q_RING - 1, next);  // into the place of turn x - 1
       next = look_up(x + Q_RING);
     }
@@ -299,34 +351,39 @@ __global__ void __launch_bounds__(Q_THREADS, 1) k_attend_fp4(AttnArgs a, Div by_
     };
     auto logits = [&](int x) {
       const uint32_t d = tmem + STAGE + (x & 1) * Q_STAGE;
-      const uint64_t kb = kd + (x & 1) * (KT / 16);
+      const uint64_t kb = kd + x % Q_AHEAD * (KT / 16);
 #pragma unroll
       for (int k = 0; k < DP / 16; ++k)
         mma_ts(go, d, tmem + k * 8, kb + ((k >> 2) * QK * 128 + (k & 3) * 32) / 16, sdesc, k > 0);
       commit(go, &ctl->sfull[x & 1]);
-      commit(go, &ctl->kempty[x & 1]);
+      commit(go, &ctl->kempty[x % Q_AHEAD]);
     };
-    bool ok = ready(&ctl->qfull, 0) && ready(&ctl->kfull[0], 0);
-    tc::fence_after_sync();
-    if (ok) logits(0);
+    bool ok = ready(&ctl->qfull, 0);
+    for (int x = 0; x < 2 && x < turns && ok; ++x) {
+      ok = ready(&ctl->kfull[x], 0);
+      tc::fence_after_sync();
+      if (ok) logits(x);
+    }
 #pragma unroll 1
     for (int x = 0; x < turns && ok; ++x) {
-      if (x + 1 < turns) {
-        ok = ready(&ctl->kfull[(x + 1) & 1], ((x + 1) >> 1) & 1);
-        if (!ok) break;
-        tc::fence_after_sync();
-        logits(x + 1);
-      }
-      ok = ready(&ctl->pfull[x & 1], (x >> 1) & 1) && ready(&ctl->vfull[x & 1], (x >> 1) & 1);
+      ok = ready(&ctl->pfull[x & 1], (x >> 1) & 1) &&
+           ready(&ctl->vfull[x % Q_AHEAD], x / Q_AHEAD & 1);
       if (!ok) break;
       tc::fence_after_sync();
-      const uint32_t p = tmem + STAGE + (x & 1) * Q_STAGE + 64, d = tmem + SUM;
-      const uint64_t vb = vd + (x & 1) * (KT / 16);
+      const uint32_t p = tmem + STAGE + (x & 1) * Q_STAGE + 64, d = tmem + SUM + (x & 1) * DP;
+      const uint64_t vb = vd + x % Q_AHEAD * (KT / 16);
 #pragma unroll
       for (int k = 0; k < QK / 16; ++k)
-        mma_ts(go, d, p + k * 8, vb + k * 2048 / 16, odesc, x > 0 || k > 0);
-      commit(go, &ctl->ofull);
-      commit(go, &ctl->vempty[x & 1]);
+        mma_ts(go, d, p + k * 8, vb + k * 2048 / 16, odesc, x > 1 || k > 0);
+      commit(go, &ctl->vempty[x % Q_AHEAD]);
+      if (x + 2 < turns) {  // into the place of logits that have become weights
+        ok = ready(&ctl->kfull[(x + 2) % Q_AHEAD], (x + 2) / Q_AHEAD & 1);
+        if (!ok) break;
+        tc::fence_after_sync();
+        logits(x + 2);
+      } else if (x + 1 == turns) {
+        commit(go, &ctl->ofull);
+      }
     }
     if (!ok) {  // products in flight end before tensor memory is freed
       commit(go, &ctl->drained);
@@ -356,9 +413,9 @@ __global__ void __launch_bounds__(Q_THREADS, 1) k_attend_fp4(AttnArgs a, Div by_
         if (valid) v[c] = *reinterpret_cast<const uint4*>(q + c * 8);
         top = max(top, fp4_top(v[c]));
       }
-      ctl->top[0][half][r] = __uint_as_float(top);
+      ctl->top[half][r] = __uint_as_float(top);
       meet(quarter);
-      top = max(top, __float_as_uint(ctl->top[0][half ^ 1][r]));
+      top = max(top, __float_as_uint(ctl->top[half ^ 1][r]));
       meet(quarter);  // both have read it
       const int e = (int)(top >> 7) - 127;
       const int k = top == 0 || top >= 0x7f80u ? 0 : min(14 - e, 126);
@@ -384,38 +441,43 @@ __global__ void __launch_bounds__(Q_THREADS, 1) k_attend_fp4(AttnArgs a, Div by_
     }
     float m = -INFINITY, l = 0.f;
     // a wait that runs out makes the next ones return at once; all threads stay in step
-    for (int x = 0; x < turns; ++x) {
-      const uint32_t at = lanes + STAGE + (x & 1) * Q_STAGE;
+    for (int x = half; x < turns; x += 2) {  // the turns of this thread's warp, whole rows
+      const uint32_t at = lanes + STAGE + half * Q_STAGE;
       const int j0 = key0(x), j1 = key1(x);
-      wait_for(&ctl->sfull[x & 1], (x >> 1) & 1, &ctl->abort);
+      wait_for(&ctl->sfull[half], (x >> 1) & 1, &ctl->abort);  // and products of turn x - 2
       __syncwarp();
       tc::fence_after_sync();
-      float s[32];
-      tc::tmem_ld32(at + half * 32, s);
       // whether every row sees every key
       const bool whole = j0 + QK <= j1 && j0 + QK - 1 <= i0 &&
                          (a.window == 0 || i0 + nt - 1 - j0 < a.window || j0 + QK <= a.sinks);
-      if (!whole) {
-        const int f = j0 + half * 32;                            // this thread's first key
-        const int hi = valid ? min(i + 1, j1) - f : 0;           // columns before hi,
-        const int lo = a.window > 0 ? i - a.window + 1 - f : 0;  // from lo on
-        const int sk = a.sinks - f;                              // or before sk
-        const uint32_t in = below(hi) & (~below(lo) | below(sk));
+      float s[32];
+      auto load = [&](int z) {  // 32 logits, -inf where the row does not see the key
+        tc::tmem_ld32(at + z * 32, s);
+        if (!whole) {
+          const int f = j0 + z * 32;                               // the first key
+          const int hi = valid ? min(i + 1, j1) - f : 0;           // columns before hi,
+          const int lo = a.window > 0 ? i - a.window + 1 - f : 0;  // from lo on
+          const int sk = a.sinks - f;                              // or before sk
+          const uint32_t in = below(hi) & (~below(lo) | below(sk));
 #pragma unroll
-        for (int y = 0; y < 32; ++y)
-          if (!(in >> y & 1)) s[y] = -INFINITY;
+          for (int y = 0; y < 32; ++y)
+            if (!(in >> y & 1)) s[y] = -INFINITY;
+        }
+      };
+      float top = -INFINITY;
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        load(z);
+        float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int c = 4; c < 28; c += 8)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) mx[y] = max3(mx[y], s[c + y], s[c + 4 + y]);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) mx[y] = fmaxf(mx[y], s[28 + y]);
+        top = max3(top, fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
       }
-      float mx[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-      for (int c = 4; c < 28; c += 8)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) mx[y] = max3(mx[y], s[c + y], s[c + 4 + y]);
-#pragma unroll
-      for (int y = 0; y < 4; ++y) mx[y] = fmaxf(mx[y], s[28 + y]);
-      float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * factor;
-      ctl->top[x & 1][half][r] = top;
-      meet(quarter);
-      top = fmaxf(top, ctl->top[x & 1][half ^ 1][r]);
+      top *= factor;
       const bool grew = top > m + GROWN || (m == -INFINITY && top > m);
       const float mn = grew ? top : m;
       const float f = m == -INFINITY || !grew ? 1.f : exp2_fast(m - mn);
@@ -424,53 +486,59 @@ __global__ void __launch_bounds__(Q_THREADS, 1) k_attend_fp4(AttnArgs a, Div by_
       const float base = m == -INFINITY ? 0.f : m;
       const f32x2 scale = pair(factor, factor), off = pair(-base, -base);
       f32x2 sum[2] = {0ull, 0ull};
-      uint32_t p[16];
 #pragma unroll
-      for (int y = 0; y < 16; ++y) {
-        const float2 v = unpair(fma2(pair(s[2 * y], s[2 * y + 1]), scale, off));
-        const float e0 = exp2_fast(v.x), e1 = exp2_fast(v.y);
-        sum[y & 1] = add2(sum[y & 1], pair(e0, e1));
-        p[y] = halves(e0, e1);
+      for (int z = 1; z >= 0; --z) {
+        if (z == 0) load(0);  // again: both halves do not fit the registers
+        uint32_t p[16];
+#pragma unroll
+        for (int y = 0; y < 16; ++y) {
+          const float2 v = unpair(fma2(pair(s[2 * y], s[2 * y + 1]), scale, off));
+          const float e0 = exp2_fast(v.x), e1 = exp2_fast(v.y);
+          sum[y & 1] = add2(sum[y & 1], pair(e0, e1));
+          p[y] = halves(e0, e1);
+        }
+        tmem_st16_async(at + 64 + z * 16, p);
       }
-      tmem_st16_async(at + 64 + half * 16, p);
       const float2 both = unpair(add2(sum[0], sum[1]));
       l += both.x + both.y;
-      if (x > 0) {  // the products before have been added
-        wait_for(&ctl->ofull, (x - 1) & 1, &ctl->abort);
-        __syncwarp();
-        if (__any_sync(FULL, f != 1.f)) {
-          tc::fence_after_sync();
+      if (x > 1 && __any_sync(FULL, f != 1.f)) {
 #pragma unroll
-          for (int c = 0; c < OC; c += 32) {
-            float v[32];
-            tc::tmem_ld32(lanes + SUM + half * OC + c, v);
+        for (int c = 0; c < DP; c += 32) {
+          float v[32];
+          tc::tmem_ld32(lanes + SUM + half * DP + c, v);
 #pragma unroll
-            for (int y = 0; y < 32; ++y) v[y] *= f;
-            tc::tmem_st32(lanes + SUM + half * OC + c, v);
-          }
+          for (int y = 0; y < 32; ++y) v[y] *= f;
+          tc::tmem_st32(lanes + SUM + half * DP + c, v);
         }
       }
       tmem_wait_st();
       tc::fence_before_sync();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&ctl->pfull[x & 1]);
+      if (lane == 0) tc::mbar_arrive(&ctl->pfull[half]);
     }
     if (turns > 0) {
-      wait_for(&ctl->ofull, (turns - 1) & 1, &ctl->abort);
+      wait_for(&ctl->ofull, 0, &ctl->abort);
       __syncwarp();
       tc::fence_after_sync();
     }
+    // the two turns' sums become one
+    ctl->top[half][r] = m;
     ctl->sum[half][r] = l;
     meet(quarter);
-    l = ctl->sum[0][r] + ctl->sum[1][r];
+    const float m0 = ctl->top[0][r], m1 = ctl->top[1][r];
+    m = fmaxf(m0, m1);
+    const float base = m == -INFINITY ? 0.f : m;
+    float f0 = exp2_fast(m0 - base), f1 = exp2_fast(m1 - base);
+    l = ctl->sum[0][r] * f0 + ctl->sum[1][r] * f1;
     long long mine_at = -1;
-    float inv = 1.f;
     if (a.splits > 1) {
       const long long pr = part_row(a, split, b, t0 + tok) * a.H + hq;
       if (valid && half == 0) a.ml[pr] = make_float2(m, l);
       if (valid) mine_at = pr * a.c.d;
     } else {
-      inv = l == 0.f ? 0.f : 1.f / l;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      f0 *= inv;
+      f1 *= inv;
       if (valid && half == 0 && a.lse)
         a.lse[row * a.H + hq] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
       if (valid) mine_at = row * a.o_row + (long long)hq * a.o_head;
@@ -481,16 +549,23 @@ __global__ void __launch_bounds__(Q_THREADS, 1) k_attend_fp4(AttnArgs a, Div by_
 #pragma unroll
     for (int c = 0; c < OC; c += 32) {
       float v[32];
+#pragma unroll
+      for (int y = 0; y < 32; ++y) v[y] = 0.f;
       if (turns > 0) {
         tc::tmem_ld32(lanes + SUM + half * OC + c, v);
-      } else {
 #pragma unroll
-        for (int y = 0; y < 32; ++y) v[y] = 0.f;
+        for (int y = 0; y < 32; ++y) v[y] *= f0;
+      }
+      if (turns > 1) {
+        float w[32];
+        tc::tmem_ld32(lanes + SUM + DP + half * OC + c, w);
+#pragma unroll
+        for (int y = 0; y < 32; ++y) v[y] = fmaf(w[y], f1, v[y]);
       }
 #pragma unroll
       for (int y = 0; y < 32; y += 4)
         *reinterpret_cast<float4*>(st + lane * OC * 4 + ((((c + y) / 4) ^ (lane & 7)) * 16)) =
-            make_float4(v[y] * inv, v[y + 1] * inv, v[y + 2] * inv, v[y + 3] * inv);
+            make_float4(v[y], v[y + 1], v[y + 2], v[y + 3]);
     }
     __syncwarp();
     const int pc = lane % PC;
@@ -556,7 +631,7 @@ int attend_direct_splits(const KV& c, int G, int T) {
   const long long rows = (long long)c.B * T, ctas = c.Hkv * fp4_tiles(c, G, rows, T);
   if (ctas > sm_count() / 2) return 1;
   return cheapest_parts(std::min<long long>({sm_count() / ctas, 32, c.cap / (2 * QK)}),
-                        ceil_div(c.cap, QK), 0.95f, rows * G * c.Hkv * c.d);
+                        ceil_div(c.cap, QK), 0.76f, rows * G * c.Hkv * c.d);
 }
 
 cudaError_t launch_attend_direct(const AttnArgs& a, cudaStream_t st) {
