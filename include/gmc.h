@@ -550,9 +550,11 @@ int gmc_clients(const gmc_problem* prob, const gmc_params* params, const gmc_vie
  * all attention is over the values that the codes stand for, a decoded token's
  * own included.  Its products are exact in half precision (queries within 2^-39
  * of their row's largest value), weights are rounded to half.  gmc_attend reads
- * the codes itself for few tokens; for more it unpacks the seen rows to bf16 (which
- * holds them exactly) in its workspace, which grows by B * cap * Hkv * d * 4 bytes,
- * cap being max_len rounded up to 128, and goes on as with bf16 (d = 256: always).
+ * the codes itself for few tokens (d = 256: up to 16,384 of all sequences, where they
+ * or their keys are not too many, token by token the way of gmc_decode); for more it
+ * unpacks the seen rows to bf16 (which holds them exactly) in its workspace, which grows
+ * by B * cap * Hkv * d * 4 bytes, cap being max_len rounded up to 128, and goes on as
+ * with bf16.
  */
 typedef struct gmc_kv_cache {
   int B;                     /* sequences, >= 1 */
@@ -673,7 +675,8 @@ size_t gmc_cache4_part_size(int page_size, int d);
  * multiple of 128 slots fill them, others leave a part of each turn idle (48 slots
  * a quarter).  One launch, or two where the key axis is split (of GMC_FP4 one more
  * where rows are unpacked; one token a sequence without q_offsets goes the way of
- * gmc_decode).  No score is added to: only gmc_decode does that.
+ * gmc_decode; with d = 256 also up to 2 launches for every 256 tokens and 8 query heads of a
+ * key head, and two more).  No score is added to: only gmc_decode does that.
  */
 size_t gmc_attend_workspace_size(const gmc_kv_cache* cache, int H, int T);
 int gmc_attend(const gmc_kv_cache* cache, const gmc_attn* attn, const void* q,

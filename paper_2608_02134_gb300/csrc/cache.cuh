@@ -236,7 +236,7 @@ struct DecodeArgs {
   Div by_ps;
 };
 int sm_count();  // of the current device
-size_t decode_workspace(const KV&, int dtype, int H);
+size_t decode_workspace(const KV&, int dtype, int H, bool scores = true);
 cudaError_t launch_decode_fp4(const DecodeArgs&, cudaStream_t, int* launches);
 cudaError_t launch_decode(DecodeArgs a, int dtype, void* ws, cudaStream_t, int* launches);
 

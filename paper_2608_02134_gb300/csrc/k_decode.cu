@@ -533,7 +533,10 @@ cudaError_t decode_f32(int heads, const DecodeArgs& a, cudaStream_t st, int* lau
 
 }  // namespace
 
-size_t decode_workspace(const KV& c, int dtype, int H) { return decode_carve(c, dtype, H).all; }
+size_t decode_workspace(const KV& c, int dtype, int H, bool scores) {
+  const DecodeWs w = decode_carve(c, dtype, H);
+  return scores ? w.all : w.logits;
+}
 
 cudaError_t launch_decode(DecodeArgs a, int dtype, void* ws, cudaStream_t st, int* launches) {
   const int hm = heads_per_launch(dtype, a.G, a.c.d), dp = decode_dp(a.c.d);

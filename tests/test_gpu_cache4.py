@@ -346,6 +346,10 @@ ATTEND = [
     ([900, 65], [3, 2], 100, 1, 128, 16, 200, 33),   # a tile a token
     ([700] * 6, [150] * 6, 14, 2, 128, 64, 0, 0),    # unpacked
     ([700] * 6, [150] * 6, 6, 2, 64, 48, 90, 7),
+    ([1], [1], 1, 1, 256, 16, 0, 0),                 # 256 channels: token by token
+    ([700, 0, 33, 5], [3, 0, 33, 9], 8, 2, 256, 48, 0, 0),
+    ([900, 64], [40, 3], 11, 1, 256, 16, 100, 33),   # two launches
+    ([257] * 8, [257] + [3] * 7, 2, 1, 256, 16, 0, 0),  # too many for that: unpacked
 ]
 
 
@@ -399,6 +403,22 @@ def test_attend_in_parts_that_fill_the_last_wave(window, sinks):
         ref, z, _, bound, size = A.attention(c.K[0], c.V[0], c.q[x], n - t + x, window, sinks)
         _close(out[x], ref, bound, A.tolerance(c.dt, 64, size, roundings=2), f"new token {x}")
         _close(lse[x], z, torch.ones_like(z), A.lse_tolerance(64, size) * 4, "lse")
+
+
+@pytest.mark.parametrize("d,T", [(64, 5), (128, 5), (256, 5), (256, 33), (128, 200)])
+def test_attend_with_and_without_offsets(d, T):
+    """Strided queries and outputs, rows behind the last sequence, and as many tokens of each."""
+    c = _h().Case4([400, 300, 350], 6, 2, d, 16, [T] * 3)
+    want, z = _attend(c, 60, 2)
+    q = torch.full((3 * T, 9, d + 8), math.nan, dtype=torch.bfloat16, device="cuda")
+    q[:, 1:7, :d] = c.q.cuda()
+    out = torch.full((6, 3 * T + 2, d), 7.0, dtype=torch.bfloat16, device="cuda").permute(1, 0, 2)
+    lse = torch.full((3 * T, 6), 7.0, device="cuda")
+    cache = c.cache(max_len=min(401, c.table.shape[1] * c.page))
+    _gmc().attend(cache, q[:, 1:7, :d], out[:3 * T], T, window=60, sinks=2, lse=lse)
+    torch.cuda.synchronize()
+    assert int(c.status.item()) == 0 and bool((out[3 * T:] == 7.0).all())
+    assert torch.equal(out[:3 * T], want[:-1]) and torch.equal(lse, z)
 
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (100, 3)])
