@@ -289,6 +289,16 @@ __global__ void __launch_bounds__(256) k_attend_join(AttnArgs a) {
   const long long step = part_row(a, 1, 0, 0) * a.H;
   const long long x = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (x >= step) return;
+  constexpr int U = 4;
+  auto load = [&](int y0, int q0, float4* v) {  // of four parts
+    const float* part = a.part + x * a.c.d + min(y0 + lane * 4, a.c.d - 4);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (q0 + u < a.splits)
+        v[u] = *reinterpret_cast<const float4*>(part + (q0 + u) * step * a.c.d);
+  };
+  float4 v[U];
+  load(0, 0, v);  // on their way while the row and the weights are looked up
   const long long token = x / a.H;
   const int hq = (int)(x - token * a.H), b = (int)(token / a.T), t = (int)(token - (long long)b * a.T);
   const NewRows nr = new_rows(a.q_offsets, b, a.rows, a.T, a.c.status);
@@ -306,22 +316,31 @@ __global__ void __launch_bounds__(256) k_attend_join(AttnArgs a) {
   for (int y0 = 0; y0 < a.c.d; y0 += 128) {
     const int y = y0 + lane * 4;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float* part = a.part + x * a.c.d + min(y, a.c.d - 4);
-#pragma unroll 4
-    for (int q = 0; q < a.splits; ++q) {
-      float4 v = *reinterpret_cast<const float4*>(part + q * step * a.c.d);
-      const float mq = __shfl_sync(FULL, ml.x, q), f = __shfl_sync(FULL, w, q);
-      if (mq == -INFINITY) v = make_float4(0.f, 0.f, 0.f, 0.f);  // without keys: wrote no row
-      s.x += f * v.x;
-      s.y += f * v.y;
-      s.z += f * v.z;
-      s.w += f * v.w;
+    for (int q0 = 0; q0 < a.splits; q0 += U) {
+      if (y0 + q0 > 0) load(y0, q0, v);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int q = q0 + u;
+        if (q >= a.splits) break;
+        const float mq = __shfl_sync(FULL, ml.x, q), f = __shfl_sync(FULL, w, q);
+        if (mq == -INFINITY) v[u] = make_float4(0.f, 0.f, 0.f, 0.f);  // no keys: wrote no row
+        s.x += f * v[u].x;
+        s.y += f * v[u].y;
+        s.z += f * v[u].z;
+        s.w += f * v[u].w;
+      }
     }
-    if (y < a.c.d) {
-      out[y] = from_f32<T>(s.x * inv);
-      out[y + 1] = from_f32<T>(s.y * inv);
-      out[y + 2] = from_f32<T>(s.z * inv);
-      out[y + 3] = from_f32<T>(s.w * inv);
+    if (y < a.c.d) {  // rows and heads lie 16 bytes apart
+      if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4*>(out + y) =
+            make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv);
+      } else {
+        const T z[4] = {from_f32<T>(s.x * inv), from_f32<T>(s.y * inv), from_f32<T>(s.z * inv),
+                        from_f32<T>(s.w * inv)};
+        uint2 both;
+        memcpy(&both, z, 8);
+        *reinterpret_cast<uint2*>(out + y) = both;
+      }
     }
   }
 }
