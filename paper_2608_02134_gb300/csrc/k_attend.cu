@@ -299,8 +299,12 @@ __global__ void __launch_bounds__(256) k_attend_join(AttnArgs a) {
   };
   float4 v[U];
   load(0, 0, v);  // on their way while the row and the weights are looked up
-  const long long token = x / a.H;
-  const int hq = (int)(x - token * a.H), b = (int)(token / a.T), t = (int)(token - (long long)b * a.T);
+  // divisions of 32 bits where the numbers are: 57,344 rows of two parts 25.2 us, with 64 bits 26.4
+  const bool small = step <= 0xffffffffLL;
+  const long long token = small ? (unsigned)x / (unsigned)a.H : x / a.H;
+  const int hq = (int)(x - token * a.H);
+  const int b = (int)(small ? (unsigned)token / (unsigned)a.T : token / a.T);
+  const int t = (int)(token - (long long)b * a.T);
   const NewRows nr = new_rows(a.q_offsets, b, a.rows, a.T, a.c.status);
   if (t >= nr.T) return;
   const long long row = nr.off + t;

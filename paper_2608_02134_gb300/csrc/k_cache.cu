@@ -286,29 +286,34 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
     e0 += total & 0xffff;
   }
   __syncthreads();  // this CTA's places are written
-  // pieces of a row: of 4 bits the codes' and, as one more, the scales (d / 16 bytes).  They wait
-  // for nothing of each other: 32 x 385 kept rows and their reading 16.2 us, where the scales went
-  // over before the next piece was loaded 18.1.
-  const int codes = FP4 ? a.src.d / 32 : a.src.d * esize / 16, rc = FP4 ? codes + 1 : codes;
+  // Pieces of a row; of 4 bits those of its codes.  Its scales (d / 16 bytes) are on their way
+  // before and written behind them, a row's key or value a thread (caches flushed: 385 of 1,027
+  // places of 32 sequences 10.8 us, where a piece's thread moved them 12.5; 4,096 of 16,004 14.5
+  // and 15.0).
+  const int rc = FP4 ? a.src.d / 32 : a.src.d * esize / 16;
   const int words = a.src.d / 64;  // of a row's scales: 1, 2 or 4
-  auto move = [&](int4& x, const char* from, bool scales) {
-    if (!FP4 || !scales || words == 4) {
-      x = *(const int4*)from;
+  auto load_z = [&](int row, int v) {
+    const char* from = (v ? a.src.v : a.src.k) + s->src_z[row];
+    int4 z = make_int4(0, 0, 0, 0);
+    if (words == 4) {
+      z = *(const int4*)from;
     } else if (words == 2) {
       const int2 y = *(const int2*)from;
-      x.x = y.x;
-      x.y = y.y;
+      z.x = y.x;
+      z.y = y.y;
     } else {
-      x.x = *(const int*)from;
+      z.x = *(const int*)from;
     }
+    return z;
   };
-  auto leave = [&](char* to, const int4& x, bool scales) {
-    if (!FP4 || !scales || words == 4)
-      *(int4*)to = x;
+  auto store_z = [&](int row, int v, const int4& z) {
+    char* to = (v ? a.dst.v : a.dst.k) + s->dst_z[row];
+    if (words == 4)
+      *(int4*)to = z;
     else if (words == 2)
-      *(int2*)to = make_int2(x.x, x.y);
+      *(int2*)to = make_int2(z.x, z.y);
     else
-      *(int*)to = x.x;
+      *(int*)to = z.x;
   };
   for (int q0 = p0; q0 < p1; q0 += EV_THREADS) {
     const int nr = min(EV_THREADS, p1 - q0);
@@ -328,6 +333,13 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
       }
     }
     __syncthreads();
+    int4 z[2];
+    if constexpr (FP4)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int y = tid + i * EV_THREADS;
+        if (y < 2 * nr && s->src[y >> 1] >= 0) z[i] = load_z(y >> 1, y & 1);
+      }
     const int total = nr * rc;
     constexpr int U = 4;
     for (int x = tid; x < total; x += EV_THREADS * U) {
@@ -339,23 +351,26 @@ __global__ void __launch_bounds__(EV_THREADS, 1) k_evict(EvictArgs a, int esize,
         at[u] = -1;
         if (y < total) {
           const int row = y / rc, z = (y - row * rc) * 16;
-          if (s->src[row] < 0) continue;
-          const bool last = FP4 && z == codes * 16;
-          const long long from = last ? s->src_z[row] : s->src[row] + z;
-          at[u] = last ? s->dst_z[row] : s->dst[row] + z;
-          move(kv[u], a.src.k + from, last);
-          move(vv[u], a.src.v + from, last);
+          if (s->src[row] >= 0) {
+            at[u] = s->dst[row] + z;
+            kv[u] = *(const int4*)(a.src.k + s->src[row] + z);
+            vv[u] = *(const int4*)(a.src.v + s->src[row] + z);
+          }
         }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (at[u] >= 0) {
-          const int y = x + u * EV_THREADS;
-          const bool last = FP4 && y % rc == codes;
-          leave(a.dst.k + at[u], kv[u], last);
-          leave(a.dst.v + at[u], vv[u], last);
+          *(int4*)(a.dst.k + at[u]) = kv[u];
+          *(int4*)(a.dst.v + at[u]) = vv[u];
         }
     }
+    if constexpr (FP4)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int y = tid + i * EV_THREADS;
+        if (y < 2 * nr && s->src[y >> 1] >= 0) store_z(y >> 1, y & 1, z[i]);
+      }
     __syncthreads();
   }
 }
