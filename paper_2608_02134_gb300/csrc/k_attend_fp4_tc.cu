@@ -241,12 +241,12 @@ __global__ void __launch_bounds__(Q_THREADS, 1) k_attend_fp4(AttnArgs a, Div by_
       int page, slot;
       bool run;
     };
-    const int odd = (a.c.ps & 15) ? -1 : 15;  // a run's first place is no multiple of 16
+    const bool runs = (a.c.ps & 15) == 0;  // 16 rows from a multiple of 16 on lie in one page
     auto look_up = [&](int x) {
       Place p = {0, -1, false};
       if (x >= turns) return p;
       int j = key0(x) + w * Q_ROWS;
-      p.run = (j & odd) == 0 && j + Q_ROWS <= key1(x);
+      p.run = runs && (j & 15) == 0 && j + Q_ROWS <= key1(x);
       if (!p.run) j += lane;
       if (p.run || (lane < Q_ROWS && j < key1(x))) {
         const int y = by_ps.of(j);
