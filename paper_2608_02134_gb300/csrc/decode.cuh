@@ -239,7 +239,10 @@ __device__ __forceinline__ void add_scores(const DecodeArgs& a, const Walk<DT>& 
       for (int g = 0; g < a.heads; ++g)
         s += exp2_fast(lg[(long long)x * a.hs + g] - ml[g].x) * ml[g].y;
     }
-    out[j] = (a.fresh && j == w.n - 1 ? 0.f : in[j]) + s;
+    // a turn of 32 may hold keys that are not seen: a NaN of the others' sum is not theirs
+    const bool seen = DT != 32 || sees(w.n - 1, j, a.window, a.sinks);
+    const float old = a.fresh && j == w.n - 1 ? 0.f : in[j];
+    out[j] = seen ? old + s : old;
   }
   if (in != out)  // unseen keys keep what they had
     for (int j = w.seen.a + x0; j < w.seen.b0; j += step) out[j] = in[j];
