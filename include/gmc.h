@@ -549,7 +549,10 @@ int gmc_clients(const gmc_problem* prob, const gmc_params* params, const gmc_vie
  * gmc_cache_append, gmc_cache_append_rope and gmc_decode pack what they append;
  * all attention is over the values that the codes stand for, a decoded token's
  * own included.  Its products are exact in half precision (queries within 2^-39
- * of their row's largest value), weights are rounded to half.  gmc_attend reads
+ * of their row's largest value), weights are rounded to half: 2^-11 of a weight, of
+ * small ones 2^-32 of a largest, so N keys behind one that outweighs them lose at most
+ * N 2^-32 of the sum (where rows are unpacked, weights are rounded to bf16, 2^-8 of
+ * each; lse and scores count every weight unrounded).  gmc_attend reads
  * the codes itself for few tokens (d = 256: up to 16,384 of all sequences, where they
  * or their keys are not too many, token by token the way of gmc_decode); for more it
  * unpacks the seen rows to bf16 (which holds them exactly) in its workspace, which grows

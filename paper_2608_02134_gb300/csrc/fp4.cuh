@@ -143,6 +143,14 @@ __device__ __forceinline__ uint2 fp4_block(const uint4& v0, const uint4& v1, uin
   return make_uint2(s.codes(v0), s.codes(v1));
 }
 
+// Weights become halves.  They are 2^(x - m) of logits x, m a base FP4_UP below the maximum that
+// it was taken from, so that maximum's weight is 2^7 and a half loses 2^-32 of it at most where a
+// weight is small: a sum over N keys behind one that outweighs them N 2^-32 (taken against the
+// maximum itself N 2^-25, 0.3 % at 100,000 keys).  Above, halves reach to 2^16: m follows the
+// running maximum only once that lies FP4_ROOM above it.  Maxima are rounded up (of large logits
+// one rounding is more than that room), so no weight is beyond it.
+constexpr float FP4_UP = 7.f, FP4_ROOM = FP4_UP + 8.f;
+
 __device__ __forceinline__ void unpack_bf16(const uint4& v, float* x) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll

@@ -15,8 +15,8 @@
 //   O^T = V^T P^T: the rows are 16 channels, a thread's are consecutive again.  Here pairs are
 //   two keys' values of one channel, so the codes of two keys are interleaved first (4
 //   instructions for 16 codes).  P^T comes from S by a transposition in registers.  Weights
-//   are rounded to half (relative 2^-12, an eighth of the output's own rounding; below 2^-14 of
-//   the largest 2^-25 of it), their sum is the unrounded ones'.
+//   are rounded to half (relative 2^-11, an eighth of the output's own rounding; below 2^-21 of
+//   the largest 2^-32 of it, FP4_UP), their sum is the unrounded ones'.
 //
 // A turn is 32 keys from a multiple of 32 on.  Where they are all seen a warp copies their codes
 // and scales in straight runs, else row by row.
@@ -351,8 +351,8 @@ template <int DP, int NT> struct HeadsFp4 {
           }
       }
     }
-    // the maximum that weights are taken against follows the running one when that has grown
-    // by 2^8 (`room`: that much more as a sum of products): lanes only meet then
+    // the base that weights are taken against (FP4_UP below a maximum) follows the running maximum
+    // when that has grown by 2^8 (`room`: that much more as a sum of products): lanes only meet then
     float top[NT][2];
     bool grew = false;
 #pragma unroll
@@ -367,7 +367,7 @@ template <int DP, int NT> struct HeadsFp4 {
       for (int z = 0; z < NT; ++z)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          float mn = fmaxf(top[z][r] * factor[z][r], m[z][r]);
+          float mn = fmaxf(__fmul_ru(top[z][r], factor[z][r]) - FP4_UP, m[z][r]);
           mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 4));
           mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 8));
           mn = fmaxf(mn, __shfl_xor_sync(FULL, mn, 16));
@@ -379,7 +379,8 @@ template <int DP, int NT> struct HeadsFp4 {
             o[z][y][2 + r] *= f;
           }
           m[z][r] = mn;
-          room[z][r] = (mn + 8.f) / factor[z][r];
+          const float above = (mn + FP4_ROOM) / factor[z][r];
+          room[z][r] = fmaf(fabsf(above), -0x1p-22f, above);  // not more by two roundings
         }
     }
     uint32_t p[NT][2][2];  // weights: of group n the first and the second eight keys'
