@@ -634,7 +634,8 @@ int gmc_cache_append(const gmc_kv_cache* cache, const void* k_new, const void* v
  *   q           [rows][H][d], rows q_row_stride apart; NULL with H == 0
  *   out         as q, out_row_stride apart; may be q itself with the same stride, and
  *               overlaps nothing else.  Rows of no sequence are left alone.
- * rot a multiple of 16, with GMC_FP4 of 32 (GMC_ERR_UNSUPPORTED otherwise).  One launch.
+ * rot a multiple of 16, with GMC_FP4 of 32, and H * d at most 2^26 (GMC_ERR_UNSUPPORTED
+ * otherwise).  One launch.
  */
 typedef struct gmc_rope {
   const float* table;  /* DEVICE fp32 [max_pos][rot]: cosines, then sines; 16-byte aligned */

@@ -189,6 +189,8 @@ int gmc_cache_append_rope(const gmc_kv_cache* cache, const gmc_rope* rope,
   const bool rows3 = pairs != 0;
   if (rows3 && (pairs != n || !positions)) return GMC_ERR_ARG;
   if (rope->H > 0 && check_heads(cache, rope->H) != GMC_OK) return check_heads(cache, rope->H);
+  // k_append_rope counts a row's channels, and the pieces of a block's 64 rows, in 32 bits
+  if ((long long)rope->H * d > 1 << 26) return GMC_ERR_UNSUPPORTED;
   // pieces of 16 bytes hold whole pairs, of 4 bits whole blocks
   if (rope->rot % (cache->dtype == GMC_FP4 ? 32 : 16) != 0) return GMC_ERR_UNSUPPORTED;
   const int64_t dense = (int64_t)cache->Hkv * d, dense_q = (int64_t)rope->H * d;
