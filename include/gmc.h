@@ -557,7 +557,9 @@ int gmc_clients(const gmc_problem* prob, const gmc_params* params, const gmc_vie
  * or their keys are not too many, token by token the way of gmc_decode); for more it
  * unpacks the seen rows to bf16 (which holds them exactly) in its workspace, which grows
  * by B * cap * Hkv * d * 4 bytes, cap being max_len rounded up to 128, and goes on as
- * with bf16.
+ * with bf16.  That is 3.6 times the 4-bit rows of one layer, whatever the lengths and the
+ * window are; nothing in it is kept from one call to the next, so calls that follow one
+ * another on a stream, those of all layers, can share one workspace.
  */
 typedef struct gmc_kv_cache {
   int B;                     /* sequences, >= 1 */

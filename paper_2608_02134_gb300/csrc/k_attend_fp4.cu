@@ -132,8 +132,8 @@ int parts(const KV& c, int G, int T, long long most) {
 }
 
 // ---- d = 256: the new tokens one by one, as gmc_decode's sequences ---------------------------
-// The tensor cores' kernels have no room for 256 channels, and decode's reads the codes anyway.
-// Token t of sequence b becomes sequence b T + t: its tokens are those up to its place, its pages
+// The tensor cores' kernels are built for up to 128 channels; decode's takes 256 and reads the
+// codes, once for every token.  Token t of sequence b becomes sequence b T + t: its tokens are those up to its place, its pages
 // are the same.  Of ragged calls the queries move there and the outputs back.
 // Tokens of a launch: every warp of decode looks through their lengths (2,048 tokens on themselves
 // 1,413 us in one launch, 589 in eight).
